@@ -198,9 +198,9 @@ def _moved(c):
 # ---- the cache's form ---------------------------------------------------------------------------------------------------
 
 def _k_rows(codes, c):
-    """[..., blocks, dim/64, 16, 64] -> [..., tokens, dim]: a block's keys lie in halves of 64 channels, token by token."""
-    x = codes.movedim(-3, -2)
-    return x.reshape(*x.shape[:-4], -1, c["dim"])
+    """[..., blocks, dim/64, 4, 16, 16] -> [..., tokens, dim]: key (token i, channel 64 h + 16 g + l) lies at [h, g, i, l]."""
+    x = codes.movedim(-2, -4)
+    return x.reshape(*x.shape[:-5], -1, c["dim"])
 
 
 def _v_rows(codes, c):
@@ -211,8 +211,8 @@ def _v_rows(codes, c):
 
 
 def _k_lay(rows, c):
-    """[..., tokens, dim] -> [..., blocks, dim/64, 16, 64]."""
-    return rows.reshape(*rows.shape[:-2], -1, BLOCK, c["dim"] // 64, 64).movedim(-2, -3)
+    """[..., tokens, dim] -> [..., blocks, dim/64, 4, 16, 16]."""
+    return rows.reshape(*rows.shape[:-2], -1, BLOCK, c["dim"] // 64, 4, 16).movedim(-4, -2)
 
 
 def _v_lay(rows, c):
@@ -239,7 +239,7 @@ def _codes(x, e):
 
 def _shapes(c, pages):
     one = (c["layers"], pages, c["heads"], c["page"] // BLOCK, c["dim"] // 64)
-    return one + (16, 64), one + (4, 16, 4, 4)
+    return one + (4, 16, 16), one + (4, 16, 4, 4)
 
 
 def _pool(c, pages, g):
@@ -335,7 +335,7 @@ def _cached(s, table):
     c = s["case"]
     at = table.clamp(min=0).long()
     ex = torch.exp2(s["exps"][0][at].float())                                     # slots, pages, heads, blocks, 2
-    k = _floats(s["k"][0][at]) * ex[..., 0, None, None, None]
+    k = _floats(s["k"][0][at]) * ex[..., 0, None, None, None, None]
     v = _floats(s["v"][0][at]) * ex[..., 1, None, None, None, None, None]
     join = lambda x: x.transpose(1, 2).reshape(x.shape[0], c["heads"], -1, c["dim"])  # noqa: E731
     return join(_k_rows(k, c)), join(_v_rows(v, c))
@@ -536,7 +536,7 @@ def _token(s, slot, name, which, pool):
     page = s["table"][slot].long()[t // c["page"]].clamp(min=0)
     block, i = t % c["page"] // BLOCK, t % BLOCK
     if which == 0:
-        got = pool[0][page, :, block, d // 64, i, d % 64]
+        got = pool[0][page, :, block, d // 64, d % 64 // 16, i, d % 16]
     else:
         got = pool[0][page, :, block, d // 64, i // 4, d % 16, d % 64 // 16, i % 4]
     e = s["exps"][0][page, :, block, which].double()
