@@ -43,6 +43,7 @@ extern "C" {
 
 #define LESSDEC_DTYPE_F32 0 /* q/k/v, cache, weights and out are float   */
 #define LESSDEC_DTYPE_F16 1 /* q/k/v, cache, weights and out are IEEE half */
+#define LESSDEC_DTYPE_BF16 2 /* paged cache only: q/k/v and out are bfloat16 */
 
 /* flags */
 #define LESSDEC_FLAG_SPARSE_DENOM 1u /* H2O accumulates e^s over the sparse-only denominator
@@ -250,6 +251,139 @@ int lessdec_step_static(const lessdec_desc *desc, const void *q, const void *k, 
  */
 int lessdec_probe_stream_read(const void *buf, size_t bytes, int32_t waves, uint32_t *sink,
                               void *hip_stream);
+
+/*
+ * ---- Paged cache in 8 bits --------------------------------------------------------------------
+ *
+ * For sequences (or layers) whose tokens are kept: the full cache, or with `window` the cache of
+ * Lambda-masking without a low-rank state (Sec. 4, "Setup": the first `sinks` tokens and the `window`
+ * most recent ones; Sec. 3.1's plain sparse cache), beside the compressed one above.  The conventions
+ * at the top of this file hold here too.
+ *
+ * A pool of `pages` pages serves `slots` sequences.  A page holds page_tokens tokens of all `heads`
+ * key/value heads; the same page index is used in all `layers` layers, each of which has its own keys and values
+ * in it.  Row s of `table` names the pages of slot s in token order (-1: none), length[s] counts its
+ * tokens, refs[p] counts the table entries that name page p (0: free).  Several slots may share a page;
+ * lessdec_pages_reserve gives a slot a page of its own before it is written.
+ *
+ * A block is 16 consecutive tokens of a page and head.  An element is stored as an e4m3 code c (bias 7,
+ * largest finite value 448, no infinity) and stands for c * 2^e with one exponent e per block for its
+ * keys and one for its values: the least e >= -40 for which every finite magnitude written to the block is
+ * within 448 * 2^e, at most 40 (what is larger is held as +-448 * 2^40).  Codes are rounded to nearest, ties to
+ * even; what is not finite is held as NaN and does not count for e.  As e only takes powers of two, the
+ * cache is defined to the bit.  A block that goes on being filled keeps its exponent or raises it (the older codes
+ * are then rounded again); a block's first token starts it afresh.
+ * In memory, byte for byte (tokens 16 b + i of the page, channel d):
+ *   k_codes [layers][pages][heads][page_tokens/16][D/64][4][16][16]: channel d = 64 h + 16 g + l at [h][g][i][l]
+ *   v_codes [layers][pages][heads][page_tokens/16][D/64][4][16][4][4]: token i = 4 g + j, channel
+ *           d = 64 h + 16 t + l at [h][g][l][t][j]: one 16-byte piece is a matrix operand of four tokens
+ *   exps    [layers][pages][heads][page_tokens/16][2]: e of the keys, e of the values
+ *
+ * Row arguments (q, k, v, out) are packed over the slots: rows start[s] .. start[s+1] - 1 belong to slot s, start
+ * [slots+1] ascending; they are the slot's LAST start[s+1] - start[s] tokens, so row start[s] + i is the token at position
+ * length[s] - (start[s+1] - start[s]) + i.  Rows behind the last slot's are neither read nor written; a row whose position would be
+ * below 0 is not stored and sees nothing.
+ * length, table and refs change through lessdec_pages_reserve, _select, _compact and _reset alone; a slot ends, or starts again, by _select.
+ * A generation step: lessdec_pages_reserve (which advances length), lessdec_pages_copy, then for every layer
+ * lessdec_pages_append and lessdec_pages_attend.  All of it can be captured in a HIP graph: lengths, tables and plans are
+ * read on the device.  Whatever table, length, refs, start and the index arguments hold, every access stays inside the
+ * arrays (a page index outside the pool reads as no page, a length outside [0, table_len * page_tokens] and an
+ * entry of start outside [0, rows] as the nearer end).
+ */
+#define LESSDEC_MAX_SLOTS 4096
+#define LESSDEC_PAGE_BLOCK 16
+
+typedef struct lessdec_pages_desc {
+  int32_t slots, pages;           /* 1 <= slots <= LESSDEC_MAX_SLOTS; 1 <= pages < 2^28          */
+  int32_t page_tokens, table_len; /* a multiple of 16 up to 1024; entries of a table row, table_len * page_tokens <= 2^30 */
+  int32_t heads, head_dim;        /* key/value heads <= 1024; 64 or 128                         */
+  int32_t q_per_kv, layers;       /* query heads per key/value head (0 or 1: one), at most
+                                     LESSDEC_MAX_Q_PER_KV; layers <= 1024                      */
+  int32_t dtype;                  /* LESSDEC_DTYPE_F16 or _BF16: q, k, v, out                   */
+  int32_t sinks, window;          /* a row at position p sees the tokens j <= p with j > p - window or
+                                     j < sinks; window = 0: all j <= p                       */
+  float scale;                    /* of the scores; 0: 1 / sqrt(D)                             */
+  uint8_t *k_codes, *v_codes;     /* 16-byte aligned                                           */
+  int8_t *exps;                   /* 2-byte aligned                                            */
+  int32_t *table, *length, *refs; /* [slots][table_len], [slots], [pages]                      */
+  void *workspace;                /* >= lessdec_pages_workspace_bytes(), 256-byte aligned; scratch without
+                                     conditions on what it holds.  Calls that share one must be ordered by a stream */
+  size_t workspace_bytes;
+} lessdec_pages_desc;
+
+/*
+ * Bytes of scratch: for lessdec_pages_attend with up to max_rows rows and the other calls.  Never
+ * falls with max_rows.  Host only; 0 if the shape fields are invalid.
+ */
+size_t lessdec_pages_workspace_bytes(const lessdec_pages_desc *desc, int32_t max_rows);
+
+/* Every slot empty, every page free. */
+int lessdec_pages_reset(const lessdec_pages_desc *desc, void *hip_stream);
+
+/*
+ * Room for n_new[s] more tokens in every slot ([slots], <= 0: none): length[s] grows by granted[s] ([slots] or NULL, another array than
+ * n_new), which is n_new[s] or 0.  For each slot that wants tokens
+ *  - with `window`: pages that hold only tokens which no row at position >= length[s] (as it was) sees are let go;
+ *  - if its last page is partly filled and other slots still share it, the slot gets a page of its own in its place (the last of
+ *    the sharers that write keeps the page if no one else has it) and the pair of pages goes on the plan;
+ *  - pages for the new tokens.
+ * Free pages are handed out in ascending order to the slots in ascending order.  A slot that would outgrow its
+ * table row is passed over; where the free pages do not suffice for a slot, neither it nor a later one gets any.
+ * plan: [1 + 2 slots]: the number of pairs, then (from, to) by slot; to be carried out by
+ * lessdec_pages_copy before the slots are appended to.
+ */
+int lessdec_pages_reserve(const lessdec_pages_desc *desc, const int32_t *n_new, int32_t *granted, int32_t *plan,
+                          void *hip_stream);
+
+/*
+ * Forks, reorders and frees: slot s becomes a copy of what slot from[s] was before the call ([slots]; s itself:
+ * stays; -1: becomes empty; any other value outside [0, slots): stays).  Pages are shared, no token moves.
+ */
+int lessdec_pages_select(const lessdec_pages_desc *desc, const int32_t *from, void *hip_stream);
+
+/*
+ * Moves the pages in use to the front of the pool: with U of them, those at index >= U take, in ascending order, the places of the free
+ * ones below U.  plan: [1 + 2 (pages / 2)], as above, to be carried out before anything else writes to the pool.
+ */
+int lessdec_pages_compact(const lessdec_pages_desc *desc, int32_t *plan, void *hip_stream);
+
+/*
+ * Carries out a plan of at most max_pairs pairs in all layers: page `to` gets what page `from` holds.  No `to` may occur twice
+ * or be a `from` (which holds for the plans of the two calls above); pairs outside the pool are passed over.
+ */
+int lessdec_pages_copy(const lessdec_pages_desc *desc, const int32_t *plan, int32_t max_pairs, void *hip_stream);
+
+/*
+ * Keys and values of the slots' last tokens into a layer of the cache.  k, v: [rows][heads][D] dtype, 16-byte aligned, row_stride
+ * elements from a row to the next (0: packed; a multiple of 8, at least heads * D).  Tokens on pages that the table does not
+ * name are passed over.
+ */
+int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const void *k, const void *v, int64_t row_stride,
+                         const int32_t *start, int32_t rows, void *hip_stream);
+
+/*
+ * Attention of the slots' last tokens over a layer of the cache (their own keys and values among it: append comes first):
+ *   out = sum_j e^{s_j} v_j / sum_j e^{s_j},  s_j = scale * q.k_j,  over the tokens that the row sees.
+ * q, out: [rows][heads * q_per_kv][D] dtype, 16-byte aligned (head h's query heads in a row, as above), q_stride elements from
+ * a row of q to the next (0: packed; a multiple of 8, at least heads * q_per_kv * D).
+ * lse: [rows][heads * q_per_kv] or NULL, ln sum_j e^{s_j}.
+ * max_new: no slot has more rows than this; rows of one that does may be left unwritten.
+ * A row that sees nothing, or only scores of -inf, gives zeros and an lse of -inf.  What a token that a row does not see holds, NaN among
+ * it, does not reach that row.
+ * Scores, softmax statistics and sums are fp32; the weights are rounded to fp16 for the product with the values (a relative
+ * error of 2^-11 at most in each, down to 2^-28 of the row's largest contribution).
+ */
+int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t q_stride, void *out, float *lse,
+                         const int32_t *start, int32_t rows, int32_t max_new, void *hip_stream);
+
+/*
+ * The values that a layer of the cache holds, e.g. for lessdec_prefill, when a sequence goes over to the compressed cache.
+ * slots: [n], n <= 65535.  K, V: [n][heads][count][D] dtype, 16-byte aligned: tokens first .. first + count - 1 of
+ * slots[i], counted from the slot's end if first < 0 (-count: its last count tokens).  Tokens that the slot does not
+ * have (or no longer has) and slots outside [0, slots) give zeros; what exceeds dtype's largest finite value gives that value.
+ */
+int lessdec_pages_read(const lessdec_pages_desc *desc, int32_t layer, const int32_t *slots, int32_t n, int32_t first,
+                       int32_t count, void *K, void *V, void *hip_stream);
 
 /* Static message for a return code. */
 const char *lessdec_strerror(int code);

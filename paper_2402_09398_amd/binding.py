@@ -13,7 +13,7 @@ from pathlib import Path
 _HERE = Path(__file__).resolve().parent
 LIB_PATH = _HERE / "liblessdec.so"
 
-DTYPE_F32, DTYPE_F16 = 0, 1
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 FLAG_SPARSE_DENOM = 1
 FLAG_LAMBDA = 2
 FLAG_PROMPT_STEPWISE = 4
@@ -22,7 +22,9 @@ STATIC_SCRATCH_BYTES = 4 << 20
 
 EXPORTS = ("lessdec_workspace_bytes", "lessdec_state_reset", "lessdec_state_sync", "lessdec_prefill", "lessdec_step", "lessdec_step_features", "lessdec_step_attend", "lessdec_step_static",
            "lessdec_probe_stream_read", "lessdec_step_launches",
-           "lessdec_strerror", "lessdec_budget_tokens")
+           "lessdec_strerror", "lessdec_budget_tokens",
+           "lessdec_pages_workspace_bytes", "lessdec_pages_reset", "lessdec_pages_reserve", "lessdec_pages_select",
+           "lessdec_pages_compact", "lessdec_pages_copy", "lessdec_pages_append", "lessdec_pages_attend", "lessdec_pages_read")
 
 
 class LessdecError(RuntimeError):
@@ -42,6 +44,18 @@ class Desc(C.Structure):
         ("pend_slot", C.c_void_p), ("pend_v", C.c_void_p), ("pend_psi", C.c_void_p),
         ("Wq1", C.c_void_p), ("Wq2", C.c_void_p),
         ("Wk1", C.c_void_p), ("Wk2", C.c_void_p), ("Wk3", C.c_void_p),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class PagesDesc(C.Structure):
+    """Mirror of struct lessdec_pages_desc."""
+    _fields_ = [
+        ("slots", C.c_int32), ("pages", C.c_int32), ("page_tokens", C.c_int32), ("table_len", C.c_int32),
+        ("heads", C.c_int32), ("head_dim", C.c_int32), ("q_per_kv", C.c_int32), ("layers", C.c_int32),
+        ("dtype", C.c_int32), ("sinks", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+        ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("exps", C.c_void_p),
+        ("table", C.c_void_p), ("length", C.c_void_p), ("refs", C.c_void_p),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
@@ -81,6 +95,15 @@ def lib():
         L.lessdec_strerror.argtypes = [C.c_int]
         L.lessdec_budget_tokens.restype = C.c_int32
         L.lessdec_budget_tokens.argtypes = [C.c_double, C.c_int32]
+        L.lessdec_pages_workspace_bytes.restype = C.c_size_t
+        L.lessdec_pages_workspace_bytes.argtypes = [C.POINTER(PagesDesc), C.c_int32]
+        i32, ptr = C.c_int32, C.c_void_p
+        for name, args in (("reset", [ptr]), ("reserve", [ptr] * 4), ("select", [ptr] * 2), ("compact", [ptr] * 2),
+                           ("copy", [ptr, i32, ptr]), ("append", [i32, ptr, ptr, C.c_int64, ptr, i32, ptr]),
+                           ("attend", [i32, ptr, C.c_int64, ptr, ptr, ptr, i32, i32, ptr]),
+                           ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr])):
+            f = getattr(L, "lessdec_pages_" + name)
+            f.restype, f.argtypes = C.c_int, [C.POINTER(PagesDesc)] + args
         _lib = L
     return _lib
 

@@ -1,0 +1,370 @@
+// Bookkeeping of the paged cache: making room, forking, freeing, compacting, and the copies that these ask for.
+//
+// Tables, lengths and reference counts live on the device, so that a generation step can be captured in a graph; everything here
+// but the copy touches a few bytes a slot or page and is bound by the latency of its dependent loads.  What has an order
+// (which free page goes to which slot) is settled by prefix sums over slots and pages in one workgroup, never by the order in
+// which atomics arrive: the same state gives the same pages every time.  Counts change by integer atomics, which commute.
+#include "lessdec_pages.h"
+
+namespace lessdec {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / kWave;
+constexpr int kSpan = kWave * 16;                    // pages that a wave looks at in one turn: sixteen ballots
+constexpr int kMaxSlots = LESSDEC_MAX_SLOTS, kTurns = kMaxSlots / kThreads;
+
+// refs are changed by atomics, which work in the L2: read there, past this compute unit's own cache
+__device__ inline int count_of(const int *refs, int p)
+{
+  return __hip_atomic_load(refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// sum over the threads before this one; total: over all of them
+template <typename T>
+__device__ inline T scan_exclusive(T x, T *shared, T &total)
+{
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T upto = x;
+  for (int d = 1; d < kWave; d <<= 1) {
+    const T y = __shfl_up(upto, d, kWave);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();
+  if (lane == 63) shared[wave] = upto;
+  __syncthreads();
+  T before = 0;
+  total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w == wave) before = total;
+    total += shared[w];
+  }
+  return before + upto - x;
+}
+
+__global__ void reset_kernel(Pages c)
+{
+  const long n = (long)c.slots * c.table_len, at = (long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long stride = (long)gridDim.x * blockDim.x;
+  for (long i = at; i < n; i += stride) c.table[i] = -1;
+  for (long i = at; i < c.pages; i += stride) c.refs[i] = 0;
+  for (long i = at; i < c.slots; i += stride) c.length[i] = 0;
+}
+
+// One workgroup.  free_list: [pages].
+__global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n_new, int *granted, int *plan, int *free_list)
+{
+  __shared__ int open_page[kMaxSlots];               // the shared page that the slot goes on filling, or -1
+  __shared__ int upto[kMaxSlots];                    // pages needed by the slots up to this one
+  __shared__ int want[kMaxSlots];                    // pages needed by this one
+  __shared__ long sums[kWaves];
+  __shared__ int page_sums[kWaves], pairs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pt = c.page_tokens;
+  const long room = (long)c.table_len * pt;
+  if (tid == 0) pairs = 0;
+
+  // pages behind the window: from the newest down to the last that was let go, 64 at a time
+  if (c.window > 0) {
+    const int a = (int)(((long)c.sinks + pt - 1) / pt);
+    for (int s = wave; s < c.slots; s += kWaves) {
+      const int n = n_new[s], len = slot_length(c, s);
+      if (n <= 0 || len + (long)n > room || len < c.window) continue;
+      for (int j = (len - c.window + 1) / pt - 1; j >= a; j -= kWave) {
+        const int i = j - lane;
+        int *at = c.table + (size_t)s * c.table_len + i;
+        const int p = i >= a ? *at : -1;
+        if (p >= 0) {
+          if (p < c.pages) atomicSub(c.refs + p, 1);
+          *at = -1;
+        }
+        if (__ballot(p < 0)) break;
+      }
+    }
+    __syncthreads();
+  }
+
+  // what each slot needs; a thread has the slots tid, tid + kThreads, ..
+  int old_page[kTurns], pair[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int s = tid + t * kThreads;
+    old_page[t] = pair[t] = -1;
+    if (s >= c.slots) continue;
+    const int n = n_new[s], len = slot_length(c, s);
+    if (n > 0 && len + (long)n <= room && len % pt) {
+      const int p = c.table[(size_t)s * c.table_len + len / pt];
+      old_page[t] = (unsigned)p < (unsigned)c.pages ? p : -1;
+    }
+    open_page[s] = old_page[t];
+  }
+  __syncthreads();
+  long before_turn = 0;
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    if (t * kThreads >= c.slots) break;
+    const int s = tid + t * kThreads;
+    int need = 0, copies = 0;
+    if (s < c.slots) {
+      const int n = n_new[s], len = slot_length(c, s);
+      if (n > 0 && len + (long)n <= room) {
+        int own = 0;                                 // a new page in the place of the partly filled one: shared, or not there
+        if (len % pt) {
+          const int p = old_page[t], sharers = p >= 0 ? count_of(c.refs, p) : 0;
+          if (sharers > 1) {
+            int before = 0;                          // slots before this one that write to the same page
+            for (int i = 0; i < s; ++i) before += open_page[i] == p;
+            copies = sharers - before > 1;
+          }
+          own = p < 0 || copies;
+        }
+        need = (int)((len + (long)n + pt - 1) / pt) - (len + pt - 1) / pt + own;
+      }
+    }
+    long all;                                        // both sums in one word: 2^12 slots of less than 2^27 pages each
+    const long x = scan_exclusive<long>(need | (long)copies << 48, sums, all) + before_turn;
+    before_turn += all;
+    if (copies) pair[t] = (int)(x >> 48);
+    if (s < c.slots) {
+      const long u = (x & ((1L << 48) - 1)) + need;
+      upto[s] = u < (1 << 30) ? (int)u : 1 << 30;
+      want[s] = need;
+    }
+  }
+  const long total = before_turn & ((1L << 48) - 1);
+
+  // the first free pages, in order
+  int found = 0;
+  for (long base = 0; base < c.pages && found < total; base += (long)kWaves * kSpan) {
+    unsigned long long free_of[16];
+    int count = 0;
+    for (int k = 0; k < 16; ++k) {
+      const long p = base + (long)wave * kSpan + k * kWave + lane;
+      free_of[k] = __ballot(p < c.pages && count_of(c.refs, (int)(p < c.pages ? p : 0)) == 0);
+      count += __popcll(free_of[k]);
+    }
+    __syncthreads();
+    if (lane == 0) page_sums[wave] = count;
+    __syncthreads();
+    int at = found;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) at += page_sums[w];
+      found += page_sums[w];
+    }
+    for (int k = 0; k < 16; ++k) {
+      const int mine = at + __popcll(free_of[k] & ((1ull << lane) - 1));
+      if (free_of[k] >> lane & 1) free_list[mine] = (int)(base + (long)wave * kSpan + k * kWave + lane);
+      at += __popcll(free_of[k]);
+    }
+  }
+  __syncthreads();                                   // free_list and want, upto
+
+  // tables: by the slot's thread where few pages are wanted, else by a wave
+  auto take = [&](int s, int j, int need, int end) {
+    const int p = free_list[upto[s] - need + j];
+    c.table[(size_t)s * c.table_len + end - need + j] = p;
+    c.refs[p] = 1;
+  };
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int s = tid + t * kThreads;
+    if (s >= c.slots) continue;
+    const int n = n_new[s], len = slot_length(c, s), need = want[s];
+    const bool wants = n > 0 && len + (long)n <= room, fits = wants && upto[s] <= found;
+    if (granted) granted[s] = fits ? n : 0;
+    if (!fits) {
+      want[s] = 0;
+      continue;
+    }
+    const int end = (int)((len + (long)n + pt - 1) / pt);
+    if (need <= 4)
+      for (int j = 0; j < need; ++j) take(s, j, need, end);
+    if (pair[t] >= 0) {
+      atomicSub(c.refs + old_page[t], 1);
+      plan[1 + 2 * pair[t]] = old_page[t];
+      plan[2 + 2 * pair[t]] = free_list[upto[s] - need];
+      atomicMax(&pairs, pair[t] + 1);
+    }
+  }
+  __syncthreads();
+  for (int base = 0; base < c.slots; base += kThreads) {
+    const int mine = base + lane * kWaves + wave;    // neighbours to different waves
+    unsigned long long many = __ballot(mine < c.slots && want[mine < c.slots ? mine : 0] > 4);
+    for (; many; many &= many - 1) {
+      const int s = base + (__ffsll(many) - 1) * kWaves + wave, need = want[s];
+      const int end = (int)((slot_length(c, s) + (long)n_new[s] + pt - 1) / pt);
+      for (int j = lane; j < need; j += kWave) take(s, j, need, end);
+    }
+  }
+  if (tid == 0) plan[0] = pairs;
+  __syncthreads();                                   // lengths are read up to here
+  for (int s = tid; s < c.slots; s += kThreads) {
+    const int n = n_new[s], len = slot_length(c, s);
+    if (n > 0 && len + (long)n <= room && upto[s] <= found) c.length[s] = len + n;
+  }
+}
+
+// A workgroup has some columns of the table, all slots of them, so that every old entry is read before one is written; the
+// last workgroup has the lengths.
+__global__ __launch_bounds__(256) void select_kernel(Pages c, const int *from, int columns)
+{
+  extern __shared__ int old[];
+  const bool lengths = blockIdx.x == gridDim.x - 1;
+  const int wide = lengths ? 1 : columns, base = blockIdx.x * columns;
+  for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
+    const int s = i / wide, j = base + i % wide;
+    old[i] = lengths ? c.length[s] : j < c.table_len ? c.table[(size_t)s * c.table_len + j] : -1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
+    const int s = i / wide, j = base + i % wide, f = from[s];
+    if (f == s || f < -1 || f >= c.slots) continue;
+    const int was = old[i], now = f < 0 ? (lengths ? 0 : -1) : old[f * wide + i % wide];
+    if (was == now) continue;
+    if (lengths) {
+      c.length[s] = now;
+    } else if (j < c.table_len) {
+      c.table[(size_t)s * c.table_len + j] = now;
+      if ((unsigned)was < (unsigned)c.pages) atomicSub(c.refs + was, 1);
+      if ((unsigned)now < (unsigned)c.pages) atomicAdd(c.refs + now, 1);
+    }
+  }
+}
+
+// One workgroup.  moved[p], p >= pages in use: where page p goes (-1: nothing there); moved[0]: pages in use.
+__global__ __launch_bounds__(kThreads) void compact_kernel(Pages c, int *plan, int *moved)
+{
+  __shared__ int sums[kWaves], sums2[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int mine = 0;
+  for (long p = tid; p < c.pages; p += kThreads) mine += c.refs[p] != 0;
+  int used;
+  scan_exclusive<int>(mine, sums, used);
+  int sources = 0, places = 0;
+  for (long base = 0; base < c.pages; base += (long)kWaves * kSpan) {
+    unsigned long long in_use[16];
+    int above = 0, below = 0;
+    for (int k = 0; k < 16; ++k) {
+      const long first = base + (long)wave * kSpan + k * kWave, p = first + lane;
+      in_use[k] = __ballot(p < c.pages && c.refs[p < c.pages ? p : 0] != 0);
+      const unsigned long long high = __ballot(p >= used), low = __ballot(p < used);
+      above += __popcll(in_use[k] & high);
+      below += __popcll(~in_use[k] & low);
+    }
+    __syncthreads();
+    if (lane == 0) { sums[wave] = above; sums2[wave] = below; }
+    __syncthreads();
+    int a = sources, b = places;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) { a += sums[w]; b += sums2[w]; }
+      sources += sums[w];
+      places += sums2[w];
+    }
+    for (int k = 0; k < 16; ++k) {
+      const long p = base + (long)wave * kSpan + k * kWave + lane;
+      const unsigned long long from = in_use[k] & __ballot(p >= used), to = ~in_use[k] & __ballot(p < used);
+      const unsigned long long below_me = (1ull << lane) - 1;
+      if (from >> lane & 1) plan[1 + 2 * (a + __popcll(from & below_me))] = (int)p;
+      else if (p >= used && p < c.pages) moved[p] = -1;
+      if (to >> lane & 1) plan[2 + 2 * (b + __popcll(to & below_me))] = (int)p;
+      a += __popcll(from);
+      b += __popcll(to);
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < sources; i += kThreads) {
+    const int p = plan[1 + 2 * i], to = plan[2 + 2 * i];
+    c.refs[to] = c.refs[p];
+    c.refs[p] = 0;
+    moved[p] = to;
+  }
+  if (tid == 0) {
+    plan[0] = sources;
+    if (used > 0) moved[0] = used;
+  }
+}
+
+__global__ void rename_kernel(Pages c, const int *moved)
+{
+  const long n = (long)c.slots * c.table_len;
+  const int used = moved[0];
+  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long)gridDim.x * blockDim.x) {
+    const int p = c.table[i];
+    if ((unsigned)p < (unsigned)c.pages && p >= used) c.table[i] = moved[p];
+  }
+}
+
+// 16 KiB of a page's keys or values to a workgroup at a time, 64 bytes a thread in flight.
+constexpr int kPiece = 16384;
+__global__ __launch_bounds__(256) void copy_kernel(Pages c, int layers, const int *plan, int max_pairs)
+{
+  const int n = plan[0] < max_pairs ? plan[0] : max_pairs;
+  const long page = (long)c.heads * c.page_tokens * c.head_dim, scales = (long)c.heads * page_blocks(c);
+  const int pieces = (int)((page + kPiece - 1) / kPiece);
+  const long total = (long)(n > 0 ? n : 0) * layers * pieces;
+  for (long item = blockIdx.x; item < total; item += gridDim.x) {
+    const int piece = (int)(item % pieces), layer = (int)(item / pieces % layers), pair = (int)(item / pieces / layers);
+    const int from = plan[1 + 2 * pair], to = plan[2 + 2 * pair];
+    if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages) continue;
+    const long a = ((long)layer * c.pages + from) * page, b = ((long)layer * c.pages + to) * page;
+    uint4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const long at = (long)piece * kPiece + (i / 2) * 4096 + threadIdx.x * 16;
+      if (at < page) x[i] = *reinterpret_cast<const uint4 *>((i & 1 ? c.v : c.k) + a + at);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const long at = (long)piece * kPiece + (i / 2) * 4096 + threadIdx.x * 16;
+      if (at < page) *reinterpret_cast<uint4 *>((i & 1 ? c.v : c.k) + b + at) = x[i];
+    }
+    if (piece == 0) {
+      const unsigned short *e = reinterpret_cast<const unsigned short *>(c.exps) + ((long)layer * c.pages + from) * scales;
+      unsigned short *f = reinterpret_cast<unsigned short *>(c.exps) + ((long)layer * c.pages + to) * scales;
+      for (long i = threadIdx.x; i < scales; i += 256) f[i] = e[i];
+    }
+  }
+}
+
+int blocks_for(long n, int threads, int most)
+{
+  const long b = (n + threads - 1) / threads;
+  return (int)(b < 1 ? 1 : b < most ? b : most);
+}
+
+}  // namespace
+
+hipError_t launch_pages_reset(const Pages &c, hipStream_t st)
+{
+  const long table = (long)c.slots * c.table_len;
+  reset_kernel<<<blocks_for(table > c.pages ? table : c.pages, 256, 2048), 256, 0, st>>>(c);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_reserve(const Pages &c, const int *n_new, int *granted, int *plan, int *free_list, hipStream_t st)
+{
+  reserve_kernel<<<1, kThreads, 0, st>>>(c, n_new, granted, plan, free_list);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_select(const Pages &c, const int *from, hipStream_t st)
+{
+  const int columns = c.slots <= 1024 ? 16 : 65536 / 4 / c.slots;      // 64 KiB of LDS at most; 64 bytes of a row where they fit
+  select_kernel<<<(c.table_len + columns - 1) / columns + 1, 256, (size_t)c.slots * columns * sizeof(int), st>>>(c, from, columns);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const Pages &c, int *plan, int *moved, hipStream_t st)
+{
+  compact_kernel<<<1, kThreads, 0, st>>>(c, plan, moved);
+  rename_kernel<<<blocks_for((long)c.slots * c.table_len, 256, 2048), 256, 0, st>>>(c, moved);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const Pages &c, int layers, const int *plan, int max_pairs, hipStream_t st)
+{
+  const long page = (long)c.heads * c.page_tokens * c.head_dim;
+  const long items = (long)max_pairs * layers * ((page + kPiece - 1) / kPiece);
+  copy_kernel<<<(unsigned)(items < 2048 ? items : 2048), 256, 0, st>>>(c, layers, plan, max_pairs);
+  return hipGetLastError();
+}
+
+}  // namespace lessdec

@@ -1,0 +1,764 @@
+// Paged cache: attention of the slots' last tokens over their cached ones.
+//
+// A row's output is sum_j 2^{t_j} c_j / sum_j 2^{t_j - e_j} with t_j = log2(e) scale 2^{k_j} (q . kc_j) + e_j, where kc_j, c_j are the
+// e4m3 codes of token j's key and value and k_j, e_j their blocks' exponents.  With the values' exponents in t, the product with the
+// values takes bare codes, which fp16 holds exactly, and weights 2^{t_j - M} <= 1 relative to the largest contribution so far (not
+// the largest score), so that fp16 holds the weights for any exponents: |e_j| <= 40 also keeps both sums within fp32.
+//
+// One pass over the tokens with the running maximum M and both sums (fp32).  M follows the maximum only where a weight would pass
+// 2^kSlack (a wave asks once per tile); until then the weights' range in fp16 above 1 takes it up and nothing is rescaled.
+//
+// Both kernels form the scores transposed, S^T = K Q^T, with tokens along the rows of a matrix tile: a lane's accumulator
+// registers are then tokens of one query column, and just those tokens are what the lane has to bring to the second product, O^T = V^T P^T,
+// so the weights never leave their registers.  A query column is a (row, query head of the group) pair: the heads of a group share the
+// cached keys and values that a tile has loaded.
+#include "lessdec_pages.h"
+
+namespace lessdec {
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kSlack = 8.f, kBase = 6.f;           // weights reach 2^(kBase + kSlack) = 2^14 (fp16: below 2^16), normal down to 2^-14
+
+template <bool BF16> struct Operand;
+template <> struct Operand<false> {
+  typedef half8 Vec;
+  __device__ static inline unsigned pair(unsigned w, bool high)
+  {
+    const half2v x = high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+    return __builtin_bit_cast(unsigned, x);
+  }
+  __device__ static inline f4 mma16(u4 a, u4 b, f4 c)
+  {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+  }
+  __device__ static inline f16v mma32(u4 a, u4 b, f16v c)
+  {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+  }
+  __device__ static inline unsigned short store(float x) { return __half_as_ushort(__float2half_rn(x)); }
+};
+template <> struct Operand<true> {
+  typedef bf8 Vec;
+  __device__ static inline unsigned pair(unsigned w, bool high)
+  {
+    const bf2v x = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
+    return __builtin_bit_cast(unsigned, x);
+  }
+  __device__ static inline f4 mma16(u4 a, u4 b, f4 c)
+  {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  }
+  __device__ static inline f16v mma32(u4 a, u4 b, f16v c)
+  {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  }
+  __device__ static inline unsigned short store(float x) { return __builtin_bit_cast(unsigned short, (__bf16)x); }
+};
+// eight codes as an operand
+template <bool BF16> __device__ inline u4 widen(unsigned a, unsigned b)
+{
+  return u4{Operand<BF16>::pair(a, false), Operand<BF16>::pair(a, true), Operand<BF16>::pair(b, false), Operand<BF16>::pair(b, true)};
+}
+__device__ inline unsigned half_pair(float a, float b)
+{
+  return __builtin_bit_cast(unsigned, half2v{(_Float16)a, (_Float16)b});
+}
+__device__ inline bool code_nan(unsigned w)          // any of four codes
+{
+  return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+}
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The blocks of 16 tokens that rows at positions lo .. hi see some token of, as a list: the first ones, then those of the window.
+struct Span {
+  int sinks, window, count;                          // blocks of the first tokens; the window's first block; blocks in all
+  __device__ inline int block(int i) const { return i < sinks ? i : i - sinks + window; }
+};
+__device__ inline Span span_of(const Pages &c, int lo, int hi)
+{
+  Span s = {0, 0, 0};
+  if (hi < 0) return s;
+  const int last = hi / kBlock;
+  if (c.window > 0 && lo >= c.window) {
+    const int w = (lo - c.window + 1) / kBlock, n = (int)min(((long)c.sinks + kBlock - 1) / kBlock, (long)last + 1);
+    if (w > n) { s.sinks = n; s.window = w; }
+  }
+  s.count = s.sinks + last - s.window + 1;
+  return s;
+}
+__device__ inline bool sees(const Pages &c, int p, int token)
+{
+  return token <= p && (c.window == 0 || token > p - c.window || token < c.sinks);
+}
+// whether rows at lo .. hi all see all of a block
+__device__ inline bool all_see(const Pages &c, int lo, int hi, int t0)
+{
+  return t0 + kBlock - 1 <= lo && (c.window == 0 || t0 > hi - c.window || t0 + kBlock <= c.sinks);
+}
+
+// ---- few rows a slot: up to 16 query columns -----------------------------------------------------------------------------
+//
+// Bound by the read of the cache.  The work is a list of steps, 128 tokens of a slot and head each, that is dealt out evenly to as many
+// workgroups as the chip holds at once, whatever the slots' lengths; every workgroup finds its part from the lengths.  A
+// step is 32 tokens for each of four waves, which stay apart until the workgroup leaves a (slot, head).  What a
+// workgroup has of a (slot, head) that it shares with others goes to memory and is joined by a second launch, in the order of the tokens.
+
+constexpr int kCols = 16, kStepBlocks = 8;
+constexpr int kWorkers = 768;
+
+__device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
+{
+  const Rows r = slot_rows(a.start, s, a.rows);
+  if (r.count == 0 || r.count * c.q_per_kv > kCols) return 0;
+  const int len = slot_length(c, s);
+  const int n = (span_of(c, len - r.count, len - 1).count + kStepBlocks - 1) / kStepBlocks;
+  return n > 0 ? n : 1;                              // (rows that see nothing are written too)
+}
+
+// Worker w's part [begin, end) of the steps, and where its step `at` lies: slot, and step among the slot's (head by head).
+struct Part {
+  long begin, end, per;
+  int slot;
+  long in_slot;
+};
+template <bool LAST>
+__device__ inline Part part_of(const Pages &c, const AttendArgs &a, int w, int workers)
+{
+  __shared__ long sums[4];
+  __shared__ int found;
+  __shared__ long found_at;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Part p;
+  long total = 0;
+  for (int round = 0; round < 2; ++round) {          // the sum first, then the slot that holds the step
+    long at = 0, want = 0;
+    if (round) {
+      p.per = (total + workers - 1) / workers;
+      p.begin = w * p.per;
+      p.end = p.begin + p.per < total ? p.begin + p.per : total;
+      if (p.begin >= p.end) return p;
+      want = LAST ? p.end - 1 : p.begin;
+    }
+    for (int base = 0; base < c.slots; base += 256) {
+      const int s = base + tid;
+      const long n = s < c.slots ? (long)steps_of(c, a, s) * c.heads : 0;
+      long upto = n;
+      for (int d = 1; d < kWave; d <<= 1) {
+        const long y = __shfl_up(upto, d, kWave);
+        if (lane >= d) upto += y;
+      }
+      __syncthreads();
+      if (lane == 63) sums[wave] = upto;
+      __syncthreads();
+      long before = at;
+      for (int i = 0; i < 4; ++i) {
+        if (i < wave) before += sums[i];
+        at += sums[i];
+      }
+      if (round && n > 0 && want >= before + upto - n && want < before + upto) {
+        found = s;
+        found_at = want - (before + upto - n);
+      }
+      if (round && at > want) break;
+    }
+    total = at;
+  }
+  __syncthreads();
+  p.slot = __builtin_amdgcn_readfirstlane(found);
+  p.in_slot = found_at;
+  return p;
+}
+
+constexpr int part_floats(int D) { return kCols * (D + 2); }
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
+{
+  constexpr int H = D / 64, T = D / 16, kRow = D + 4;
+  __shared__ float sums[4][kCols][kRow];
+  __shared__ float tops[4][kCols], totals[4][kCols];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int G = c.q_per_kv, per = page_blocks(c);
+  const Part part = part_of<false>(c, a, blockIdx.x, gridDim.x);
+  if (part.begin >= part.end) return;
+  int s = part.slot;
+  long in_slot = part.in_slot;
+  for (long pos = part.begin; pos < part.end;) {
+    const int steps = steps_of(c, a, s);
+    if (steps == 0) { ++s; in_slot = 0; continue; }
+    const int head = (int)(in_slot / steps), from = (int)(in_slot % steps);
+    const int to = (int)min((long)steps, from + (part.end - pos));
+
+    const Rows rows = slot_rows(a.start, s, a.rows);
+    const int len = slot_length(c, s), lo = len - rows.count, hi = len - 1, cols = rows.count * G;
+    const Span span = span_of(c, lo, hi);
+    const int p = lo + n / G;
+    u4 q[H][2];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        q[h][i] = u4{0, 0, 0, 0};
+        if (n < cols)
+          q[h][i] = reinterpret_cast<const u4 *>(a.q)[(rows.first + n / G) * (a.stride / 8) + (head * G + n % G) * (D / 8) + h * 8 + g * 2 + i];
+      }
+
+    // Two blocks a step.  Pages are looked up two steps ahead of their use, codes are requested one step ahead.
+    const int *table = c.table + (size_t)s * c.table_len;
+    auto page_at = [&](int step, int b) {
+      const int i = step * kStepBlocks + wave * 2 + b;
+      return step < to && i < span.count ? table[span.block(i) / per] : -1;
+    };
+    u4 k[2][H], v[2][H], k1[2][H], v1[2][H];
+    unsigned ex[2], ex1[2];
+    int t0[2], t01[2], page[2];
+    auto request = [&](int step) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int block = span.block(step * kStepBlocks + wave * 2 + b);
+        const bool there = (unsigned)page[b] < (unsigned)c.pages;
+        t01[b] = there ? block * kBlock : -1;
+        ex1[b] = 0;
+#pragma unroll
+        for (int h = 0; h < H; ++h) k1[b][h] = v1[b][h] = u4{0, 0, 0, 0};
+        if (there) {
+          const long at = ((long)page[b] * c.heads + head) * per + block % per;
+          ex1[b] = reinterpret_cast<const unsigned short *>(c.exps)[at];
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            k1[b][h] = reinterpret_cast<const u4 *>(c.k + at * (kBlock * D))[h * kWave + lane];
+            v1[b][h] = reinterpret_cast<const u4 *>(c.v + at * (kBlock * D))[h * kWave + lane];
+          }
+        }
+      }
+    };
+
+    f4 acc[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) acc[t] = f4{0, 0, 0, 0};
+    float top = kLowest, total = 0;
+    page[0] = page_at(from, 0); page[1] = page_at(from, 1);
+    request(from);
+    page[0] = page_at(from + 1, 0); page[1] = page_at(from + 1, 1);
+    for (int step = from; step < to; ++step) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        t0[b] = t01[b]; ex[b] = ex1[b];
+#pragma unroll
+        for (int h = 0; h < H; ++h) { k[b][h] = k1[b][h]; v[b][h] = v1[b][h]; }
+      }
+      request(step + 1);
+      page[0] = page_at(step + 2, 0); page[1] = page_at(step + 2, 1);
+      if (t0[0] < 0 && t0[1] < 0) continue;
+
+      float t[2][4];
+      float most = kLowest;
+      bool edge = false;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) x = Operand<BF16>::mma16(widen<BF16>(k[b][h][2 * i], k[b][h][2 * i + 1]), q[h][i], x);
+        const float factor = pow2((signed char)ex[b]) * c.scale_log2, ve = (float)(signed char)(ex[b] >> 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[b][i] = fmaf(x[i], factor, ve);
+        if (t0[b] < 0 || !all_see(c, lo, hi, t0[b])) {
+          edge = true;
+          unsigned keep = 0;                         // values that no row sees are taken out, so that nothing in them counts
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int token = t0[b] + 4 * g + i;
+            if (t0[b] < 0 || !sees(c, p, token)) t[b][i] = -__builtin_inff();
+            if (t0[b] >= 0 && token <= hi && (c.window == 0 || token > lo - c.window || token < c.sinks)) keep |= 255u << 8 * i;
+          }
+#pragma unroll
+          for (int h = 0; h < H; ++h) v[b][h] &= keep;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, t[b][i]);
+      }
+      if (__ballot(most > top + kSlack)) {
+        most = fmaxf(most, __shfl_xor(most, 16, kWave));
+        most = fmaxf(most, __shfl_xor(most, 32, kWave));
+        const float now = fmaxf(top, most), f = exp2_fast(top - now);
+        top = now;
+        total *= f;
+#pragma unroll
+        for (int i = 0; i < T; ++i) acc[i] *= f;
+      }
+      float w[2][4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        float part_sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[b][i] = exp2_fast(t[b][i] - (top - kBase));
+          part_sum += w[b][i];
+        }
+        total = fmaf(part_sum, pow2(-(signed char)(ex[b] >> 8)), total);
+      }
+      const u4 weights = {half_pair(w[0][0], w[0][1]), half_pair(w[0][2], w[0][3]), half_pair(w[1][0], w[1][1]), half_pair(w[1][2], w[1][3])};
+      // a NaN among values that only some of the rows see reaches those alone: 0 * NaN is NaN, so it is counted apart
+      bool apart = false;
+      if (edge && rows.count > 1) {
+        bool mine = false;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine |= code_nan(v[b][h][i]);
+        apart = __ballot(mine) != 0;
+      }
+      if (!apart) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[h * 4 + i] = Operand<false>::mma16(widen<false>(v[0][h][i], v[1][h][i]), weights, acc[h * 4 + i]);
+      } else {
+        half8 seen;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) seen[i] = t0[i / 4] >= 0 && sees(c, p, t0[i / 4] + 4 * g + i % 4) ? 1 : 0;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            half8 x = __builtin_bit_cast(half8, widen<false>(v[0][h][i], v[1][h][i])), bad;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              bad[j] = x[j] != x[j] ? 1 : 0;
+              x[j] = x[j] != x[j] ? 0 : x[j];
+            }
+            f4 &y = acc[h * 4 + i];
+            y = Operand<false>::mma16(__builtin_bit_cast(u4, x), weights, y);
+            const f4 count = Operand<false>::mma16(__builtin_bit_cast(u4, bad), __builtin_bit_cast(u4, seen), f4{0, 0, 0, 0});
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = count[j] > 0 ? __builtin_nanf("") : y[j];
+          }
+      }
+    }
+
+    // the four waves' sums, relative to the largest of their maxima
+    total += __shfl_xor(total, 16, kWave);
+    total += __shfl_xor(total, 32, kWave);
+    if (g == 0) { tops[wave][n] = top; totals[wave][n] = total; }
+    __syncthreads();
+    const float largest = fmaxf(fmaxf(tops[0][n], tops[1][n]), fmaxf(tops[2][n], tops[3][n])), f = exp2_fast(top - largest);
+    if (n < cols)
+#pragma unroll
+      for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
+    __syncthreads();
+    const bool whole = from == 0 && to == steps;
+    float *to_parts = a.parts + ((long)blockIdx.x * 2 + (from == 0)) * part_floats(D);
+    for (int i = threadIdx.x; i < cols * (D / 2); i += 256) {
+      const int col = i / (D / 2), d = i % (D / 2) * 2;
+      float t4 = fmaxf(fmaxf(tops[0][col], tops[1][col]), fmaxf(tops[2][col], tops[3][col])), l = 0, x = 0, y = 0;
+#pragma unroll
+      for (int wv = 0; wv < 4; ++wv) {
+        l += totals[wv][col] * exp2_fast(tops[wv][col] - t4);
+        x += sums[wv][col][d];
+        y += sums[wv][col][d + 1];
+      }
+      if (whole) {
+        const float r = l == 0.f ? 0.f : 1.f / l;
+        const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
+        reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
+            (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+        if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (t4 - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+      } else {
+        to_parts[col * D + d] = x;
+        to_parts[col * D + d + 1] = y;
+        if (d == 0) { to_parts[kCols * D + col] = t4; to_parts[kCols * (D + 1) + col] = l; }
+      }
+    }
+    __syncthreads();
+    pos += to - from;
+    in_slot += to - from;
+    if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
+  }
+}
+
+// The (slot, head) that begins in worker w's part and ends behind it.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void few_join_kernel(Pages c, AttendArgs a, int workers)
+{
+  const int G = c.q_per_kv, w = blockIdx.x;
+  const Part part = part_of<true>(c, a, w, workers);
+  if (part.begin >= part.end) return;
+  const int s = part.slot, steps = steps_of(c, a, s), head = (int)(part.in_slot / steps);
+  const long first = part.end - 1 - part.in_slot % steps, last = first + steps;
+  if (first < part.begin || last <= part.end) return;
+  const int n = (int)((last - 1) / part.per) - w + 1;
+  const Rows rows = slot_rows(a.start, s, a.rows);
+  const int cols = rows.count * G;
+  const float *base = a.parts + (long)w * 2 * part_floats(D);
+  auto from = [&](int i) { return base + (i == 0 ? 1 : 2 * i) * (long)part_floats(D); };
+  for (int i = threadIdx.x; i < cols * (D / 2); i += 256) {
+    const int col = i / (D / 2), d = i % (D / 2) * 2;
+    float top = kLowest;
+    for (int k = 0; k < n; ++k) top = fmaxf(top, from(k)[kCols * D + col]);
+    float l = 0, x = 0, y = 0;
+    for (int k = 0; k < n; ++k) {
+      const float *f = from(k), e = exp2_fast(f[kCols * D + col] - top);
+      l = fmaf(f[kCols * (D + 1) + col], e, l);
+      x = fmaf(f[col * D + d], e, x);
+      y = fmaf(f[col * D + d + 1], e, y);
+    }
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
+    reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
+        (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+    if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+// ---- many rows a slot ---------------------------------------------------------------------------------------------------
+//
+// Bound by the matrix and vector instructions.  A workgroup has 128 query columns of a (slot, head), 32 to a wave, and goes through the
+// tokens in tiles of 64: the codes of the tile after the next are on their way from memory, those of the next are widened once for
+// all four waves and put into the LDS in the order in which the matrix operands read them (whole lines, no padding), one
+// barrier a tile.  Where there are too few workgroups for the chip, several share a (slot, head, 128 columns), each some
+// of its tiles, and a second launch joins them.
+
+constexpr int kWide = 128, kTile = 64;               // columns and tokens
+constexpr int kEnough = 512;                         // workgroups: two to a compute unit
+
+__host__ __device__ inline long wide_items(int slots, int q_per_kv, long rows) { return rows * q_per_kv / kWide + slots; }
+inline int wide_splits(long items, long tokens)
+{
+  const long most = (tokens / kTile + 3) / 2;        // two tiles each, at least
+  const long n = items >= kEnough ? 1 : (kEnough + items - 1) / items;
+  return (int)(n < most ? n : most);
+}
+constexpr int wide_floats(int D) { return kWide * (D + 2); }
+
+// Column tile x of the list over all slots: floor(start[s] G / 128) + s leaves every slot as many as it can have.
+struct Columns { int slot, first, count, rows; };    // first column, columns of the slot in all; rows.count
+__device__ inline bool columns_of(const Pages &c, const AttendArgs &a, long x, Columns &t, Rows &rows)
+{
+  const int G = c.q_per_kv;
+  auto base = [&](int s) {
+    const int f = a.start[s];
+    return (long)(f < 0 ? 0 : f < a.rows ? f : a.rows) * G / kWide + s;
+  };
+  t.slot = __builtin_amdgcn_readfirstlane(last_slot_at(c.slots, x, base));
+  rows = slot_rows(a.start, t.slot, a.rows);
+  t.count = rows.count * G;
+  const long i = x - base(t.slot), n = (t.count + kWide - 1) / kWide;
+  if (i >= n || t.count <= kCols) return false;      // (up to 16 columns: the other kernel's)
+  t.first = (int)(n - 1 - i) * kWide;                // the longest first
+  return true;
+}
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, long items, int splits)
+{
+  constexpr int H = D / 64, KK = D / 16, OB = D / 32;
+  __shared__ __align__(16) u4 keys[2][kTile * D / 8], values[2][kTile * D / 8];
+  __shared__ int nan_tile[2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  const int G = c.q_per_kv, per = page_blocks(c);
+  // each die works through neighbouring items, head by head: what a (slot, head) has cached stays in its L2
+  const long total = items * c.heads * splits;
+  long id = blockIdx.x;
+  if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
+  const int split = (int)(id % splits);
+  const long item = id / splits;
+  const int head = (int)(item / items);
+  Columns t;
+  Rows rows;
+  if (!columns_of(c, a, item % items, t, rows)) return;
+  const int len = slot_length(c, t.slot), before = len - rows.count;
+  const int last_col = min(t.first + kWide, t.count) - 1;
+  const int lo = before + t.first / G, hi = before + last_col / G;
+  const Span span = span_of(c, lo, hi);
+  const int tiles = (span.count + 3) / 4, each = max(2, (tiles + splits - 1) / splits);
+  const int from = split * each, to = min(tiles, from + each);
+
+  // this wave's columns
+  const int col = t.first + wave * 32 + n;
+  const int wave_last = min(t.first + wave * 32 + 31, last_col);
+  const int wave_lo = before + (t.first + wave * 32) / G, wave_hi = before + wave_last / G;
+  const bool have = t.first + wave * 32 <= last_col;
+  const int row = rows.first + col / G, q_head = head * G + col % G, p = col <= last_col ? before + col / G : -1;
+  u4 q[KK];
+#pragma unroll
+  for (int k = 0; k < KK; ++k) {
+    q[k] = u4{0, 0, 0, 0};
+    if (col <= last_col) q[k] = reinterpret_cast<const u4 *>(a.q)[row * (a.stride / 8) + q_head * (D / 8) + k * 2 + h];
+  }
+
+  // Staging: a wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.
+  const int *table = c.table + (size_t)t.slot * c.table_len;
+  u4 kc[H], vc[H];
+  unsigned ex[4], ex1[4];
+  auto block_of = [&](int tile, int b, int &block) -> long {
+    const int i = tile * 4 + b;
+    if (tile >= to || i >= span.count) return -1;
+    block = span.block(i);
+    const int page = table[block / per];
+    return (unsigned)page < (unsigned)c.pages ? ((long)page * c.heads + head) * per + block % per : -1;
+  };
+  auto request = [&](int tile) {
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+      int block;
+      const long at = block_of(tile, H == 2 ? wave / 2 + 2 * j : wave, block);
+      kc[j] = vc[j] = u4{0, 0, 0, 0};
+      if (at >= 0) {
+        const int half = H == 2 ? wave % 2 : 0;
+        kc[j] = reinterpret_cast<const u4 *>(c.k + at * (kBlock * D))[half * kWave + lane];
+        vc[j] = reinterpret_cast<const u4 *>(c.v + at * (kBlock * D))[half * kWave + lane];
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      int block;
+      const long at = block_of(tile, b, block);
+      ex1[b] = at >= 0 ? reinterpret_cast<const unsigned short *>(c.exps)[at] : 0x10000u;
+    }
+  };
+  auto stage = [&](int tile) {
+    const int buf = tile & 1;
+    const int tok = lane & 15, g = lane >> 4;
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+      const int b = H == 2 ? wave / 2 + 2 * j : wave, half = H == 2 ? wave % 2 : 0;
+      // key operands: [32 tokens][16 channels][half of 8 channels][token]
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        keys[buf][(((b >> 1) * KK + half * 4 + g) * 2 + e) * 32 + (b & 1) * 16 + tok] = widen<BF16>(kc[j][2 * e], kc[j][2 * e + 1]);
+      // value operands: [block][32 channels][which eight of the 16 tokens][channel]: tokens 0-3, 8-11 and 4-7, 12-15
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = half * 64 + i * 16 + tok;
+        bad |= code_nan(vc[j][i]);
+        reinterpret_cast<uint2 *>(values[buf])[(((b * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1)] =
+            make_uint2(Operand<false>::pair(vc[j][i], false), Operand<false>::pair(vc[j][i], true));
+      }
+    }
+    if (bad) nan_tile[buf] = tile;
+  };
+
+  f16v acc[OB];
+#pragma unroll
+  for (int o = 0; o < OB; ++o) acc[o] = f16v{0};
+  float top = kLowest, sum = 0;
+  if (threadIdx.x < 2) nan_tile[threadIdx.x] = -1;
+  __syncthreads();
+  if (from < to) {
+    request(from);
+    stage(from);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) ex[b] = ex1[b];
+    request(from + 1);
+  }
+  for (int tile = from; tile < to; ++tile) {
+    __syncthreads();
+    const int buf = tile & 1;
+    unsigned next_ex[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) next_ex[b] = ex1[b];
+    if (tile + 1 < to) {
+      stage(tile + 1);
+      request(tile + 2);
+    }
+    int t0[4];
+    bool whole = true, some = false;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int i = tile * 4 + b;
+      t0[b] = i < span.count && ex[b] < 0x10000u ? span.block(i) * kBlock : -1;
+      whole &= t0[b] >= 0 && all_see(c, wave_lo, wave_hi, t0[b]);
+      some |= t0[b] >= 0 && t0[b] <= wave_hi && (c.window == 0 || t0[b] + kBlock > wave_lo - c.window || t0[b] < c.sinks);
+    }
+    if (have && some) {
+      f16v x[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        x[m] = f16v{0};
+#pragma unroll
+        for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+      }
+      float most = kLowest;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const float factor = pow2((signed char)ex[b]) * c.scale_log2, ve = (float)(signed char)(ex[b] >> 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float y = fmaf(x[b / 2][b % 2 * 8 + i], factor, ve);
+          if (!whole) {
+            const int token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2);
+            if (t0[b] < 0 || !sees(c, p, token)) y = -__builtin_inff();
+          }
+          x[b / 2][b % 2 * 8 + i] = y;
+          most = fmaxf(most, y);
+        }
+      }
+      if (__ballot(most > top + kSlack)) {
+        most = fmaxf(most, __shfl_xor(most, 32, kWave));
+        const float now = fmaxf(top, most), f = exp2_fast(top - now);
+        top = now;
+        sum *= f;
+#pragma unroll
+        for (int o = 0; o < OB; ++o) acc[o] *= f;
+      }
+      const float zero = top - kBase;
+      u4 weights[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        float part = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const float y = exp2_fast(x[b / 2][b % 2 * 8 + i] - zero), z = exp2_fast(x[b / 2][b % 2 * 8 + i + 1] - zero);
+          part += y + z;
+          weights[b][i / 2] = half_pair(y, z);
+        }
+        sum = fmaf(part, pow2(-(signed char)(ex[b] >> 8)), sum);
+      }
+      if (whole || nan_tile[buf] != tile) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][(b * OB + o) * 64 + lane], weights[b], acc[o]);
+      } else {
+        // a NaN among values that only some rows see: counted apart, since 0 * NaN is NaN
+#pragma unroll 1
+        for (int b = 0; b < 4; ++b) {
+          half8 seen;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) seen[i] = t0[b] >= 0 && sees(c, p, t0[b] + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
+#pragma unroll
+          for (int o = 0; o < OB; ++o) {
+            half8 y = __builtin_bit_cast(half8, values[buf][(b * OB + o) * 64 + lane]), bad;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              bad[i] = y[i] != y[i] ? 1 : 0;
+              y[i] = y[i] != y[i] ? 0 : y[i];
+            }
+            acc[o] = Operand<false>::mma32(__builtin_bit_cast(u4, y), weights[b], acc[o]);
+            const f16v count = Operand<false>::mma32(__builtin_bit_cast(u4, bad), __builtin_bit_cast(u4, seen), f16v{0});
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[o][i] = count[i] > 0 ? __builtin_nanf("") : acc[o][i];
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) ex[b] = next_ex[b];
+  }
+  sum += __shfl_xor(sum, 32, kWave);
+  if (splits > 1) {
+    float *part = a.parts + (item * splits + split) * wide_floats(D);
+    const int at = wave * 32 + n;
+    if (from < to)
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f4 *>(part + at * D + o * 32 + i * 8 + h * 4) = f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]};
+    if (h == 0) { part[kWide * D + at] = top; part[kWide * (D + 1) + at] = sum; }
+    return;
+  }
+  if (col > last_col) return;
+  const float r = sum == 0.f ? 0.f : 1.f / sum;
+  const long at = (long)row * c.heads * G + q_head;
+#pragma unroll
+  for (int o = 0; o < OB; ++o)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint2 y;
+      y.x = (unsigned)Operand<BF16>::store(acc[o][4 * i] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 1] * r) << 16;
+      y.y = (unsigned)Operand<BF16>::store(acc[o][4 * i + 2] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 3] * r) << 16;
+      reinterpret_cast<uint2 *>(a.out)[at * (D / 4) + o * 8 + i * 2 + h] = y;
+    }
+  if (a.lse && h == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(sum)) * 0.6931471805599453f;
+}
+
+// 32 columns of an item to a workgroup.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, long items, int splits)
+{
+  const int G = c.q_per_kv;
+  const long item = blockIdx.x;
+  const int head = (int)(item / items);
+  Columns t;
+  Rows rows;
+  if (!columns_of(c, a, item % items, t, rows)) return;
+  const float *base = a.parts + item * splits * wide_floats(D);
+  for (int i = threadIdx.x; i < 32 * (D / 2); i += 256) {
+    const int at = blockIdx.y * 32 + i / (D / 2), d = i % (D / 2) * 2, col = t.first + at;
+    if (col >= t.count) return;
+    float top = kLowest;
+    for (int k = 0; k < splits; ++k) top = fmaxf(top, base[(long)k * wide_floats(D) + kWide * D + at]);
+    float l = 0, x = 0, y = 0;
+    for (int k = 0; k < splits; ++k) {
+      const float *f = base + (long)k * wide_floats(D), m = f[kWide * D + at], e = exp2_fast(m - top);
+      if (m == kLowest) continue;                    // nothing seen there, nothing written
+      l = fmaf(f[kWide * (D + 1) + at], e, l);
+      x = fmaf(f[at * D + d], e, x);
+      y = fmaf(f[at * D + d + 1], e, y);
+    }
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
+    reinterpret_cast<unsigned *>(a.out)[to * (D / 2) + d / 2] =
+        (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+    if (a.lse && d == 0) a.lse[to] = l == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+template <bool BF16, int D>
+hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
+{
+  if (c.q_per_kv <= kCols) {
+    few_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a);
+    few_join_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a, kWorkers);
+  }
+  if ((long)a.max_new * c.q_per_kv > kCols) {
+    const long items = wide_items(c.slots, c.q_per_kv, a.rows);
+    const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
+    wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits), 256, 0, st>>>(c, a, items, splits);
+    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / 32), 256, 0, st>>>(c, a, items, splits);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows)
+{
+  size_t n = q_per_kv <= kCols ? (size_t)kWorkers * 2 * part_floats(head_dim) : 0;
+  if ((long)rows * q_per_kv > kCols) {
+    long items = wide_items(slots, q_per_kv, rows) * heads, fewest = wide_items(slots, q_per_kv, 0) * heads;
+    if (fewest < kEnough) {
+      // splits items: less than kEnough + items workgroups, for any number of rows up to this one
+      const long most = wide_splits(fewest, tokens), now = items < kEnough ? items : kEnough - 1;
+      long parts = now * most < kEnough + now ? now * most : kEnough + now;
+      const size_t wide = (size_t)parts * wide_floats(head_dim);
+      n = n > wide ? n : wide;
+    }
+  }
+  return n;
+}
+
+hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st)
+{
+  const bool bf16 = dtype == LESSDEC_DTYPE_BF16;
+  if (c.head_dim == 128) return bf16 ? attend<true, 128>(c, a, st) : attend<false, 128>(c, a, st);
+  return bf16 ? attend<true, 64>(c, a, st) : attend<false, 64>(c, a, st);
+}
+
+}  // namespace lessdec

@@ -1,0 +1,303 @@
+// Paged cache: keys and values into the cache (append) and back out of it (read).
+//
+// Both are bound by memory: a token of a head is 2 D elements of two bytes on one side and 2 D bytes on the other.  A wave has one
+// block of 16 tokens of one head, keys and values, so that the block's exponents are the wave's own reduction, nothing is
+// shared and no wave waits for another.
+#include "lessdec_pages.h"
+
+namespace lessdec {
+namespace {
+
+constexpr int kTop = 40;                             // exponents lie within +-kTop
+
+// Raw 16-bit elements as fp32.
+template <bool BF16> __device__ inline float element(unsigned short x)
+{
+  if constexpr (BF16) return __uint_as_float((unsigned)x << 16);
+  else return __half2float(__ushort_as_half(x));
+}
+template <bool BF16> __device__ inline unsigned short rounded(float x)
+{
+  if constexpr (BF16) {
+    const unsigned b = __float_as_uint(x);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;
+    return (unsigned short)((b + 0x7fffu + (b >> 16 & 1)) >> 16);
+  } else {
+    return __half_as_ushort(__float2half_rn(x));
+  }
+}
+
+__device__ inline unsigned magnitude(float x)        // bits of |x|, 0 where x is not finite
+{
+  const unsigned b = __float_as_uint(x) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0;
+}
+
+// The least e with x <= 448 * 2^e = 1.75 * 2^(e + 8), within +-kTop; x by its bits.
+__device__ inline int exponent_of(unsigned bits)
+{
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+  return e < -kTop ? -kTop : e < kTop ? e : kTop;
+}
+
+__device__ inline unsigned wave_max(unsigned x)
+{
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const unsigned y = __shfl_xor(x, d, kWave);
+    x = y > x ? y : x;
+  }
+  return x;
+}
+
+// x / 2^e for the conversion: at most 448 (more only at e = kTop), NaN where x is not finite
+__device__ inline float scaled(float x, float inverse)
+{
+  const float y = fminf(fmaxf(x * inverse, -448.f), 448.f);
+  return magnitude(x) || x == 0.f ? y : __builtin_nanf("");
+}
+__device__ inline unsigned four_codes(float a, float b, float c, float d)
+{
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// four codes, rounded again for an exponent that is larger by shift (factor = 2^-shift)
+__device__ inline unsigned again(unsigned w, float factor)
+{
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return four_codes(a[0] * factor, a[1] * factor, b[0] * factor, b[1] * factor);
+}
+
+constexpr int kRowPad = 16;                          // bytes behind a token's codes in the LDS: the four tokens of a group in other banks
+
+// Block b of a slot's new tokens: the wave's index less start[s] / 16 + 2 s, which leaves every slot as many waves as it can
+// touch blocks (count / 16 + 2) without a prefix sum over the slots.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
+{
+  constexpr int H = D / 64;
+  __shared__ __align__(16) unsigned char turned[4][kBlock * (D + kRowPad)];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y;
+  const long w = (long)blockIdx.x * 4 + wave;
+  auto base = [&](int s) {
+    const int f = a.start[s];
+    return (long)((f < 0 ? 0 : f < a.rows ? f : a.rows) / kBlock) + 2 * (long)s;
+  };
+  const int s = last_slot_at(c.slots, w, base);
+  const Rows r = slot_rows(a.start, s, a.rows);
+  const int len = slot_length(c, s), begin = len > r.count ? len - r.count : 0;
+  const int row0 = r.first + r.count - (len - begin);                  // row of the token at position begin
+  const long b = begin / kBlock + w - base(s);
+  if (r.count == 0 || b < 0 || b * kBlock >= len) return;
+  const int t0 = (int)b * kBlock;
+  const long block = block_index(c, s, head, (int)b);
+  if (block < 0) return;
+  const int off = begin > t0 ? begin - t0 : 0;                         // older tokens of the block
+
+  const int tok = lane & 15, g = lane >> 4;
+  const bool fresh = tok >= off && t0 + tok < len;
+  unsigned short *exps = reinterpret_cast<unsigned short *>(c.exps) + block;
+  uint4 *kb = reinterpret_cast<uint4 *>(c.k + block * (kBlock * D)) + lane, *vb = reinterpret_cast<uint4 *>(c.v + block * (kBlock * D)) + lane;
+  uint4 x[2][H][2];
+  const long row = (long)(row0 + t0 + tok - begin) * (a.stride / 8) + head * (D / 8);
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[which][h][i] = make_uint4(0, 0, 0, 0);
+        if (fresh) x[which][h][i] = reinterpret_cast<const uint4 *>(which ? a.v : a.k)[row + h * 8 + g * 2 + i];
+      }
+  uint4 old[H];
+  const bool mixed = off > 0 && 4 * g + 3 >= off && t0 + 4 * g < len;  // the lane's four tokens of a value piece are not all older
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    old[h] = make_uint4(0, 0, 0, 0);
+    if (mixed) old[h] = vb[h * kWave];
+  }
+  const unsigned was = off > 0 ? *exps : 0;
+
+  int e[2], shift[2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    unsigned m = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned word = (&x[which][h][i / 4].x)[i % 4];
+        const unsigned lo = magnitude(element<BF16>((unsigned short)word)), hi = magnitude(element<BF16>((unsigned short)(word >> 16)));
+        m = m > lo ? m : lo;
+        m = m > hi ? m : hi;
+      }
+    e[which] = exponent_of(wave_max(m));
+    shift[which] = 0;
+    if (off > 0) {
+      int before = (signed char)(which ? was >> 8 : was);
+      before = before < -kTop ? -kTop : before < kTop ? before : kTop;
+      if (e[which] > before) shift[which] = e[which] - before;
+      else e[which] = before;
+    }
+  }
+  if (lane == 0) *exps = (unsigned short)((e[0] & 255) | (e[1] & 255) << 8);
+
+  // codes of the lane's sixteen channels of a token
+  uint4 code[2][H];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float inverse = pow2(-e[which]);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned p = (&x[which][h][i / 2].x)[i % 2 * 2], q = (&x[which][h][i / 2].x)[i % 2 * 2 + 1];
+        (&code[which][h].x)[i] = four_codes(scaled(element<BF16>((unsigned short)p), inverse), scaled(element<BF16>((unsigned short)(p >> 16)), inverse),
+                                            scaled(element<BF16>((unsigned short)q), inverse), scaled(element<BF16>((unsigned short)(q >> 16)), inverse));
+      }
+  }
+
+  // keys: a lane's piece is one token's
+  if (fresh || off == 0) {                                             // (the rest of a new block: zeros)
+#pragma unroll
+    for (int h = 0; h < H; ++h) kb[h * kWave] = code[0][h];
+  } else if (shift[0] && tok < off) {
+    const float factor = pow2(-shift[0]);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      uint4 k = kb[h * kWave];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) (&k.x)[i] = again((&k.x)[i], factor);
+      kb[h * kWave] = k;
+    }
+  }
+
+  // values: a lane's piece is four channels of four tokens; the codes are turned in the LDS
+  unsigned char *mine = turned[wave];
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+    *reinterpret_cast<uint4 *>(mine + tok * (D + kRowPad) + h * 64 + g * 16) = code[1][h];
+  wave_lds_sync();
+  const bool rescale = off > 0 && shift[1] > 0;
+  if (off == 0 || mixed || rescale) {
+    const float factor = pow2(-shift[1]);
+    unsigned keep = 0;                                                 // bytes of tokens that are not new
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (4 * g + j < off || (off > 0 && t0 + 4 * g + j >= len)) keep |= 255u << 8 * j;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      if (rescale && !mixed) old[h] = vb[h * kWave];
+      uint4 v;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        unsigned word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          word |= (unsigned)mine[(4 * g + j) * (D + kRowPad) + h * 64 + t * 16 + (lane & 15)] << 8 * j;
+        unsigned before = (&old[h].x)[t];
+        if (rescale) before = again(before, factor);
+        (&v.x)[t] = (word & ~keep) | (before & keep);
+      }
+      vb[h * kWave] = v;
+    }
+  }
+}
+
+// A wave has a block of the cache and writes those of its tokens that are asked for.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void read_kernel(Pages c, ReadArgs a)
+{
+  constexpr int H = D / 64;
+  __shared__ __align__(16) unsigned char turned[4][kBlock * (D + kRowPad)];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y, i = blockIdx.z;
+  const int s = a.slots[i];
+  const bool there = (unsigned)s < (unsigned)c.slots;
+  const int len = there ? slot_length(c, s) : 0;
+  const long first = a.first >= 0 ? a.first : (long)len + a.first;
+  const long b = (first >> 4) + (long)blockIdx.x * 4 + wave;           // (floor: first may be negative)
+  if (b * kBlock >= first + a.count) return;
+  const long t0 = b * kBlock;
+  const long block = t0 >= 0 && t0 < len ? block_index(c, s, head, (int)b) : -1;
+  uint4 k[H], v[H];
+  unsigned e = 0;
+#pragma unroll
+  for (int h = 0; h < H; ++h) k[h] = v[h] = make_uint4(0, 0, 0, 0);
+  if (block >= 0) {
+    e = reinterpret_cast<const unsigned short *>(c.exps)[block];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      k[h] = reinterpret_cast<const uint4 *>(c.k + block * (kBlock * D))[h * kWave + lane];
+      v[h] = reinterpret_cast<const uint4 *>(c.v + block * (kBlock * D))[h * kWave + lane];
+    }
+  }
+  unsigned char *mine = turned[wave];
+  const int tok = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        mine[(4 * g + j) * (D + kRowPad) + h * 64 + t * 16 + (lane & 15)] = (unsigned char)((&v[h].x)[t] >> 8 * j);
+  wave_lds_sync();
+#pragma unroll
+  for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const uint4 *>(mine + tok * (D + kRowPad) + h * 64 + g * 16);
+
+  const long at = t0 + tok - first;
+  if (at < 0 || at >= a.count) return;
+  const bool held = block >= 0 && t0 + tok < len;
+  const long row = (((long)i * c.heads + head) * a.count + at) * (D / 8);
+  const float most = BF16 ? __uint_as_float(0x7f7f0000u) : 65504.f;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    int ex = (signed char)(which ? e >> 8 : e);
+    ex = ex < -kTop ? -kTop : ex < kTop ? ex : kTop;
+    const float scale = pow2(ex);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint4 out;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const uint4 &x = which ? v[h] : k[h];
+          const unsigned word = (&x.x)[half * 2 + n / 2];
+          const auto p = n % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)word, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)word, false);
+          unsigned pair = 0;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float y = held ? p[j] * scale : 0.f;
+            y = y > most ? most : y < -most ? -most : y;               // (NaN stays)
+            pair |= (unsigned)rounded<BF16>(y) << 16 * j;
+          }
+          (&out.x)[n] = pair;
+        }
+        reinterpret_cast<uint4 *>(which ? a.v : a.k)[row + h * 8 + g * 2 + half] = out;
+      }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pages_append(const Pages &c, int dtype, const AppendArgs &a, hipStream_t st)
+{
+  const long waves = a.rows / kBlock + 2 * (long)c.slots;
+  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)c.heads);
+  const bool bf16 = dtype == LESSDEC_DTYPE_BF16;
+  if (c.head_dim == 128) bf16 ? append_kernel<true, 128><<<grid, 256, 0, st>>>(c, a) : append_kernel<false, 128><<<grid, 256, 0, st>>>(c, a);
+  else bf16 ? append_kernel<true, 64><<<grid, 256, 0, st>>>(c, a) : append_kernel<false, 64><<<grid, 256, 0, st>>>(c, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_read(const Pages &c, int dtype, const ReadArgs &a, hipStream_t st)
+{
+  const long blocks = a.count / kBlock + 2;
+  const dim3 grid((unsigned)((blocks + 3) / 4), (unsigned)c.heads, (unsigned)a.n);
+  const bool bf16 = dtype == LESSDEC_DTYPE_BF16;
+  if (c.head_dim == 128) bf16 ? read_kernel<true, 128><<<grid, 256, 0, st>>>(c, a) : read_kernel<false, 128><<<grid, 256, 0, st>>>(c, a);
+  else bf16 ? read_kernel<true, 64><<<grid, 256, 0, st>>>(c, a) : read_kernel<false, 64><<<grid, 256, 0, st>>>(c, a);
+  return hipGetLastError();
+}
+
+}  // namespace lessdec
