@@ -294,7 +294,8 @@ int lessdec_probe_stream_read(const void *buf, size_t bytes, int32_t waves, uint
 #define LESSDEC_PAGE_BLOCK 16
 
 typedef struct lessdec_pages_desc {
-  int32_t slots, pages;           /* 1 <= slots <= LESSDEC_MAX_SLOTS; 1 <= pages < 2^28          */
+  int32_t slots, pages;           /* 1 <= slots <= LESSDEC_MAX_SLOTS; 1 <= pages < 2^28, and pages * heads *
+                                     page_tokens / 16 < 2^31                                  */
   int32_t page_tokens, table_len; /* a multiple of 16 up to 1024; entries of a table row, table_len * page_tokens <= 2^30 */
   int32_t heads, head_dim;        /* key/value heads <= 1024; 64 or 128                         */
   int32_t q_per_kv, layers;       /* query heads per key/value head (0 or 1: one), at most
@@ -302,7 +303,7 @@ typedef struct lessdec_pages_desc {
   int32_t dtype;                  /* LESSDEC_DTYPE_F16 or _BF16: q, k, v, out                   */
   int32_t sinks, window;          /* a row at position p sees the tokens j <= p with j > p - window or
                                      j < sinks; window = 0: all j <= p                       */
-  float scale;                    /* of the scores; 0: 1 / sqrt(D)                             */
+  float scale;                    /* of the scores, 2^-40 to 2^40; 0: 1 / sqrt(D)             */
   uint8_t *k_codes, *v_codes;     /* 16-byte aligned                                           */
   int8_t *exps;                   /* 2-byte aligned                                            */
   int32_t *table, *length, *refs; /* [slots][table_len], [slots], [pages]                      */

@@ -14,6 +14,7 @@ constexpr int kBlock = LESSDEC_PAGE_BLOCK;           // tokens that share an exp
 // A layer of the cache, as a kernel argument.  k, v, exps point at the layer.
 struct Pages {
   int slots, pages, page_tokens, table_len, heads, head_dim, q_per_kv, sinks, window;
+  unsigned inverse;                                  // 2^32 / (blocks of a page), rounded up; 0: a page is a block
   float scale_log2;                                  // of the scores, times log2 e
   unsigned char *k, *v;
   int8_t *exps;
@@ -37,11 +38,17 @@ __device__ inline Rows slot_rows(const int *start, int s, int rows)
   r.count = end > r.first ? end - r.first : 0;
   return r;
 }
-// index of a block in its layer, or -1 where the table names no page of the pool
-__device__ inline long block_index(const Pages &c, int s, int head, int block)
+// table entry of a slot's block: block / page_blocks, exact for the 2^26 blocks that a slot can have
+__device__ inline int entry_of(const Pages &c, int block) { return c.inverse ? (int)__umulhi((unsigned)block, c.inverse) : block; }
+// index of a block in its layer (a layer has less than 2^31), or -1 where page is none of the pool's
+__device__ inline int block_in(const Pages &c, int page, int head, int block)
 {
-  const int per = page_blocks(c), page = c.table[(size_t)s * c.table_len + block / per];
-  return (unsigned)page < (unsigned)c.pages ? ((long)page * c.heads + head) * per + block % per : -1;
+  const int per = page_blocks(c);
+  return (unsigned)page < (unsigned)c.pages ? (page * c.heads + head) * per + (block - entry_of(c, block) * per) : -1;
+}
+__device__ inline int block_index(const Pages &c, int s, int head, int block)
+{
+  return block_in(c, c.table[(size_t)s * c.table_len + entry_of(c, block)], head, block);
 }
 
 // The last slot s in [0, slots) whose base(s) is at most x, for a base that does not fall with s: 64 lanes ask at a time, so that

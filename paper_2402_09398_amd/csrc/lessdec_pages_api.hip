@@ -13,11 +13,12 @@ bool shape_ok(const lessdec_pages_desc *d)
   if (d->slots < 1 || d->slots > LESSDEC_MAX_SLOTS || d->pages < 1 || d->pages >= 1 << 28) return false;
   if (d->page_tokens < kBlock || d->page_tokens > 1024 || d->page_tokens % kBlock) return false;
   if (d->table_len < 1 || (long)d->table_len * d->page_tokens > 1L << 30) return false;
-  if (d->heads < 1 || d->heads > 1024 || (d->head_dim != 64 && d->head_dim != 128)) return false;
+  if (d->heads < 1 || (long)d->pages * d->heads * (d->page_tokens / kBlock) >= 1L << 31) return false;
+  if (d->heads > 1024 || (d->head_dim != 64 && d->head_dim != 128)) return false;
   if (d->q_per_kv < 0 || d->q_per_kv > LESSDEC_MAX_Q_PER_KV || d->layers < 1 || d->layers > 1024) return false;
   if (d->dtype != LESSDEC_DTYPE_F16 && d->dtype != LESSDEC_DTYPE_BF16) return false;
   if (d->sinks < 0 || d->window < 0) return false;
-  if (!(d->scale >= 0.f) || d->scale > 1e30f) return false;
+  if (d->scale != 0.f && !(d->scale >= 0x1p-40f && d->scale <= 0x1p40f)) return false;
   return true;
 }
 
@@ -46,6 +47,8 @@ int check(const lessdec_pages_desc *d, int needs, int rows, int layer, Pages *c)
   if ((needs & kWork) && (!d->workspace || !aligned(d->workspace, 256) || d->workspace_bytes < workspace_for(d, rows))) return LESSDEC_EWORKSPACE;
   c->slots = d->slots; c->pages = d->pages; c->page_tokens = d->page_tokens; c->table_len = d->table_len;
   c->heads = d->heads; c->head_dim = d->head_dim; c->q_per_kv = d->q_per_kv > 1 ? d->q_per_kv : 1;
+  const unsigned per = (unsigned)(d->page_tokens / kBlock);
+  c->inverse = per == 1 ? 0 : (unsigned)(((1ull << 32) + per - 1) / per);
   c->sinks = d->sinks; c->window = d->window;
   const double scale = d->scale > 0.f ? (double)d->scale : d->head_dim == 64 ? 0.125 : 0.08838834764831845;
   c->scale_log2 = (float)(scale * 1.4426950408889634);

@@ -72,9 +72,9 @@ __device__ inline unsigned half_pair(float a, float b)
 {
   return __builtin_bit_cast(unsigned, half2v{(_Float16)a, (_Float16)b});
 }
-__device__ inline bool code_nan(unsigned w)          // any of four codes
+__device__ inline unsigned code_nans(unsigned w)     // 0xff where one of four codes is a NaN
 {
-  return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+  return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
 }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
   __shared__ float sums[4][kCols][kRow];
   __shared__ float tops[4][kCols], totals[4][kCols];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int G = c.q_per_kv, per = page_blocks(c);
+  const int G = c.q_per_kv;
   const Part part = part_of<false>(c, a, blockIdx.x, gridDim.x);
   if (part.begin >= part.end) return;
   int s = part.slot;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
     const int *table = c.table + (size_t)s * c.table_len;
     auto page_at = [&](int step, int b) {
       const int i = step * kStepBlocks + wave * 2 + b;
-      return step < to && i < span.count ? table[span.block(i) / per] : -1;
+      return step < to && i < span.count ? table[entry_of(c, span.block(i))] : -1;
     };
     u4 k[2][H], v[2][H], k1[2][H], v1[2][H];
     unsigned ex[2], ex1[2];
@@ -225,18 +225,17 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int block = span.block(step * kStepBlocks + wave * 2 + b);
-        const bool there = (unsigned)page[b] < (unsigned)c.pages;
-        t01[b] = there ? block * kBlock : -1;
+        const int at = block_in(c, page[b], head, block);
+        t01[b] = at >= 0 ? block * kBlock : -1;
         ex1[b] = 0;
 #pragma unroll
         for (int h = 0; h < H; ++h) k1[b][h] = v1[b][h] = u4{0, 0, 0, 0};
-        if (there) {
-          const long at = ((long)page[b] * c.heads + head) * per + block % per;
+        if (at >= 0) {
           ex1[b] = reinterpret_cast<const unsigned short *>(c.exps)[at];
 #pragma unroll
           for (int h = 0; h < H; ++h) {
-            k1[b][h] = reinterpret_cast<const u4 *>(c.k + at * (kBlock * D))[h * kWave + lane];
-            v1[b][h] = reinterpret_cast<const u4 *>(c.v + at * (kBlock * D))[h * kWave + lane];
+            k1[b][h] = reinterpret_cast<const u4 *>(c.k + at * ((long)kBlock * D))[h * kWave + lane];
+            v1[b][h] = reinterpret_cast<const u4 *>(c.v + at * ((long)kBlock * D))[h * kWave + lane];
           }
         }
       }
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
           for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine |= code_nan(v[b][h][i]);
+            for (int i = 0; i < 4; ++i) mine |= code_nans(v[b][h][i]) != 0;
         apart = __ballot(mine) != 0;
       }
       if (!apart) {
@@ -467,9 +466,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
   __shared__ __align__(16) u4 keys[2][kTile * D / 8], values[2][kTile * D / 8];
-  __shared__ int nan_tile[2];
+  __shared__ int spoiled;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int G = c.q_per_kv, per = page_blocks(c);
+  const int G = c.q_per_kv;
   // each die works through neighbouring items, head by head: what a (slot, head) has cached stays in its L2
   const long total = items * c.heads * splits;
   long id = blockIdx.x;
@@ -500,40 +499,59 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     if (col <= last_col) q[k] = reinterpret_cast<const u4 *>(a.q)[row * (a.stride / 8) + q_head * (D / 8) + k * 2 + h];
   }
 
-  // Staging: a wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.
+  // Staging.  Lanes 0-3 (and their repetitions) look up a tile's four blocks: the table three tiles ahead, the exponents with the codes two
+  // ahead.  A wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.
   const int *table = c.table + (size_t)t.slot * c.table_len;
-  u4 kc[H], vc[H];
-  unsigned ex[4], ex1[4];
-  auto block_of = [&](int tile, int b, int &block) -> long {
-    const int i = tile * 4 + b;
-    if (tile >= to || i >= span.count) return -1;
-    block = span.block(i);
-    const int page = table[block / per];
-    return (unsigned)page < (unsigned)c.pages ? ((long)page * c.heads + head) * per + block % per : -1;
+  auto look = [&](int tile) {
+    const int i = tile * 4 + (lane & 3);
+    return tile < to && i < span.count ? table[entry_of(c, span.block(i))] : -1;
   };
+  constexpr int kNone = 0x10000;                     // an exponent word of a block that is not there
+  u4 kc[H], vc[H];
+  int page, ex_next;
   auto request = [&](int tile) {
+    const int at = block_in(c, page, head, span.block(tile * 4 + (lane & 3)));
+    ex_next = kNone;
+    if (at >= 0) ex_next = reinterpret_cast<const unsigned short *>(c.exps)[at];
 #pragma unroll
     for (int j = 0; j < H; ++j) {
-      int block;
-      const long at = block_of(tile, H == 2 ? wave / 2 + 2 * j : wave, block);
+      const int block = __builtin_amdgcn_readlane(at, H == 2 ? wave / 2 + 2 * j : wave), half = H == 2 ? wave % 2 : 0;
       kc[j] = vc[j] = u4{0, 0, 0, 0};
-      if (at >= 0) {
-        const int half = H == 2 ? wave % 2 : 0;
-        kc[j] = reinterpret_cast<const u4 *>(c.k + at * (kBlock * D))[half * kWave + lane];
-        vc[j] = reinterpret_cast<const u4 *>(c.v + at * (kBlock * D))[half * kWave + lane];
+      if (block >= 0) {
+        kc[j] = reinterpret_cast<const u4 *>(c.k + block * ((long)kBlock * D))[half * kWave + lane];
+        vc[j] = reinterpret_cast<const u4 *>(c.v + block * ((long)kBlock * D))[half * kWave + lane];
       }
     }
+  };
+  // where a word of four tokens' codes of channel 64 half + 16 i + (lane & 15) goes: [block][32 channels][which eight of the 16
+  // tokens][channel], tokens 0-3 and 8-11, or 4-7 and 12-15
+  auto value_at = [&](int j, int i) {
+    const int b = H == 2 ? wave / 2 + 2 * j : wave, d = (H == 2 ? wave % 2 : 0) * 64 + i * 16 + (lane & 15), g = lane >> 4;
+    return (((b * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1);
+  };
+  auto is_edge = [&](int tile) {                     // some row of the workgroup does not see all of the tile
+    bool whole = true;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      int block;
-      const long at = block_of(tile, b, block);
-      ex1[b] = at >= 0 ? reinterpret_cast<const unsigned short *>(c.exps)[at] : 0x10000u;
+      const int i = tile * 4 + b;
+      whole &= i < span.count && all_see(c, lo, hi, span.block(i) * kBlock);
     }
+    return !whole;
   };
-  auto stage = [&](int tile) {
-    const int buf = tile & 1;
+  bool mine_spoiled = false;
+  auto stage = [&](int tile, int buf) {
     const int tok = lane & 15, g = lane >> 4;
-    bool bad = false;
+    // a NaN among values that only some rows see is taken out (0 * NaN is NaN) and given to those that see it in the end
+    if (is_edge(tile)) {
+#pragma unroll
+      for (int j = 0; j < H; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned bad = code_nans(vc[j][i]);
+          mine_spoiled |= bad != 0;
+          vc[j][i] &= ~bad;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < H; ++j) {
       const int b = H == 2 ? wave / 2 + 2 * j : wave, half = H == 2 ? wave % 2 : 0;
@@ -541,125 +559,130 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         keys[buf][(((b >> 1) * KK + half * 4 + g) * 2 + e) * 32 + (b & 1) * 16 + tok] = widen<BF16>(kc[j][2 * e], kc[j][2 * e + 1]);
-      // value operands: [block][32 channels][which eight of the 16 tokens][channel]: tokens 0-3, 8-11 and 4-7, 12-15
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int d = half * 64 + i * 16 + tok;
-        bad |= code_nan(vc[j][i]);
-        reinterpret_cast<uint2 *>(values[buf])[(((b * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1)] =
-            make_uint2(Operand<false>::pair(vc[j][i], false), Operand<false>::pair(vc[j][i], true));
-      }
+      for (int i = 0; i < 4; ++i)
+        reinterpret_cast<uint2 *>(values[buf])[value_at(j, i)] = make_uint2(Operand<false>::pair(vc[j][i], false), Operand<false>::pair(vc[j][i], true));
     }
-    if (bad) nan_tile[buf] = tile;
   };
 
   f16v acc[OB];
 #pragma unroll
   for (int o = 0; o < OB; ++o) acc[o] = f16v{0};
   float top = kLowest, sum = 0;
-  if (threadIdx.x < 2) nan_tile[threadIdx.x] = -1;
-  __syncthreads();
+  if (threadIdx.x == 0) spoiled = 0;
+  int ex = kNone;
   if (from < to) {
+    page = look(from);
     request(from);
-    stage(from);
-#pragma unroll
-    for (int b = 0; b < 4; ++b) ex[b] = ex1[b];
+    page = look(from + 1);
+    stage(from, from & 1);
+    ex = ex_next;
     request(from + 1);
+    page = look(from + 2);
   }
   for (int tile = from; tile < to; ++tile) {
     __syncthreads();
-    const int buf = tile & 1;
-    unsigned next_ex[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) next_ex[b] = ex1[b];
+    const int buf = tile & 1, ex_staged = ex_next;
     if (tile + 1 < to) {
-      stage(tile + 1);
+      stage(tile + 1, buf ^ 1);
       request(tile + 2);
+      page = look(tile + 3);
     }
-    int t0[4];
+    int e[4], t0[4];
     bool whole = true, some = false;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       const int i = tile * 4 + b;
-      t0[b] = i < span.count && ex[b] < 0x10000u ? span.block(i) * kBlock : -1;
+      e[b] = __builtin_amdgcn_readlane(ex, b);
+      t0[b] = e[b] < kNone ? span.block(i) * kBlock : -1;
       whole &= t0[b] >= 0 && all_see(c, wave_lo, wave_hi, t0[b]);
       some |= t0[b] >= 0 && t0[b] <= wave_hi && (c.window == 0 || t0[b] + kBlock > wave_lo - c.window || t0[b] < c.sinks);
     }
-    if (have && some) {
-      f16v x[2];
+    ex = ex_staged;
+    if (!have || !some) continue;
+    f16v x[2];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        x[m] = f16v{0};
+    for (int m = 0; m < 2; ++m) {
+      x[m] = f16v{0};
 #pragma unroll
-        for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
-      }
-      float most = kLowest;
+      for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+    }
+    if (!whole) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const float factor = pow2((signed char)ex[b]) * c.scale_log2, ve = (float)(signed char)(ex[b] >> 8);
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          float y = fmaf(x[b / 2][b % 2 * 8 + i], factor, ve);
-          if (!whole) {
-            const int token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2);
-            if (t0[b] < 0 || !sees(c, p, token)) y = -__builtin_inff();
-          }
-          x[b / 2][b % 2 * 8 + i] = y;
-          most = fmaxf(most, y);
+          const int token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2);
+          const bool seen = t0[b] >= 0 && sees(c, p, token);
+          x[b / 2][b % 2 * 8 + i] = seen ? x[b / 2][b % 2 * 8 + i] : -__builtin_inff();
         }
-      }
-      if (__ballot(most > top + kSlack)) {
-        most = fmaxf(most, __shfl_xor(most, 32, kWave));
-        const float now = fmaxf(top, most), f = exp2_fast(top - now);
-        top = now;
-        sum *= f;
+    }
+    // t = factor x + ve; the factor is positive, so a block's largest x gives its largest t
+    float most = kLowest, factor[4];
 #pragma unroll
-        for (int o = 0; o < OB; ++o) acc[o] *= f;
-      }
-      const float zero = top - kBase;
-      u4 weights[4];
+    for (int b = 0; b < 4; ++b) {
+      factor[b] = pow2((signed char)e[b]) * c.scale_log2;
+      float y = x[b / 2][b % 2 * 8];
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float part = 0;
+      for (int i = 1; i < 8; ++i) y = fmaxf(y, x[b / 2][b % 2 * 8 + i]);
+      most = fmaxf(most, fmaf(y, factor[b], (float)(signed char)(e[b] >> 8)));
+    }
+    if (__ballot(most > top + kSlack)) {
+      most = fmaxf(most, __shfl_xor(most, 32, kWave));
+      const float now = fmaxf(top, most), f = exp2_fast(top - now);
+      top = now;
+      sum *= f;
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          const float y = exp2_fast(x[b / 2][b % 2 * 8 + i] - zero), z = exp2_fast(x[b / 2][b % 2 * 8 + i + 1] - zero);
-          part += y + z;
-          weights[b][i / 2] = half_pair(y, z);
-        }
-        sum = fmaf(part, pow2(-(signed char)(ex[b] >> 8)), sum);
-      }
-      if (whole || nan_tile[buf] != tile) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-          for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][(b * OB + o) * 64 + lane], weights[b], acc[o]);
-      } else {
-        // a NaN among values that only some rows see: counted apart, since 0 * NaN is NaN
-#pragma unroll 1
-        for (int b = 0; b < 4; ++b) {
-          half8 seen;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) seen[i] = t0[b] >= 0 && sees(c, p, t0[b] + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
-#pragma unroll
-          for (int o = 0; o < OB; ++o) {
-            half8 y = __builtin_bit_cast(half8, values[buf][(b * OB + o) * 64 + lane]), bad;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              bad[i] = y[i] != y[i] ? 1 : 0;
-              y[i] = y[i] != y[i] ? 0 : y[i];
-            }
-            acc[o] = Operand<false>::mma32(__builtin_bit_cast(u4, y), weights[b], acc[o]);
-            const f16v count = Operand<false>::mma32(__builtin_bit_cast(u4, bad), __builtin_bit_cast(u4, seen), f16v{0});
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[o][i] = count[i] > 0 ? __builtin_nanf("") : acc[o][i];
-          }
-        }
-      }
+      for (int o = 0; o < OB; ++o) acc[o] *= f;
     }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) ex[b] = next_ex[b];
+    for (int b = 0; b < 4; ++b) {
+      const float zero = (float)(signed char)(e[b] >> 8) - (top - kBase);
+      float part = 0;
+      u4 weights;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float y = exp2_fast(fmaf(x[b / 2][b % 2 * 8 + i], factor[b], zero)), z = exp2_fast(fmaf(x[b / 2][b % 2 * 8 + i + 1], factor[b], zero));
+        part += y + z;
+        weights[i / 2] = half_pair(y, z);
+      }
+      sum = fmaf(part, pow2(-(signed char)(e[b] >> 8)), sum);
+#pragma unroll
+      for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][(b * OB + o) * 64 + lane], weights, acc[o]);
+    }
   }
+
+  if (mine_spoiled) spoiled = 1;
+  __syncthreads();
+  if (spoiled)                                       // the NaN that were taken out, counted for the rows that see them
+    for (int tile = from; tile < to; ++tile) {
+      if (!is_edge(tile)) continue;
+      page = look(tile);
+      request(tile);
+#pragma unroll
+      for (int j = 0; j < H; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned one = code_nans(vc[j][i]) & 0x38383838u;      // the code of 1
+          reinterpret_cast<uint2 *>(values[0])[value_at(j, i)] = make_uint2(Operand<false>::pair(one, false), Operand<false>::pair(one, true));
+        }
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int e = __builtin_amdgcn_readlane(ex_next, b), t0 = e < kNone ? span.block(tile * 4 + b) * kBlock : -1;
+        half8 seen;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) seen[i] = t0 >= 0 && sees(c, p, t0 + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
+#pragma unroll
+        for (int o = 0; o < OB; ++o) {
+          const f16v count = Operand<false>::mma32(values[0][(b * OB + o) * 64 + lane], __builtin_bit_cast(u4, seen), f16v{0});
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[o][i] = count[i] > 0 ? __builtin_nanf("") : acc[o][i];
+        }
+      }
+      __syncthreads();
+    }
+
   sum += __shfl_xor(sum, 32, kWave);
   if (splits > 1) {
     float *part = a.parts + (item * splits + split) * wide_floats(D);

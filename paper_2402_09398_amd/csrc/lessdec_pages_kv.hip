@@ -90,14 +90,14 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   const long b = begin / kBlock + w - base(s);
   if (r.count == 0 || b < 0 || b * kBlock >= len) return;
   const int t0 = (int)b * kBlock;
-  const long block = block_index(c, s, head, (int)b);
+  const int block = block_index(c, s, head, (int)b);
   if (block < 0) return;
   const int off = begin > t0 ? begin - t0 : 0;                         // older tokens of the block
 
   const int tok = lane & 15, g = lane >> 4;
   const bool fresh = tok >= off && t0 + tok < len;
   unsigned short *exps = reinterpret_cast<unsigned short *>(c.exps) + block;
-  uint4 *kb = reinterpret_cast<uint4 *>(c.k + block * (kBlock * D)) + lane, *vb = reinterpret_cast<uint4 *>(c.v + block * (kBlock * D)) + lane;
+  uint4 *kb = reinterpret_cast<uint4 *>(c.k + block * ((long)kBlock * D)) + lane, *vb = reinterpret_cast<uint4 *>(c.v + block * ((long)kBlock * D)) + lane;
   uint4 x[2][H][2];
   const long row = (long)(row0 + t0 + tok - begin) * (a.stride / 8) + head * (D / 8);
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void read_kernel(Pages c, ReadArgs a)
   const long b = (first >> 4) + (long)blockIdx.x * 4 + wave;           // (floor: first may be negative)
   if (b * kBlock >= first + a.count) return;
   const long t0 = b * kBlock;
-  const long block = t0 >= 0 && t0 < len ? block_index(c, s, head, (int)b) : -1;
+  const int block = t0 >= 0 && t0 < len ? block_index(c, s, head, (int)b) : -1;
   uint4 k[H], v[H];
   unsigned e = 0;
 #pragma unroll
@@ -227,8 +227,8 @@ __global__ __launch_bounds__(256) void read_kernel(Pages c, ReadArgs a)
     e = reinterpret_cast<const unsigned short *>(c.exps)[block];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      k[h] = reinterpret_cast<const uint4 *>(c.k + block * (kBlock * D))[h * kWave + lane];
-      v[h] = reinterpret_cast<const uint4 *>(c.v + block * (kBlock * D))[h * kWave + lane];
+      k[h] = reinterpret_cast<const uint4 *>(c.k + block * ((long)kBlock * D))[h * kWave + lane];
+      v[h] = reinterpret_cast<const uint4 *>(c.v + block * ((long)kBlock * D))[h * kWave + lane];
     }
   }
   unsigned char *mine = turned[wave];
