@@ -307,8 +307,10 @@ typedef struct lessdec_pages_desc {
   uint8_t *k_codes, *v_codes;     /* 16-byte aligned                                           */
   int8_t *exps;                   /* 2-byte aligned                                            */
   int32_t *table, *length, *refs; /* [slots][table_len], [slots], [pages]                      */
-  void *workspace;                /* >= lessdec_pages_workspace_bytes(), 256-byte aligned; scratch without
-                                     conditions on what it holds.  Calls that share one must be ordered by a stream */
+  void *workspace;                /* >= lessdec_pages_workspace_bytes(), 256-byte aligned.  Scratch, filled
+                                     with zeros once before its first use (its first bytes count the workgroups that
+                                     share a row's tokens, and every call leaves them 0).  Calls that share one must be
+                                     ordered by a stream; it serves descriptors of any shape that it is large enough for */
   size_t workspace_bytes;
 } lessdec_pages_desc;
 

@@ -106,8 +106,10 @@ struct AttendArgs {
   float *lse;
   const int *start;
   int rows, max_new;
+  int *counters;                                     // [3 kPagesWorkers], 0 before and after a call
   float *parts;
 };
+constexpr int kPagesWorkers = 768;                   // workgroups of the kernel of few rows: three to a compute unit
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 // floats of AttendArgs::parts for up to `rows` rows
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows);

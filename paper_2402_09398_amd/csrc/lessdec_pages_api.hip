@@ -27,11 +27,15 @@ size_t floats_for(const lessdec_pages_desc *d, int rows)
   return pages_attend_floats(d->slots, d->heads, d->q_per_kv > 1 ? d->q_per_kv : 1, d->head_dim, (long)d->table_len * d->page_tokens, rows);
 }
 
+// Workspace: counters of lessdec_pages_attend | its shares, or the lists of the other calls
+constexpr size_t kCounterBytes = (3 * kPagesWorkers * sizeof(int) + 255) / 256 * 256;
+inline void *scratch(const lessdec_pages_desc *d) { return static_cast<char *>(d->workspace) + kCounterBytes; }
+
 size_t workspace_for(const lessdec_pages_desc *d, int rows)
 {
   const size_t attend = rows > 0 ? floats_for(d, rows) * sizeof(float) : 0, lists = (size_t)d->pages * sizeof(int32_t);
   const size_t n = attend > lists ? attend : lists;
-  return (n + 255) / 256 * 256;
+  return kCounterBytes + (n + 255) / 256 * 256;
 }
 
 enum Needs { kTables = 1, kPool = 2, kWork = 4 };
@@ -92,7 +96,7 @@ int lessdec_pages_reserve(const lessdec_pages_desc *desc, const int32_t *n_new, 
   if (rc) return rc;
   if (!n_new || !plan || !aligned(n_new, 4) || !aligned(granted, 4) || !aligned(plan, 4)) return LESSDEC_EINVAL;
   if (granted == n_new || plan == n_new || plan == granted) return LESSDEC_EINVAL;
-  return result(launch_pages_reserve(c, n_new, granted, plan, static_cast<int *>(desc->workspace), (hipStream_t)hip_stream));
+  return result(launch_pages_reserve(c, n_new, granted, plan, static_cast<int *>(scratch(desc)), (hipStream_t)hip_stream));
 }
 
 int lessdec_pages_select(const lessdec_pages_desc *desc, const int32_t *from, void *hip_stream)
@@ -110,7 +114,7 @@ int lessdec_pages_compact(const lessdec_pages_desc *desc, int32_t *plan, void *h
   const int rc = check(desc, kTables | kWork, 0, 0, &c);
   if (rc) return rc;
   if (!plan || !aligned(plan, 4)) return LESSDEC_EINVAL;
-  return result(launch_pages_compact(c, plan, static_cast<int *>(desc->workspace), (hipStream_t)hip_stream));
+  return result(launch_pages_compact(c, plan, static_cast<int *>(scratch(desc)), (hipStream_t)hip_stream));
 }
 
 int lessdec_pages_copy(const lessdec_pages_desc *desc, const int32_t *plan, int32_t max_pairs, void *hip_stream)
@@ -146,7 +150,8 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
   rc = check(desc, kWork, rows, layer, &c);
   if (rc) return rc;
   if (rows == 0 || max_new == 0) return LESSDEC_OK;
-  AttendArgs a{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<float *>(desc->workspace)};
+  AttendArgs a{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<int *>(desc->workspace),
+               static_cast<float *>(scratch(desc))};
   return result(launch_pages_attend(c, desc->dtype, a, (hipStream_t)hip_stream));
 }
 

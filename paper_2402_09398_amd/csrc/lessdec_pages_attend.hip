@@ -110,10 +110,11 @@ __device__ inline bool all_see(const Pages &c, int lo, int hi, int t0)
 // Bound by the read of the cache.  The work is a list of steps, 128 tokens of a slot and head each, that is dealt out evenly to as many
 // workgroups as the chip holds at once, whatever the slots' lengths; every workgroup finds its part from the lengths.  A
 // step is 32 tokens for each of four waves, which stay apart until the workgroup leaves a (slot, head).  What a
-// workgroup has of a (slot, head) that it shares with others goes to memory and is joined by a second launch, in the order of the tokens.
+// workgroup has of a (slot, head) that it shares with others goes to memory, past the L2 of its die, and the last of them to arrive joins
+// the shares in the order of the tokens: 32 neighbours first, then the joined ones, so that one sequence can be spread over the chip.
 
 constexpr int kCols = 16, kStepBlocks = 8;
-constexpr int kWorkers = 768;
+constexpr int kWorkers = kPagesWorkers, kGroup = 32;
 
 __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
 {
@@ -124,53 +125,57 @@ __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
   return n > 0 ? n : 1;                              // (rows that see nothing are written too)
 }
 
-// Worker w's part [begin, end) of the steps, and where its step `at` lies: slot, and step among the slot's (head by head).
+// Worker w's part [begin, end) of the steps, and where it begins: slot, and step among the slot's (head by head).
 struct Part {
   long begin, end, per;
   int slot;
   long in_slot;
 };
-template <bool LAST>
 __device__ inline Part part_of(const Pages &c, const AttendArgs &a, int w, int workers)
 {
-  __shared__ long sums[4];
+  __shared__ long sums[4], found_at;
   __shared__ int found;
-  __shared__ long found_at;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto scan = [&](int base, long &n, long &upto, long &at) {           // at: the sum before this chunk, then behind it
+    const int s = base + tid;
+    n = s < c.slots ? (long)steps_of(c, a, s) * c.heads : 0;
+    upto = n;
+    for (int d = 1; d < kWave; d <<= 1) {
+      const long y = __shfl_up(upto, d, kWave);
+      if (lane >= d) upto += y;
+    }
+    if (base) __syncthreads();
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    long before = at;
+    for (int i = 0; i < 4; ++i) {
+      if (i < wave) before += sums[i];
+      at += sums[i];
+    }
+    upto += before;
+  };
   Part p;
-  long total = 0;
-  for (int round = 0; round < 2; ++round) {          // the sum first, then the slot that holds the step
-    long at = 0, want = 0;
-    if (round) {
-      p.per = (total + workers - 1) / workers;
-      p.begin = w * p.per;
-      p.end = p.begin + p.per < total ? p.begin + p.per : total;
-      if (p.begin >= p.end) return p;
-      want = LAST ? p.end - 1 : p.begin;
+  long total = 0, n, upto;
+  for (int base = 0; base < c.slots; base += 256) scan(base, n, upto, total);
+  p.per = (total + workers - 1) / workers;
+  p.begin = w * p.per;
+  p.end = p.begin + p.per < total ? p.begin + p.per : total;
+  if (p.begin >= p.end) return p;
+  auto look = [&](int base) {
+    if (n > 0 && p.begin >= upto - n && p.begin < upto) {
+      found = base + tid;
+      found_at = p.begin - (upto - n);
     }
-    for (int base = 0; base < c.slots; base += 256) {
-      const int s = base + tid;
-      const long n = s < c.slots ? (long)steps_of(c, a, s) * c.heads : 0;
-      long upto = n;
-      for (int d = 1; d < kWave; d <<= 1) {
-        const long y = __shfl_up(upto, d, kWave);
-        if (lane >= d) upto += y;
-      }
+  };
+  if (c.slots <= 256) {
+    look(0);
+  } else {
+    long at = 0;
+    for (int base = 0; base < c.slots && at <= p.begin; base += 256) {
       __syncthreads();
-      if (lane == 63) sums[wave] = upto;
-      __syncthreads();
-      long before = at;
-      for (int i = 0; i < 4; ++i) {
-        if (i < wave) before += sums[i];
-        at += sums[i];
-      }
-      if (round && n > 0 && want >= before + upto - n && want < before + upto) {
-        found = s;
-        found_at = want - (before + upto - n);
-      }
-      if (round && at > want) break;
+      scan(base, n, upto, at);
+      look(base);
     }
-    total = at;
   }
   __syncthreads();
   p.slot = __builtin_amdgcn_readfirstlane(found);
@@ -178,24 +183,91 @@ __device__ inline Part part_of(const Pages &c, const AttendArgs &a, int w, int w
   return p;
 }
 
+// A share: [columns][D] sums, maxima, totals.  Stored and loaded past the caches that other dies do not see.
 constexpr int part_floats(int D) { return kCols * (D + 2); }
+__device__ inline void put(float *p, float x, float y)
+{
+  const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float2 get(const float *p)
+{
+  const unsigned long long v =
+      __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+__device__ inline void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline float get1(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Whether this workgroup is the last of n to arrive; the counter is 0 again then.  What the workgroup stored before is in memory,
+// and what the others stored is seen behind it.
+__device__ inline bool last_to_arrive(int *counter, int n)
+{
+  __shared__ int arrived;
+  __syncthreads();                                   // (waits for the stores)
+  if (threadIdx.x == 0) {
+    arrived = __hip_atomic_fetch_add(counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    if (arrived == n) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  const bool last = arrived == n;
+  __syncthreads();
+  return last;
+}
+
+// Joins n shares; done(column, channel, sum, sum of the next channel, maximum, total).
+template <int D, typename Share, typename Done>
+__device__ inline void join(int n, int cols, Share share, Done done)
+{
+  for (int i = threadIdx.x; i < cols * (D / 2); i += 256) {
+    const int col = i / (D / 2), d = i % (D / 2) * 2;
+    float top = kLowest, l = 0, x = 0, y = 0;
+    for (int k = 0; k < n; k += 8) {                 // eight at a time on their way
+      float m[8], t[8];
+      float2 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float *f = share(k + j < n ? k + j : k);
+        m[j] = get1(f + kCols * D + col);
+        t[j] = get1(f + kCols * (D + 1) + col);
+        v[j] = get(f + col * D + d);
+      }
+      float now = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) now = fmaxf(now, m[j]);
+      const float f = exp2_fast(top - now);
+      top = now;
+      l *= f; x *= f; y *= f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (k + j >= n) break;
+        const float e = exp2_fast(m[j] - top);
+        l = fmaf(t[j], e, l);
+        x = fmaf(v[j].x, e, x);
+        y = fmaf(v[j].y, e, y);
+      }
+    }
+    done(col, d, x, y, top, l);
+  }
+}
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
+__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 {
   constexpr int H = D / 64, T = D / 16, kRow = D + 4;
   __shared__ float sums[4][kCols][kRow];
   __shared__ float tops[4][kCols], totals[4][kCols];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int G = c.q_per_kv;
-  const Part part = part_of<false>(c, a, blockIdx.x, gridDim.x);
+  const Part part = part_of(c, a, blockIdx.x, gridDim.x);
   if (part.begin >= part.end) return;
   int s = part.slot;
   long in_slot = part.in_slot;
   for (long pos = part.begin; pos < part.end;) {
     const int steps = steps_of(c, a, s);
     if (steps == 0) { ++s; in_slot = 0; continue; }
-    const int head = (int)(in_slot / steps), from = (int)(in_slot % steps);
+    const int head = (int)((unsigned long)in_slot >> 32 ? in_slot / steps : (unsigned)in_slot / (unsigned)steps);
+    const int from = (int)(in_slot - (long)head * steps);
     const int to = (int)min((long)steps, from + (part.end - pos));
 
     const Rows rows = slot_rows(a.start, s, a.rows);
@@ -245,6 +317,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
     for (int t = 0; t < T; ++t) acc[t] = f4{0, 0, 0, 0};
     float top = kLowest, total = 0;
+    bool spoiled = false;
     page[0] = page_at(from, 0); page[1] = page_at(from, 1);
     request(from);
     page[0] = page_at(from + 1, 0); page[1] = page_at(from + 1, 1);
@@ -259,33 +332,46 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
       page[0] = page_at(step + 2, 0); page[1] = page_at(step + 2, 1);
       if (t0[0] < 0 && t0[1] < 0) continue;
 
-      float t[2][4];
-      float most = kLowest;
-      bool edge = false;
+      f4 x[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        f4 x = {0, 0, 0, 0};
+        x[b] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) x = Operand<BF16>::mma16(widen<BF16>(k[b][h][2 * i], k[b][h][2 * i + 1]), q[h][i], x);
-        const float factor = pow2((signed char)ex[b]) * c.scale_log2, ve = (float)(signed char)(ex[b] >> 8);
+          for (int i = 0; i < 2; ++i) x[b] = Operand<BF16>::mma16(widen<BF16>(k[b][h][2 * i], k[b][h][2 * i + 1]), q[h][i], x[b]);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t[b][i] = fmaf(x[i], factor, ve);
+      for (int b = 0; b < 2; ++b)
         if (t0[b] < 0 || !all_see(c, lo, hi, t0[b])) {
-          edge = true;
-          unsigned keep = 0;                         // values that no row sees are taken out, so that nothing in them counts
+          // What no row sees is taken out, and where rows see different tokens NaN values are too (0 * NaN is NaN); those that some row
+          // sees are given to it in the end.
+          unsigned keep = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int token = t0[b] + 4 * g + i;
-            if (t0[b] < 0 || !sees(c, p, token)) t[b][i] = -__builtin_inff();
+            x[b][i] = t0[b] >= 0 && sees(c, p, token) ? x[b][i] : -__builtin_inff();
             if (t0[b] >= 0 && token <= hi && (c.window == 0 || token > lo - c.window || token < c.sinks)) keep |= 255u << 8 * i;
           }
 #pragma unroll
-          for (int h = 0; h < H; ++h) v[b][h] &= keep;
-        }
+          for (int h = 0; h < H; ++h) {
+            v[b][h] &= keep;
+            if (rows.count > 1)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = fmaxf(most, t[b][i]);
+              for (int i = 0; i < 4; ++i) {
+                const unsigned bad = code_nans(v[b][h][i]);
+                spoiled |= bad != 0;
+                v[b][h][i] &= ~bad;
+              }
+          }
+        }
+      // t = factor x + ve; the factor is positive, so a block's largest x gives its largest t
+      float most = kLowest, factor[2], ve[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        factor[b] = pow2((signed char)ex[b]) * c.scale_log2;
+        ve[b] = (float)(signed char)(ex[b] >> 8);
+        most = fmaxf(most, fmaf(fmaxf(fmaxf(x[b][0], x[b][1]), fmaxf(x[b][2], x[b][3])), factor[b], ve[b]));
       }
       if (__ballot(most > top + kSlack)) {
         most = fmaxf(most, __shfl_xor(most, 16, kWave));
@@ -296,58 +382,44 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
         for (int i = 0; i < T; ++i) acc[i] *= f;
       }
-      float w[2][4];
+      u4 weights;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        float part_sum = 0;
+        float w[4];
+        const float zero = ve[b] - (top - kBase);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[b][i] = exp2_fast(t[b][i] - (top - kBase));
-          part_sum += w[b][i];
-        }
-        total = fmaf(part_sum, pow2(-(signed char)(ex[b] >> 8)), total);
+        for (int i = 0; i < 4; ++i) w[i] = exp2_fast(fmaf(x[b][i], factor[b], zero));
+        total = fmaf((w[0] + w[1]) + (w[2] + w[3]), pow2(-(signed char)(ex[b] >> 8)), total);
+        weights[2 * b] = half_pair(w[0], w[1]);
+        weights[2 * b + 1] = half_pair(w[2], w[3]);
       }
-      const u4 weights = {half_pair(w[0][0], w[0][1]), half_pair(w[0][2], w[0][3]), half_pair(w[1][0], w[1][1]), half_pair(w[1][2], w[1][3])};
-      // a NaN among values that only some of the rows see reaches those alone: 0 * NaN is NaN, so it is counted apart
-      bool apart = false;
-      if (edge && rows.count > 1) {
-        bool mine = false;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-          for (int h = 0; h < H; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine |= code_nans(v[b][h][i]) != 0;
-        apart = __ballot(mine) != 0;
-      }
-      if (!apart) {
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            acc[h * 4 + i] = Operand<false>::mma16(widen<false>(v[0][h][i], v[1][h][i]), weights, acc[h * 4 + i]);
-      } else {
+        for (int i = 0; i < 4; ++i)
+          acc[h * 4 + i] = Operand<false>::mma16(widen<false>(v[0][h][i], v[1][h][i]), weights, acc[h * 4 + i]);
+    }
+    if (__ballot(spoiled))                           // the NaN that were taken out, counted for the rows that see them
+#pragma unroll 1
+      for (int step = from; step < to; ++step) {
+        page[0] = page_at(step, 0); page[1] = page_at(step, 1);
+        request(step);
         half8 seen;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) seen[i] = t0[i / 4] >= 0 && sees(c, p, t0[i / 4] + 4 * g + i % 4) ? 1 : 0;
+        for (int i = 0; i < 8; ++i) {
+          const int b = i / 4;
+          seen[i] = t01[b] >= 0 && !all_see(c, lo, hi, t01[b]) && sees(c, p, t01[b] + 4 * g + i % 4) ? 1 : 0;
+        }
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            half8 x = __builtin_bit_cast(half8, widen<false>(v[0][h][i], v[1][h][i])), bad;
+            const u4 ones = widen<false>(code_nans(v1[0][h][i]) & 0x38383838u, code_nans(v1[1][h][i]) & 0x38383838u);    // the code of 1
+            const f4 count = Operand<false>::mma16(ones, __builtin_bit_cast(u4, seen), f4{0, 0, 0, 0});
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              bad[j] = x[j] != x[j] ? 1 : 0;
-              x[j] = x[j] != x[j] ? 0 : x[j];
-            }
-            f4 &y = acc[h * 4 + i];
-            y = Operand<false>::mma16(__builtin_bit_cast(u4, x), weights, y);
-            const f4 count = Operand<false>::mma16(__builtin_bit_cast(u4, bad), __builtin_bit_cast(u4, seen), f4{0, 0, 0, 0});
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = count[j] > 0 ? __builtin_nanf("") : y[j];
+            for (int j = 0; j < 4; ++j) acc[h * 4 + i][j] = count[j] > 0 ? __builtin_nanf("") : acc[h * 4 + i][j];
           }
       }
-    }
 
     // the four waves' sums, relative to the largest of their maxima
     total += __shfl_xor(total, 16, kWave);
@@ -359,67 +431,65 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
       for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
     __syncthreads();
+    auto finish = [&](int col, int d, float x, float y, float m, float l) {
+      const float r = l == 0.f ? 0.f : 1.f / l;
+      const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
+      reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
+          (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+      if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+    };
     const bool whole = from == 0 && to == steps;
-    float *to_parts = a.parts + ((long)blockIdx.x * 2 + (from == 0)) * part_floats(D);
-    for (int i = threadIdx.x; i < cols * (D / 2); i += 256) {
-      const int col = i / (D / 2), d = i % (D / 2) * 2;
-      float t4 = fmaxf(fmaxf(tops[0][col], tops[1][col]), fmaxf(tops[2][col], tops[3][col])), l = 0, x = 0, y = 0;
+    // this share is number i of the (slot, head), which begins in worker w0; share 0 lies in that worker's second place, the others in the first
+    const long first = pos - from;
+    const int w0 = (int)(first / part.per), shares = (int)((first + steps - 1) / part.per) - w0 + 1, i = (int)blockIdx.x - w0;
+    auto share = [&](int k) { return a.parts + ((long)(w0 + k) * 2 + (k == 0)) * part_floats(D); };
+    auto store = [&](float *to_share) {
+      return [=](int col, int d, float x, float y, float m, float l) {
+        put(to_share + col * D + d, x, y);
+        if (d == 0) { put(to_share + kCols * D + col, m); put(to_share + kCols * (D + 1) + col, l); }
+      };
+    };
+    const auto to_mine = store(share(i));
+    for (int at = threadIdx.x; at < cols * (D / 2); at += 256) {
+      const int col = at / (D / 2), d = at % (D / 2) * 2;
+      const float m = fmaxf(fmaxf(tops[0][col], tops[1][col]), fmaxf(tops[2][col], tops[3][col]));
+      float l = 0, x = 0, y = 0;
 #pragma unroll
       for (int wv = 0; wv < 4; ++wv) {
-        l += totals[wv][col] * exp2_fast(tops[wv][col] - t4);
+        l += totals[wv][col] * exp2_fast(tops[wv][col] - m);
         x += sums[wv][col][d];
         y += sums[wv][col][d + 1];
       }
-      if (whole) {
-        const float r = l == 0.f ? 0.f : 1.f / l;
-        const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
-        reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
-            (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
-        if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (t4 - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
-      } else {
-        to_parts[col * D + d] = x;
-        to_parts[col * D + d + 1] = y;
-        if (d == 0) { to_parts[kCols * D + col] = t4; to_parts[kCols * (D + 1) + col] = l; }
+      if (whole) finish(col, d, x, y, m, l);
+      else to_mine(col, d, x, y, m, l);
+    }
+    if (!whole) {
+      // counters of a worker: of the (slot, head) that begins in it, of one that goes on, of the groups
+      const int group = i / kGroup, members = min(kGroup, shares - group * kGroup), groups = (shares + kGroup - 1) / kGroup;
+      int *counters = a.counters + 3 * (w0 + group * kGroup);
+      if (last_to_arrive(counters + (group > 0), members)) {
+        auto mine = [&](int k) { return share(group * kGroup + k); };
+        if (groups == 1) {
+          join<D>(members, cols, mine, finish);
+        } else {
+          join<D>(members, cols, mine, [&](int col, int d, float x, float y, float m, float l) {
+            *reinterpret_cast<float2 *>(&sums[0][col][d]) = make_float2(x, y);
+            if (d == 0) { tops[0][col] = m; totals[0][col] = l; }
+          });
+          __syncthreads();                           // every share is read: the first one's place is free
+          const auto to_first = store(share(group * kGroup));
+          for (int at = threadIdx.x; at < cols * (D / 2); at += 256) {
+            const int col = at / (D / 2), d = at % (D / 2) * 2;
+            to_first(col, d, sums[0][col][d], sums[0][col][d + 1], tops[0][col], totals[0][col]);
+          }
+          if (last_to_arrive(a.counters + 3 * w0 + 2, groups)) join<D>(groups, cols, [&](int k) { return share(k * kGroup); }, finish);
+        }
       }
     }
     __syncthreads();
     pos += to - from;
     in_slot += to - from;
     if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
-  }
-}
-
-// The (slot, head) that begins in worker w's part and ends behind it.
-template <bool BF16, int D>
-__global__ __launch_bounds__(256) void few_join_kernel(Pages c, AttendArgs a, int workers)
-{
-  const int G = c.q_per_kv, w = blockIdx.x;
-  const Part part = part_of<true>(c, a, w, workers);
-  if (part.begin >= part.end) return;
-  const int s = part.slot, steps = steps_of(c, a, s), head = (int)(part.in_slot / steps);
-  const long first = part.end - 1 - part.in_slot % steps, last = first + steps;
-  if (first < part.begin || last <= part.end) return;
-  const int n = (int)((last - 1) / part.per) - w + 1;
-  const Rows rows = slot_rows(a.start, s, a.rows);
-  const int cols = rows.count * G;
-  const float *base = a.parts + (long)w * 2 * part_floats(D);
-  auto from = [&](int i) { return base + (i == 0 ? 1 : 2 * i) * (long)part_floats(D); };
-  for (int i = threadIdx.x; i < cols * (D / 2); i += 256) {
-    const int col = i / (D / 2), d = i % (D / 2) * 2;
-    float top = kLowest;
-    for (int k = 0; k < n; ++k) top = fmaxf(top, from(k)[kCols * D + col]);
-    float l = 0, x = 0, y = 0;
-    for (int k = 0; k < n; ++k) {
-      const float *f = from(k), e = exp2_fast(f[kCols * D + col] - top);
-      l = fmaf(f[kCols * (D + 1) + col], e, l);
-      x = fmaf(f[col * D + d], e, x);
-      y = fmaf(f[col * D + d + 1], e, y);
-    }
-    const float r = l == 0.f ? 0.f : 1.f / l;
-    const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
-    reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
-        (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
-    if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
   }
 }
 
@@ -746,10 +816,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, l
 template <bool BF16, int D>
 hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
 {
-  if (c.q_per_kv <= kCols) {
-    few_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a);
-    few_join_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a, kWorkers);
-  }
+  if (c.q_per_kv <= kCols) few_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a);
   if ((long)a.max_new * c.q_per_kv > kCols) {
     const long items = wide_items(c.slots, c.q_per_kv, a.rows);
     const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);

@@ -105,21 +105,21 @@ class PagedCache:
             setattr(d, name, t.data_ptr())
         if buffers is None:
             self.table, self.exps = self.table.view(slots, table_len), self.exps.view(layers, pages, heads, page_tokens // BLOCK, 2)
-        self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)   # (zeros: lessdec.h)
         d.workspace, d.workspace_bytes = self.workspace.data_ptr(), need
         self.desc = d
         if buffers is None:
             self.reset()
 
     def _call(self, name, stream, *args):
-        torch = self.torch
-        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        torch, index = self.torch, self.device.index
+        s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
         f = getattr(lib(), name)
-        if torch.cuda.current_device() == self.device.index:
-            rc = f(self.desc, *args, s.cuda_stream)
+        if torch.cuda.current_device() == index:
+            rc = f(self.desc, *args, s)
         else:
-            with torch.cuda.device(self.device):
-                rc = f(self.desc, *args, s.cuda_stream)
+            with torch.cuda.device(index):
+                rc = f(self.desc, *args, s)
         if rc:
             _check(rc, name)
 
