@@ -114,7 +114,10 @@ __device__ inline bool all_see(const Pages &c, int lo, int hi, int t0)
 // the shares in the order of the tokens: 32 neighbours first, then the joined ones, so that one sequence can be spread over the chip.
 
 constexpr int kCols = 16, kStepBlocks = 8;
-constexpr int kWorkers = kPagesWorkers, kGroup = 32;
+constexpr int kGroup = 32;
+// Three workgroups to a compute unit; where that would make more than 32 shares of a (slot, head) down to one, which reads as
+// fast (one sequence of 131072 tokens, 8 heads: 54 us with 256 workgroups, 61 with 512, 64 with 768).
+inline int few_workers(long items) { return (int)(items * kGroup < 256 ? 256 : items * kGroup < kPagesWorkers ? items * kGroup : kPagesWorkers); }
 
 __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
 {
@@ -199,14 +202,16 @@ __device__ inline float2 get(const float *p)
 __device__ inline void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ inline float get1(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Whether this workgroup is the last of n to arrive; the counter is 0 again then.  What the workgroup stored before is in memory,
-// and what the others stored is seen behind it.
+// Whether this workgroup is the last of n to arrive; the counter is 0 again then.  The shares go past the L2 of the die both ways (put,
+// get), so that all it takes is that a wave's stores are done before it is counted.  Ordered by acquire and release instead, every
+// arrival writes back and invalidates the L2 under the other workgroups' reads: 64 slots of up to 8192 tokens took 160 us, in place of 111.
 __device__ inline bool last_to_arrive(int *counter, int n)
 {
   __shared__ int arrived;
-  __syncthreads();                                   // (waits for the stores)
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  __syncthreads();
   if (threadIdx.x == 0) {
-    arrived = __hip_atomic_fetch_add(counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    arrived = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
     if (arrived == n) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
@@ -284,33 +289,34 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
           q[h][i] = reinterpret_cast<const u4 *>(a.q)[(rows.first + n / G) * (a.stride / 8) + (head * G + n % G) * (D / 8) + h * 8 + g * 2 + i];
       }
 
-    // Two blocks a step.  Pages are looked up two steps ahead of their use, codes are requested one step ahead.
+    // A wave's blocks are looked up 64 at a time, a lane each: two of every step.  The next step's keys are requested as soon as this one's
+    // are multiplied, its values likewise; every load is made (of the last step's blocks behind it, of the pool's first block where
+    // there is none): with a branch around it the compiler would wait for all loads where it means to wait for the older ones.
     const int *table = c.table + (size_t)s * c.table_len;
-    auto page_at = [&](int step, int b) {
-      const int i = step * kStepBlocks + wave * 2 + b;
-      return step < to && i < span.count ? table[entry_of(c, span.block(i))] : -1;
+    u4 k[2][H], v[2][H];
+    int ats, exs, base, end;                         // the lane's block in the pool, or -1, and its exponents; steps [base, end)
+    auto look = [&](int step) {
+      base = step;
+      end = min(to, base + kWave / 2);
+      const int i = (base + lane / 2) * kStepBlocks + wave * 2 + (lane & 1), block = span.block(i);
+      const bool there = base + lane / 2 < to && i < span.count;
+      const int page = table[there ? entry_of(c, block) : 0];
+      ats = there ? block_in(c, page, head, block) : -1;
+      exs = reinterpret_cast<const unsigned short *>(c.exps)[max(ats, 0)];
     };
-    u4 k[2][H], v[2][H], k1[2][H], v1[2][H];
-    unsigned ex[2], ex1[2];
-    int t0[2], t01[2], page[2];
-    auto request = [&](int step) {
+    auto request = [&](u4 (&x)[2][H], const unsigned char *codes, int step) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int block = span.block(step * kStepBlocks + wave * 2 + b);
-        const int at = block_in(c, page[b], head, block);
-        t01[b] = at >= 0 ? block * kBlock : -1;
-        ex1[b] = 0;
+        const int at = max(__builtin_amdgcn_readlane(ats, (min(step, end - 1) - base) * 2 + b), 0);
+        const unsigned char *from_block = codes + at * ((long)kBlock * D);
+        asm("" : "+s"(from_block));                  // (the address stays scalar: one with the lane's offset in it takes a register that loads wait for)
 #pragma unroll
-        for (int h = 0; h < H; ++h) k1[b][h] = v1[b][h] = u4{0, 0, 0, 0};
-        if (at >= 0) {
-          ex1[b] = reinterpret_cast<const unsigned short *>(c.exps)[at];
-#pragma unroll
-          for (int h = 0; h < H; ++h) {
-            k1[b][h] = reinterpret_cast<const u4 *>(c.k + at * ((long)kBlock * D))[h * kWave + lane];
-            v1[b][h] = reinterpret_cast<const u4 *>(c.v + at * ((long)kBlock * D))[h * kWave + lane];
-          }
-        }
+        for (int h = 0; h < H; ++h) x[b][h] = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(from_block + (unsigned)(h * kWave + lane) * 16));
       }
+    };
+    auto tokens_of = [&](int step, int b) {          // the first token of a block, -1: not there
+      const int at = __builtin_amdgcn_readlane(ats, (step - base) * 2 + b);
+      return at >= 0 ? span.block(step * kStepBlocks + wave * 2 + b) * kBlock : -1;
     };
 
     f4 acc[T];
@@ -318,20 +324,11 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
     for (int t = 0; t < T; ++t) acc[t] = f4{0, 0, 0, 0};
     float top = kLowest, total = 0;
     bool spoiled = false;
-    page[0] = page_at(from, 0); page[1] = page_at(from, 1);
-    request(from);
-    page[0] = page_at(from + 1, 0); page[1] = page_at(from + 1, 1);
-    for (int step = from; step < to; ++step) {
+    auto attend_to = [&](int step) {
+      const int t0[2] = {tokens_of(step, 0), tokens_of(step, 1)};
+      int ex[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        t0[b] = t01[b]; ex[b] = ex1[b];
-#pragma unroll
-        for (int h = 0; h < H; ++h) { k[b][h] = k1[b][h]; v[b][h] = v1[b][h]; }
-      }
-      request(step + 1);
-      page[0] = page_at(step + 2, 0); page[1] = page_at(step + 2, 1);
-      if (t0[0] < 0 && t0[1] < 0) continue;
-
+      for (int b = 0; b < 2; ++b) ex[b] = t0[b] < 0 ? 0 : __builtin_amdgcn_readlane(exs, (step - base) * 2 + b);
       f4 x[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -341,6 +338,7 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
           for (int i = 0; i < 2; ++i) x[b] = Operand<BF16>::mma16(widen<BF16>(k[b][h][2 * i], k[b][h][2 * i + 1]), q[h][i], x[b]);
       }
+      request(k, c.k, step + 1);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
         if (t0[b] < 0 || !all_see(c, lo, hi, t0[b])) {
@@ -398,23 +396,30 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           acc[h * 4 + i] = Operand<false>::mma16(widen<false>(v[0][h][i], v[1][h][i]), weights, acc[h * 4 + i]);
+      request(v, c.v, step + 1);
+    };
+    for (int chunk = from; chunk < to; chunk += kWave / 2) {
+      look(chunk);
+      request(k, c.k, chunk);
+      request(v, c.v, chunk);
+      for (int step = chunk; step < end; ++step) attend_to(step);
     }
     if (__ballot(spoiled))                           // the NaN that were taken out, counted for the rows that see them
 #pragma unroll 1
       for (int step = from; step < to; ++step) {
-        page[0] = page_at(step, 0); page[1] = page_at(step, 1);
-        request(step);
+        look(step);
+        request(v, c.v, step);
         half8 seen;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int b = i / 4;
-          seen[i] = t01[b] >= 0 && !all_see(c, lo, hi, t01[b]) && sees(c, p, t01[b] + 4 * g + i % 4) ? 1 : 0;
+          const int t0 = tokens_of(step, i / 4);
+          seen[i] = t0 >= 0 && !all_see(c, lo, hi, t0) && sees(c, p, t0 + 4 * g + i % 4) ? 1 : 0;
         }
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const u4 ones = widen<false>(code_nans(v1[0][h][i]) & 0x38383838u, code_nans(v1[1][h][i]) & 0x38383838u);    // the code of 1
+            const u4 ones = widen<false>(code_nans(v[0][h][i]) & 0x38383838u, code_nans(v[1][h][i]) & 0x38383838u);    // the code of 1
             const f4 count = Operand<false>::mma16(ones, __builtin_bit_cast(u4, seen), f4{0, 0, 0, 0});
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[h * 4 + i][j] = count[j] > 0 ? __builtin_nanf("") : acc[h * 4 + i][j];
@@ -816,7 +821,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, l
 template <bool BF16, int D>
 hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
 {
-  if (c.q_per_kv <= kCols) few_kernel<BF16, D><<<kWorkers, 256, 0, st>>>(c, a);
+  if (c.q_per_kv <= kCols) few_kernel<BF16, D><<<few_workers((long)c.slots * c.heads), 256, 0, st>>>(c, a);
   if ((long)a.max_new * c.q_per_kv > kCols) {
     const long items = wide_items(c.slots, c.q_per_kv, a.rows);
     const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
@@ -830,7 +835,7 @@ hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
 
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows)
 {
-  size_t n = q_per_kv <= kCols ? (size_t)kWorkers * 2 * part_floats(head_dim) : 0;
+  size_t n = q_per_kv <= kCols ? (size_t)kPagesWorkers * 2 * part_floats(head_dim) : 0;
   if ((long)rows * q_per_kv > kCols) {
     long items = wide_items(slots, q_per_kv, rows) * heads, fewest = wide_items(slots, q_per_kv, 0) * heads;
     if (fewest < kEnough) {
