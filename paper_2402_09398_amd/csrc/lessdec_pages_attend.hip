@@ -27,6 +27,7 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kSlack = 8.f, kBase = 6.f;           // weights reach 2^(kBase + kSlack) = 2^14 (fp16: below 2^16), normal down to 2^-14
+constexpr float kMost = 32768.f;                     // of a sum of weights: no one is more
 
 template <bool BF16> struct Operand;
 template <> struct Operand<false> {
@@ -655,75 +656,117 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     request(from + 1);
     page = look(from + 2);
   }
-  for (int tile = from; tile < to; ++tile) {
-    __syncthreads();
-    const int buf = tile & 1, ex_staged = ex_next;
-    if (tile + 1 < to) {
-      stage(tile + 1, buf ^ 1);
-      request(tile + 2);
-      page = look(tile + 3);
-    }
-    int e[4], t0[4];
-    bool whole = true, some = false;
+  // A tile's 64 tokens are worked on as two halves: the scores of the second are multiplied while the weights of the first are
+  // computed, and its weights while the first half's go into the values.
+  int e[4], t0[4];
+  bool whole, active;
+  f16v x[2];
+  auto enter = [&](int tile) {
+    whole = true;
+    active = false;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       const int i = tile * 4 + b;
       e[b] = __builtin_amdgcn_readlane(ex, b);
       t0[b] = e[b] < kNone ? span.block(i) * kBlock : -1;
       whole &= t0[b] >= 0 && all_see(c, wave_lo, wave_hi, t0[b]);
-      some |= t0[b] >= 0 && t0[b] <= wave_hi && (c.window == 0 || t0[b] + kBlock > wave_lo - c.window || t0[b] < c.sinks);
+      active |= have && t0[b] >= 0 && t0[b] <= wave_hi && (c.window == 0 || t0[b] + kBlock > wave_lo - c.window || t0[b] < c.sinks);
     }
-    ex = ex_staged;
-    if (!have || !some) continue;
-    f16v x[2];
+  };
+  auto scores = [&](int buf, int m) {
+    x[m] = f16v{0};
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      x[m] = f16v{0};
+    for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+  };
+  auto mask = [&](int m) {
 #pragma unroll
-      for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+    for (int i = 0; i < 16; ++i) {
+      const int b = 2 * m + i / 8, token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2 & 1);
+      const bool seen = t0[b] >= 0 && sees(c, p, token);
+      x[m][i] = seen ? x[m][i] : -__builtin_inff();
     }
-    if (!whole) {
+  };
+  // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
+  // only looked for where one is: then M is moved and the weights are computed again.
+  u4 weights[2];
+  float part[2];
+  auto weigh = [&](int m) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 2; ++b) {
+      const int n = 2 * m + b;
+      const float factor = pow2((signed char)e[n]) * c.scale_log2, zero = (float)(signed char)(e[n] >> 8) - (top - kBase);
+      part[b] = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2);
-          const bool seen = t0[b] >= 0 && sees(c, p, token);
-          x[b / 2][b % 2 * 8 + i] = seen ? x[b / 2][b % 2 * 8 + i] : -__builtin_inff();
-        }
+      for (int i = 0; i < 8; i += 2) {
+        const float y = exp2_fast(fmaf(x[m][b * 8 + i], factor, zero)), z = exp2_fast(fmaf(x[m][b * 8 + i + 1], factor, zero));
+        part[b] += y + z;
+        weights[b][i / 2] = half_pair(y, z);
+      }
     }
-    // t = factor x + ve; the factor is positive, so a block's largest x gives its largest t
-    float most = kLowest, factor[4];
+  };
+  auto settle = [&](int m) {
+    if (__ballot(fmaxf(part[0], part[1]) > kMost)) {
+      float most = kLowest;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      factor[b] = pow2((signed char)e[b]) * c.scale_log2;
-      float y = x[b / 2][b % 2 * 8];
+      for (int b = 0; b < 2; ++b) {
+        const int n = 2 * m + b;
+        float y = x[m][b * 8];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) y = fmaxf(y, x[b / 2][b % 2 * 8 + i]);
-      most = fmaxf(most, fmaf(y, factor[b], (float)(signed char)(e[b] >> 8)));
-    }
-    if (__ballot(most > top + kSlack)) {
+        for (int i = 1; i < 8; ++i) y = fmaxf(y, x[m][b * 8 + i]);      // (the factor is positive)
+        most = fmaxf(most, fmaf(y, pow2((signed char)e[n]) * c.scale_log2, (float)(signed char)(e[n] >> 8)));
+      }
       most = fmaxf(most, __shfl_xor(most, 32, kWave));
       const float now = fmaxf(top, most), f = exp2_fast(top - now);
       top = now;
       sum *= f;
 #pragma unroll
       for (int o = 0; o < OB; ++o) acc[o] *= f;
+      weigh(m);
     }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const float zero = (float)(signed char)(e[b] >> 8) - (top - kBase);
-      float part = 0;
-      u4 weights;
+    for (int b = 0; b < 2; ++b) sum = fmaf(part[b], pow2(-(signed char)(e[2 * m + b] >> 8)), sum);
+  };
+  auto gather = [&](int buf, int m, const u4 (&w)[2]) {
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float y = exp2_fast(fmaf(x[b / 2][b % 2 * 8 + i], factor[b], zero)), z = exp2_fast(fmaf(x[b / 2][b % 2 * 8 + i + 1], factor[b], zero));
-        part += y + z;
-        weights[i / 2] = half_pair(y, z);
-      }
-      sum = fmaf(part, pow2(-(signed char)(e[b] >> 8)), sum);
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][(b * OB + o) * 64 + lane], weights, acc[o]);
+      for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][((2 * m + b) * OB + o) * 64 + lane], w[b], acc[o]);
+  };
+#pragma unroll
+  for (int k = 0; k < KK; ++k) asm volatile("" : "+v"(q[k]));          // the queries are waited for here, not (with all codes requested since) in the loop
+  __syncthreads();
+  if (from < to) {
+    enter(from);
+    if (active) {
+      scores(from & 1, 0);
+      if (!whole) mask(0);
+    }
+  }
+  for (int tile = from; tile < to; ++tile) {
+    const int buf = tile & 1;
+    ex = ex_next;
+    if (tile + 1 < to) {                             // (requested a round ago)
+      stage(tile + 1, buf ^ 1);
+      request(tile + 2);
+      page = look(tile + 3);
+    }
+    if (active) {
+      scores(buf, 1);
+      weigh(0);
+      settle(0);
+      if (!whole) mask(1);
+      const u4 first[2] = {weights[0], weights[1]};
+      gather(buf, 0, first);
+      weigh(1);
+      settle(1);
+      gather(buf, 1, weights);
+    }
+    if (tile + 1 == to) break;
+    __syncthreads();
+    enter(tile + 1);
+    if (active) {
+      scores(buf ^ 1, 0);
+      if (!whole) mask(0);
     }
   }
 
