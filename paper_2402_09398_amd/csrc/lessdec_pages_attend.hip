@@ -106,6 +106,17 @@ __device__ inline bool all_see(const Pages &c, int lo, int hi, int t0)
   return t0 + kBlock - 1 <= lo && (c.window == 0 || t0 > hi - c.window || t0 + kBlock <= c.sinks);
 }
 
+// Tiles of four blocks that rows up to position hi, from position lo on, see in full: from this one on, and before this one.  (The first
+// tokens' blocks before a window are not among them.)
+__device__ inline int inner_first(const Pages &c, const Span &s, int hi)
+{
+  if (c.window == 0 || hi < c.window) return 0;
+  const int block = (hi - c.window + kBlock) / kBlock;                 // the first whose tokens are all > hi - window
+  return (max(block - s.window, 0) + s.sinks + 3) / 4;
+}
+__device__ inline int inner_last(const Span &s, int lo) { return max((lo + 1) / kBlock - s.window + s.sinks, 0) / 4; }
+__device__ inline float read_lane(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+
 // ---- few rows a slot: up to 16 query columns -----------------------------------------------------------------------------
 //
 // Bound by the read of the cache.  The work is a list of steps, 128 tokens of a slot and head each, that is dealt out evenly to as many
@@ -575,62 +586,83 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     if (col <= last_col) q[k] = reinterpret_cast<const u4 *>(a.q)[row * (a.stride / 8) + q_head * (D / 8) + k * 2 + h];
   }
 
-  // Staging.  Lanes 0-3 (and their repetitions) look up a tile's four blocks: the table three tiles ahead, the exponents with the codes two
-  // ahead.  A wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.
+  // Tiles that all rows of the workgroup, of this wave, see in full: a range [first, last) of the list.
+  const int all_first = inner_first(c, span, hi), all_last = inner_last(span, lo);
+  const int mine_first = inner_first(c, span, wave_hi), mine_last = inner_last(span, wave_lo);
+
+  // Blocks are looked up for sixteen tiles at a time, a lane each: the table a chunk ahead, the exponents half a chunk ahead.
+  constexpr int kChunk = kWave / 4;
   const int *table = c.table + (size_t)t.slot * c.table_len;
-  auto look = [&](int tile) {
-    const int i = tile * 4 + (lane & 3);
-    return tile < to && i < span.count ? table[entry_of(c, span.block(i))] : -1;
+  int chunk = from, page, at, at_next, exps_next;    // at: the lane's block in the pool, -1: not there
+  float factor, shift, unit;                         // of the lane's block: t = factor x + shift; its weights add to the sum times unit
+  auto look = [&](int tile) {                        // of the chunk that begins with this tile
+    const int i = tile * 4 + lane;
+    const bool there = i < to * 4 && i < span.count;
+    const int found = table[there ? entry_of(c, span.block(i)) : 0];
+    page = there ? found : -1;
   };
-  constexpr int kNone = 0x10000;                     // an exponent word of a block that is not there
+  auto place = [&](int tile) {
+    at_next = block_in(c, page, head, span.block(tile * 4 + lane));
+    exps_next = reinterpret_cast<const unsigned short *>(c.exps)[max(at_next, 0)];
+  };
+  auto turn = [&] {
+    at = at_next;
+    factor = pow2((signed char)exps_next) * c.scale_log2;
+    const int e = (signed char)(exps_next >> 8);
+    shift = (float)e;
+    unit = pow2(-e);
+  };
+  auto at_of = [&](int tile, int b) {
+    const int i = (tile - chunk) * 4 + b;
+    return i < kWave ? __builtin_amdgcn_readlane(at, i) : __builtin_amdgcn_readlane(at_next, i - kWave);
+  };
+  auto lacks = [&](int tile) {                       // one of the tile's blocks is not there
+    const int i = (tile - chunk) * 4;
+    return i < kWave ? (__ballot(at < 0) >> i & 15) != 0 : (__ballot(at_next < 0) >> (i - kWave) & 15) != 0;
+  };
+
+  // Staging.  A wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.  Every load
+  // is made (of the pool's first block where there is none to read).
   u4 kc[H], vc[H];
-  int page, ex_next;
+  auto piece_block = [&](int j) { return H == 2 ? wave / 2 + 2 * j : wave; };
+  const int half = H == 2 ? wave % 2 : 0;
   auto request = [&](int tile) {
-    const int at = block_in(c, page, head, span.block(tile * 4 + (lane & 3)));
-    ex_next = kNone;
-    if (at >= 0) ex_next = reinterpret_cast<const unsigned short *>(c.exps)[at];
+    if (tile >= to) return;
 #pragma unroll
     for (int j = 0; j < H; ++j) {
-      const int block = __builtin_amdgcn_readlane(at, H == 2 ? wave / 2 + 2 * j : wave), half = H == 2 ? wave % 2 : 0;
-      kc[j] = vc[j] = u4{0, 0, 0, 0};
-      if (block >= 0) {
-        kc[j] = reinterpret_cast<const u4 *>(c.k + block * ((long)kBlock * D))[half * kWave + lane];
-        vc[j] = reinterpret_cast<const u4 *>(c.v + block * ((long)kBlock * D))[half * kWave + lane];
-      }
+      const int block = max(at_of(tile, piece_block(j)), 0);
+      const unsigned char *k = c.k + block * ((long)kBlock * D), *v = c.v + block * ((long)kBlock * D);
+      asm("" : "+s"(k), "+s"(v));                    // (scalar addresses)
+      kc[j] = *reinterpret_cast<const u4 *>(k + (unsigned)(half * kWave + lane) * 16);
+      vc[j] = *reinterpret_cast<const u4 *>(v + (unsigned)(half * kWave + lane) * 16);
     }
   };
   // where a word of four tokens' codes of channel 64 half + 16 i + (lane & 15) goes: [block][32 channels][which eight of the 16
   // tokens][channel], tokens 0-3 and 8-11, or 4-7 and 12-15
   auto value_at = [&](int j, int i) {
-    const int b = H == 2 ? wave / 2 + 2 * j : wave, d = (H == 2 ? wave % 2 : 0) * 64 + i * 16 + (lane & 15), g = lane >> 4;
-    return (((b * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1);
-  };
-  auto is_edge = [&](int tile) {                     // some row of the workgroup does not see all of the tile
-    bool whole = true;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int i = tile * 4 + b;
-      whole &= i < span.count && all_see(c, lo, hi, span.block(i) * kBlock);
-    }
-    return !whole;
+    const int d = half * 64 + i * 16 + (lane & 15), g = lane >> 4;
+    return (((piece_block(j) * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1);
   };
   bool mine_spoiled = false;
   auto stage = [&](int tile, int buf) {
     const int tok = lane & 15, g = lane >> 4;
-    // a NaN among values that only some rows see is taken out (0 * NaN is NaN) and given to those that see it in the end
-    if (is_edge(tile)) {
+    // what no row sees is left out, and a NaN among values that only some rows see is taken out (0 * NaN is NaN) and given to those
+    // that see it in the end
+    if (tile < all_first || tile >= all_last || lacks(tile)) {
 #pragma unroll
-      for (int j = 0; j < H; ++j)
+      for (int j = 0; j < H; ++j) {
+        const bool there = at_of(tile, piece_block(j)) >= 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const unsigned bad = code_nans(vc[j][i]);
-          mine_spoiled |= bad != 0;
-          vc[j][i] &= ~bad;
+          mine_spoiled |= there && bad != 0;
+          vc[j][i] = there ? vc[j][i] & ~bad : 0;
         }
+      }
     }
 #pragma unroll
     for (int j = 0; j < H; ++j) {
-      const int b = H == 2 ? wave / 2 + 2 * j : wave, half = H == 2 ? wave % 2 : 0;
+      const int b = piece_block(j);
       // key operands: [32 tokens][16 channels][half of 8 channels][token]
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -646,31 +678,39 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   for (int o = 0; o < OB; ++o) acc[o] = f16v{0};
   float top = kLowest, sum = 0;
   if (threadIdx.x == 0) spoiled = 0;
-  int ex = kNone;
   if (from < to) {
-    page = look(from);
+    look(from);
+    place(from);
+    turn();
+    look(from + kChunk);
     request(from);
-    page = look(from + 1);
     stage(from, from & 1);
-    ex = ex_next;
     request(from + 1);
-    page = look(from + 2);
   }
+
   // A tile's 64 tokens are worked on as two halves: the scores of the second are multiplied while the weights of the first are
   // computed, and its weights while the first half's go into the values.
-  int e[4], t0[4];
   bool whole, active;
+  float f[4], add[4], units[4];
   f16v x[2];
   auto enter = [&](int tile) {
-    whole = true;
-    active = false;
+    const int i = (tile - chunk) * 4;
+    whole = tile >= mine_first && tile < mine_last && !lacks(tile);
+    active = have;
+    if (!whole) {
+      bool some = false;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int t0 = span.block(tile * 4 + b) * kBlock;
+        some |= at_of(tile, b) >= 0 && t0 <= wave_hi && (c.window == 0 || t0 + kBlock > wave_lo - c.window || t0 < c.sinks);
+      }
+      active &= some;
+    }
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      const int i = tile * 4 + b;
-      e[b] = __builtin_amdgcn_readlane(ex, b);
-      t0[b] = e[b] < kNone ? span.block(i) * kBlock : -1;
-      whole &= t0[b] >= 0 && all_see(c, wave_lo, wave_hi, t0[b]);
-      active |= have && t0[b] >= 0 && t0[b] <= wave_hi && (c.window == 0 || t0[b] + kBlock > wave_lo - c.window || t0[b] < c.sinks);
+      f[b] = read_lane(factor, i + b);
+      add[b] = read_lane(shift, i + b);
+      units[b] = read_lane(unit, i + b);
     }
   };
   auto scores = [&](int buf, int m) {
@@ -678,11 +718,11 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 #pragma unroll
     for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
   };
-  auto mask = [&](int m) {
+  auto mask = [&](int tile, int m) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int b = 2 * m + i / 8, token = t0[b] + (i & 3) + 4 * h + 8 * (i >> 2 & 1);
-      const bool seen = t0[b] >= 0 && sees(c, p, token);
+      const int b = 2 * m + i / 8, token = span.block(tile * 4 + b) * kBlock + (i & 3) + 4 * h + 8 * (i >> 2 & 1);
+      const bool seen = at_of(tile, b) >= 0 && sees(c, p, token);
       x[m][i] = seen ? x[m][i] : -__builtin_inff();
     }
   };
@@ -693,12 +733,11 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   auto weigh = [&](int m) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int n = 2 * m + b;
-      const float factor = pow2((signed char)e[n]) * c.scale_log2, zero = (float)(signed char)(e[n] >> 8) - (top - kBase);
+      const float zero = add[2 * m + b] - (top - kBase);
       part[b] = 0;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const float y = exp2_fast(fmaf(x[m][b * 8 + i], factor, zero)), z = exp2_fast(fmaf(x[m][b * 8 + i + 1], factor, zero));
+        const float y = exp2_fast(fmaf(x[m][b * 8 + i], f[2 * m + b], zero)), z = exp2_fast(fmaf(x[m][b * 8 + i + 1], f[2 * m + b], zero));
         part[b] += y + z;
         weights[b][i / 2] = half_pair(y, z);
       }
@@ -709,22 +748,21 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       float most = kLowest;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int n = 2 * m + b;
         float y = x[m][b * 8];
 #pragma unroll
         for (int i = 1; i < 8; ++i) y = fmaxf(y, x[m][b * 8 + i]);      // (the factor is positive)
-        most = fmaxf(most, fmaf(y, pow2((signed char)e[n]) * c.scale_log2, (float)(signed char)(e[n] >> 8)));
+        most = fmaxf(most, fmaf(y, f[2 * m + b], add[2 * m + b]));
       }
       most = fmaxf(most, __shfl_xor(most, 32, kWave));
-      const float now = fmaxf(top, most), f = exp2_fast(top - now);
+      const float now = fmaxf(top, most), less = exp2_fast(top - now);
       top = now;
-      sum *= f;
+      sum *= less;
 #pragma unroll
-      for (int o = 0; o < OB; ++o) acc[o] *= f;
+      for (int o = 0; o < OB; ++o) acc[o] *= less;
       weigh(m);
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) sum = fmaf(part[b], pow2(-(signed char)(e[2 * m + b] >> 8)), sum);
+    for (int b = 0; b < 2; ++b) sum = fmaf(part[b], units[2 * m + b], sum);
   };
   auto gather = [&](int buf, int m, const u4 (&w)[2]) {
 #pragma unroll
@@ -739,22 +777,21 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     enter(from);
     if (active) {
       scores(from & 1, 0);
-      if (!whole) mask(0);
+      if (!whole) mask(from, 0);
     }
   }
   for (int tile = from; tile < to; ++tile) {
     const int buf = tile & 1;
-    ex = ex_next;
+    if (tile - chunk == kChunk / 2) place(chunk + kChunk);
     if (tile + 1 < to) {                             // (requested a round ago)
       stage(tile + 1, buf ^ 1);
       request(tile + 2);
-      page = look(tile + 3);
     }
     if (active) {
       scores(buf, 1);
       weigh(0);
       settle(0);
-      if (!whole) mask(1);
+      if (!whole) mask(tile, 1);
       const u4 first[2] = {weights[0], weights[1]};
       gather(buf, 0, first);
       weigh(1);
@@ -763,10 +800,15 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     }
     if (tile + 1 == to) break;
     __syncthreads();
+    if (tile + 1 - chunk == kChunk) {
+      turn();
+      chunk += kChunk;
+      look(chunk + kChunk);
+    }
     enter(tile + 1);
     if (active) {
       scores(buf ^ 1, 0);
-      if (!whole) mask(0);
+      if (!whole) mask(tile + 1, 0);
     }
   }
 
@@ -774,8 +816,11 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   __syncthreads();
   if (spoiled)                                       // the NaN that were taken out, counted for the rows that see them
     for (int tile = from; tile < to; ++tile) {
-      if (!is_edge(tile)) continue;
-      page = look(tile);
+      chunk = tile;
+      look(tile);
+      place(tile);
+      at = at_next;
+      if (tile >= all_first && tile < all_last && !lacks(tile)) continue;
       request(tile);
 #pragma unroll
       for (int j = 0; j < H; ++j)
@@ -787,10 +832,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       __syncthreads();
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const int e = __builtin_amdgcn_readlane(ex_next, b), t0 = e < kNone ? span.block(tile * 4 + b) * kBlock : -1;
+        const int t0 = span.block(tile * 4 + b) * kBlock;
         half8 seen;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) seen[i] = t0 >= 0 && sees(c, p, t0 + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
+        for (int i = 0; i < 8; ++i) seen[i] = at_of(tile, b) >= 0 && sees(c, p, t0 + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
 #pragma unroll
         for (int o = 0; o < OB; ++o) {
           const f16v count = Operand<false>::mma32(values[0][(b * OB + o) * 64 + lane], __builtin_bit_cast(u4, seen), f16v{0});
@@ -803,20 +848,20 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 
   sum += __shfl_xor(sum, 32, kWave);
   if (splits > 1) {
-    float *part = a.parts + (item * splits + split) * wide_floats(D);
-    const int at = wave * 32 + n;
+    float *share = a.parts + (item * splits + split) * wide_floats(D);
+    const int mine = wave * 32 + n;
     if (from < to)
 #pragma unroll
       for (int o = 0; o < OB; ++o)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f4 *>(part + at * D + o * 32 + i * 8 + h * 4) = f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]};
-    if (h == 0) { part[kWide * D + at] = top; part[kWide * (D + 1) + at] = sum; }
+          *reinterpret_cast<f4 *>(share + mine * D + o * 32 + i * 8 + h * 4) = f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]};
+    if (h == 0) { share[kWide * D + mine] = top; share[kWide * (D + 1) + mine] = sum; }
     return;
   }
   if (col > last_col) return;
   const float r = sum == 0.f ? 0.f : 1.f / sum;
-  const long at = (long)row * c.heads * G + q_head;
+  const long to_row = (long)row * c.heads * G + q_head;
 #pragma unroll
   for (int o = 0; o < OB; ++o)
 #pragma unroll
@@ -824,9 +869,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       uint2 y;
       y.x = (unsigned)Operand<BF16>::store(acc[o][4 * i] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 1] * r) << 16;
       y.y = (unsigned)Operand<BF16>::store(acc[o][4 * i + 2] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 3] * r) << 16;
-      reinterpret_cast<uint2 *>(a.out)[at * (D / 4) + o * 8 + i * 2 + h] = y;
+      reinterpret_cast<uint2 *>(a.out)[to_row * (D / 4) + o * 8 + i * 2 + h] = y;
     }
-  if (a.lse && h == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(sum)) * 0.6931471805599453f;
+  if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(sum)) * 0.6931471805599453f;
 }
 
 // 32 columns of an item to a workgroup.
