@@ -29,6 +29,17 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kSlack = 8.f, kBase = 6.f;           // weights reach 2^(kBase + kSlack) = 2^14 (fp16: below 2^16), normal down to 2^-14
 constexpr float kMost = 32768.f;                     // of a sum of weights: no one is more
 
+// A lane's 16 bytes at a scalar address.  The asm keeps the address from being added to the lane's offset in vector registers, which loads in
+// flight would then be waited for; the pointer says that it is global memory, which the compiler no longer sees.
+typedef const __attribute__((address_space(1))) unsigned char *Bytes;
+typedef const __attribute__((address_space(1))) u4 *Pieces;
+__device__ inline Bytes scalar_bytes(const unsigned char *base, long offset)
+{
+  Bytes p = (Bytes)base + offset;
+  asm("" : "+s"(p));
+  return p;
+}
+
 template <bool BF16> struct Operand;
 template <> struct Operand<false> {
   typedef half8 Vec;
@@ -320,10 +331,9 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int at = max(__builtin_amdgcn_readlane(ats, (min(step, end - 1) - base) * 2 + b), 0);
-        const unsigned char *from_block = codes + at * ((long)kBlock * D);
-        asm("" : "+s"(from_block));                  // (the address stays scalar: one with the lane's offset in it takes a register that loads wait for)
+        const Bytes block = scalar_bytes(codes, at * ((long)kBlock * D));
 #pragma unroll
-        for (int h = 0; h < H; ++h) x[b][h] = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(from_block + (unsigned)(h * kWave + lane) * 16));
+        for (int h = 0; h < H; ++h) x[b][h] = __builtin_nontemporal_load((Pieces)(block + (unsigned)(h * kWave + lane) * 16));
       }
     };
     auto tokens_of = [&](int step, int b) {          // the first token of a block, -1: not there
@@ -597,12 +607,11 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   float factor, shift, unit;                         // of the lane's block: t = factor x + shift; its weights add to the sum times unit
   auto look = [&](int tile) {                        // of the chunk that begins with this tile
     const int i = tile * 4 + lane;
-    const bool there = i < to * 4 && i < span.count;
-    const int found = table[there ? entry_of(c, span.block(i)) : 0];
-    page = there ? found : -1;
+    page = table[i < to * 4 && i < span.count ? entry_of(c, span.block(i)) : 0];      // (not looked at here: it is on its way)
   };
   auto place = [&](int tile) {
-    at_next = block_in(c, page, head, span.block(tile * 4 + lane));
+    const int i = tile * 4 + lane;
+    at_next = i < to * 4 && i < span.count ? block_in(c, page, head, span.block(i)) : -1;
     exps_next = reinterpret_cast<const unsigned short *>(c.exps)[max(at_next, 0)];
   };
   auto turn = [&] {
@@ -631,10 +640,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 #pragma unroll
     for (int j = 0; j < H; ++j) {
       const int block = max(at_of(tile, piece_block(j)), 0);
-      const unsigned char *k = c.k + block * ((long)kBlock * D), *v = c.v + block * ((long)kBlock * D);
-      asm("" : "+s"(k), "+s"(v));                    // (scalar addresses)
-      kc[j] = *reinterpret_cast<const u4 *>(k + (unsigned)(half * kWave + lane) * 16);
-      vc[j] = *reinterpret_cast<const u4 *>(v + (unsigned)(half * kWave + lane) * 16);
+      const Bytes k = scalar_bytes(c.k, block * ((long)kBlock * D)), v = scalar_bytes(c.v, block * ((long)kBlock * D));
+      kc[j] = *(Pieces)(k + (unsigned)(half * kWave + lane) * 16);
+      vc[j] = *(Pieces)(v + (unsigned)(half * kWave + lane) * 16);
     }
   };
   // where a word of four tokens' codes of channel 64 half + 16 i + (lane & 15) goes: [block][32 channels][which eight of the 16
