@@ -721,10 +721,22 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       units[b] = read_lane(unit, i + b);
     }
   };
+  // The first operands of a product are read from the LDS ahead of what comes before it, so that it does not begin with a wait.
+  constexpr int kAhead = 4;
+  u4 ahead[kAhead];
+  auto keys_ahead = [&](int buf, int m) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ahead[k] = keys[buf][(m * KK + k) * 64 + lane];
+  };
+  auto values_ahead = [&](int buf, int m) {
+#pragma unroll
+    for (int o = 0; o < kAhead; ++o) ahead[o] = values[buf][(2 * m * OB + o) * 64 + lane];
+  };
   auto scores = [&](int buf, int m) {
     x[m] = f16v{0};
 #pragma unroll
-    for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+    for (int k = 0; k < KK; ++k)
+      x[m] = Operand<BF16>::mma32(k < kAhead ? ahead[k] : keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
   };
   auto mask = [&](int tile, int m) {
 #pragma unroll
@@ -776,7 +788,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int o = 0; o < OB; ++o) acc[o] = Operand<false>::mma32(values[buf][((2 * m + b) * OB + o) * 64 + lane], w[b], acc[o]);
+      for (int o = 0; o < OB; ++o)
+        acc[o] = Operand<false>::mma32(b * OB + o < kAhead ? ahead[b * OB + o] : values[buf][((2 * m + b) * OB + o) * 64 + lane], w[b], acc[o]);
   };
 #pragma unroll
   for (int k = 0; k < KK; ++k) asm volatile("" : "+v"(q[k]));          // the queries are waited for here, not (with all codes requested since) in the loop
@@ -784,12 +797,14 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   if (from < to) {
     enter(from);
     if (active) {
+      keys_ahead(from & 1, 0);
       scores(from & 1, 0);
       if (!whole) mask(from, 0);
     }
   }
   for (int tile = from; tile < to; ++tile) {
     const int buf = tile & 1;
+    keys_ahead(buf, 1);
     if (tile - chunk == kChunk / 2) place(chunk + kChunk);
     if (tile + 1 < to) {                             // (requested a round ago)
       stage(tile + 1, buf ^ 1);
@@ -798,11 +813,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     if (active) {
       scores(buf, 1);
       weigh(0);
+      values_ahead(buf, 0);
       settle(0);
       if (!whole) mask(tile, 1);
       const u4 first[2] = {weights[0], weights[1]};
       gather(buf, 0, first);
       weigh(1);
+      values_ahead(buf, 1);
       settle(1);
       gather(buf, 1, weights);
     }
@@ -815,6 +832,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     }
     enter(tile + 1);
     if (active) {
+      keys_ahead(buf ^ 1, 0);
       scores(buf ^ 1, 0);
       if (!whole) mask(tile + 1, 0);
     }
