@@ -596,9 +596,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     if (col <= last_col) q[k] = reinterpret_cast<const u4 *>(a.q)[row * (a.stride / 8) + q_head * (D / 8) + k * 2 + h];
   }
 
-  // Tiles that all rows of the workgroup, of this wave, see in full: a range [first, last) of the list.
-  const int all_first = inner_first(c, span, hi), all_last = inner_last(span, lo);
-  const int mine_first = inner_first(c, span, wave_hi), mine_last = inner_last(span, wave_lo);
+  // Tiles that all rows of the workgroup, of this wave, see in full: a range [first, last) of the list, none where a page of the
+  // slot is missing (which the look-ups below find before such a tile is reached).
+  const int all_first = inner_first(c, span, hi), mine_first = inner_first(c, span, wave_hi);
+  int all_last = inner_last(span, lo), mine_last = inner_last(span, wave_lo);
 
   // Blocks are looked up for sixteen tiles at a time, a lane each: the table a chunk ahead, the exponents half a chunk ahead.
   constexpr int kChunk = kWave / 4;
@@ -613,6 +614,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     const int i = tile * 4 + lane;
     at_next = i < to * 4 && i < span.count ? block_in(c, page, head, span.block(i)) : -1;
     exps_next = reinterpret_cast<const unsigned short *>(c.exps)[max(at_next, 0)];
+    if (__ballot(at_next < 0 && i < to * 4 && i < span.count)) all_last = mine_last = 0;
   };
   auto turn = [&] {
     at = at_next;
@@ -622,12 +624,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     unit = pow2(-e);
   };
   auto at_of = [&](int tile, int b) {
-    const int i = (tile - chunk) * 4 + b;
-    return i < kWave ? __builtin_amdgcn_readlane(at, i) : __builtin_amdgcn_readlane(at_next, i - kWave);
-  };
-  auto lacks = [&](int tile) {                       // one of the tile's blocks is not there
-    const int i = (tile - chunk) * 4;
-    return i < kWave ? (__ballot(at < 0) >> i & 15) != 0 : (__ballot(at_next < 0) >> (i - kWave) & 15) != 0;
+    const int i = tile - chunk;
+    return __builtin_amdgcn_readlane(i < kChunk ? at : at_next, i % kChunk * 4 + b);
   };
 
   // Staging.  A wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.  Every load
@@ -656,7 +654,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
     const int tok = lane & 15, g = lane >> 4;
     // what no row sees is left out, and a NaN among values that only some rows see is taken out (0 * NaN is NaN) and given to those
     // that see it in the end
-    if (tile < all_first || tile >= all_last || lacks(tile)) {
+    if (tile < all_first || tile >= all_last) {
 #pragma unroll
       for (int j = 0; j < H; ++j) {
         const bool there = at_of(tile, piece_block(j)) >= 0;
@@ -703,7 +701,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   f16v x[2];
   auto enter = [&](int tile) {
     const int i = (tile - chunk) * 4;
-    whole = tile >= mine_first && tile < mine_last && !lacks(tile);
+    whole = tile >= mine_first && tile < mine_last;
     active = have;
     if (!whole) {
       bool some = false;
@@ -824,13 +822,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       gather(buf, 1, weights);
     }
     if (tile + 1 == to) break;
-    __syncthreads();
     if (tile + 1 - chunk == kChunk) {
       turn();
       chunk += kChunk;
       look(chunk + kChunk);
     }
     enter(tile + 1);
+    __syncthreads();
     if (active) {
       keys_ahead(buf ^ 1, 0);
       scores(buf ^ 1, 0);
@@ -846,7 +844,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       look(tile);
       place(tile);
       at = at_next;
-      if (tile >= all_first && tile < all_last && !lacks(tile)) continue;
+      if (tile >= all_first && tile < all_last) continue;
       request(tile);
 #pragma unroll
       for (int j = 0; j < H; ++j)
