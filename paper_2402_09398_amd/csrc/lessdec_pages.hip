@@ -53,7 +53,7 @@ __global__ void reset_kernel(Pages c)
 // One workgroup.  free_list: [pages].
 __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n_new, int *granted, int *plan, int *free_list)
 {
-  __shared__ int open_page[kMaxSlots];               // the shared page that the slot goes on filling, or -1
+  __shared__ __align__(16) int open_page[kMaxSlots]; // the shared page that the slot goes on filling, or -1
   __shared__ int upto[kMaxSlots];                    // pages needed by the slots up to this one
   __shared__ int want[kMaxSlots];                    // pages needed by this one
   __shared__ long sums[kWaves];
@@ -83,14 +83,17 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
   }
 
   // what each slot needs; a thread has the slots tid, tid + kThreads, ..
-  int old_page[kTurns], pair[kTurns];
+  int wanted[kTurns], length[kTurns], old_page[kTurns], pair[kTurns];
 #pragma unroll
   for (int t = 0; t < kTurns; ++t) {
     const int s = tid + t * kThreads;
     old_page[t] = pair[t] = -1;
+    wanted[t] = length[t] = 0;
     if (s >= c.slots) continue;
     const int n = n_new[s], len = slot_length(c, s);
-    if (n > 0 && len + (long)n <= room && len % pt) {
+    wanted[t] = n > 0 && len + (long)n <= room ? n : 0;
+    length[t] = len;
+    if (wanted[t] && len % pt) {
       const int p = c.table[(size_t)s * c.table_len + len / pt];
       old_page[t] = (unsigned)p < (unsigned)c.pages ? p : -1;
     }
@@ -103,21 +106,22 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
     if (t * kThreads >= c.slots) break;
     const int s = tid + t * kThreads;
     int need = 0, copies = 0;
-    if (s < c.slots) {
-      const int n = n_new[s], len = slot_length(c, s);
-      if (n > 0 && len + (long)n <= room) {
-        int own = 0;                                 // a new page in the place of the partly filled one: shared, or not there
-        if (len % pt) {
-          const int p = old_page[t], sharers = p >= 0 ? count_of(c.refs, p) : 0;
-          if (sharers > 1) {
-            int before = 0;                          // slots before this one that write to the same page
-            for (int i = 0; i < s; ++i) before += open_page[i] == p;
-            copies = sharers - before > 1;
+    if (wanted[t]) {
+      const int n = wanted[t], len = length[t];
+      int own = 0;                                   // a new page in the place of the partly filled one: shared, or not there
+      if (len % pt) {
+        const int p = old_page[t], sharers = p >= 0 ? count_of(c.refs, p) : 0;
+        if (sharers > 1) {
+          int before = 0;                            // slots before this one that write to the same page
+          for (int i = 0; i < s; i += 4) {
+            const int4 o = *reinterpret_cast<const int4 *>(open_page + i);
+            before += (o.x == p) + (i + 1 < s && o.y == p) + (i + 2 < s && o.z == p) + (i + 3 < s && o.w == p);
           }
-          own = p < 0 || copies;
+          copies = sharers - before > 1;
         }
-        need = (int)((len + (long)n + pt - 1) / pt) - (len + pt - 1) / pt + own;
+        own = p < 0 || copies;
       }
+      need = (int)((len + (long)n + pt - 1) / pt) - (len + pt - 1) / pt + own;
     }
     long all;                                        // both sums in one word: 2^12 slots of less than 2^27 pages each
     const long x = scan_exclusive<long>(need | (long)copies << 48, sums, all) + before_turn;
@@ -167,8 +171,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
   for (int t = 0; t < kTurns; ++t) {
     const int s = tid + t * kThreads;
     if (s >= c.slots) continue;
-    const int n = n_new[s], len = slot_length(c, s), need = want[s];
-    const bool wants = n > 0 && len + (long)n <= room, fits = wants && upto[s] <= found;
+    const int n = wanted[t], len = length[t], need = want[s];
+    const bool fits = n && upto[s] <= found;
     if (granted) granted[s] = fits ? n : 0;
     if (!fits) {
       want[s] = 0;
@@ -196,9 +200,10 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
   }
   if (tid == 0) plan[0] = pairs;
   __syncthreads();                                   // lengths are read up to here
-  for (int s = tid; s < c.slots; s += kThreads) {
-    const int n = n_new[s], len = slot_length(c, s);
-    if (n > 0 && len + (long)n <= room && upto[s] <= found) c.length[s] = len + n;
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int s = tid + t * kThreads;
+    if (wanted[t] && upto[s] <= found) c.length[s] = length[t] + wanted[t];
   }
 }
 
@@ -206,26 +211,30 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
 // last workgroup has the lengths.
 __global__ __launch_bounds__(256) void select_kernel(Pages c, const int *from, int columns)
 {
-  extern __shared__ int old[];
+  extern __shared__ int shared[];
   const bool lengths = blockIdx.x == gridDim.x - 1;
   const int wide = lengths ? 1 : columns, base = blockIdx.x * columns;
+  int *old = shared, *more = shared + c.slots * wide;                  // more[f]: slots that get slot f's entries, less f itself if it loses them
   for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
     const int s = i / wide, j = base + i % wide;
     old[i] = lengths ? c.length[s] : j < c.table_len ? c.table[(size_t)s * c.table_len + j] : -1;
   }
+  for (int s = threadIdx.x; s < c.slots; s += 256) more[s] = 0;
+  __syncthreads();
+  for (int s = threadIdx.x; s < c.slots; s += 256) {
+    const int f = from[s];
+    if (f == s || f < -1 || f >= c.slots) continue;
+    atomicSub(more + s, 1);
+    if (f >= 0) atomicAdd(more + f, 1);
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
-    const int s = i / wide, j = base + i % wide, f = from[s];
+    const int s = i / wide, j = base + i % wide, f = from[s], was = old[i];
+    if (!lengths && more[s] && (unsigned)was < (unsigned)c.pages) atomicAdd(c.refs + was, more[s]);
     if (f == s || f < -1 || f >= c.slots) continue;
-    const int was = old[i], now = f < 0 ? (lengths ? 0 : -1) : old[f * wide + i % wide];
-    if (was == now) continue;
-    if (lengths) {
-      c.length[s] = now;
-    } else if (j < c.table_len) {
-      c.table[(size_t)s * c.table_len + j] = now;
-      if ((unsigned)was < (unsigned)c.pages) atomicSub(c.refs + was, 1);
-      if ((unsigned)now < (unsigned)c.pages) atomicAdd(c.refs + now, 1);
-    }
+    const int now = f < 0 ? (lengths ? 0 : -1) : old[f * wide + i % wide];
+    if (lengths) c.length[s] = now;
+    else if (j < c.table_len) c.table[(size_t)s * c.table_len + j] = now;
   }
 }
 
@@ -292,8 +301,10 @@ __global__ void rename_kernel(Pages c, const int *moved)
   }
 }
 
-// 16 KiB of a page's keys or values to a workgroup at a time, 64 bytes a thread in flight.
+// 16 KiB of a page's keys and as much of its values to a workgroup at a time, 128 bytes a thread in flight; non-temporal, as nothing of it is
+// read again soon.
 constexpr int kPiece = 16384;
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
 __global__ __launch_bounds__(256) void copy_kernel(Pages c, int layers, const int *plan, int max_pairs)
 {
   const int n = plan[0] < max_pairs ? plan[0] : max_pairs;
@@ -305,16 +316,16 @@ __global__ __launch_bounds__(256) void copy_kernel(Pages c, int layers, const in
     const int from = plan[1 + 2 * pair], to = plan[2 + 2 * pair];
     if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages) continue;
     const long a = ((long)layer * c.pages + from) * page, b = ((long)layer * c.pages + to) * page;
-    uint4 x[8];
+    u4 x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const long at = (long)piece * kPiece + (i / 2) * 4096 + threadIdx.x * 16;
-      if (at < page) x[i] = *reinterpret_cast<const uint4 *>((i & 1 ? c.v : c.k) + a + at);
+      if (at < page) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u4 *>((i & 1 ? c.v : c.k) + a + at));
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const long at = (long)piece * kPiece + (i / 2) * 4096 + threadIdx.x * 16;
-      if (at < page) *reinterpret_cast<uint4 *>((i & 1 ? c.v : c.k) + b + at) = x[i];
+      if (at < page) __builtin_nontemporal_store(x[i], reinterpret_cast<u4 *>((i & 1 ? c.v : c.k) + b + at));
     }
     if (piece == 0) {
       const unsigned short *e = reinterpret_cast<const unsigned short *>(c.exps) + ((long)layer * c.pages + from) * scales;
@@ -347,8 +358,8 @@ hipError_t launch_pages_reserve(const Pages &c, const int *n_new, int *granted, 
 
 hipError_t launch_pages_select(const Pages &c, const int *from, hipStream_t st)
 {
-  const int columns = c.slots <= 1024 ? 16 : 65536 / 4 / c.slots;      // 64 KiB of LDS at most; 64 bytes of a row where they fit
-  select_kernel<<<(c.table_len + columns - 1) / columns + 1, 256, (size_t)c.slots * columns * sizeof(int), st>>>(c, from, columns);
+  const int columns = c.slots <= 960 ? 16 : 65536 / 4 / c.slots - 1;   // 64 KiB of LDS at most; 64 bytes of a row where they fit
+  select_kernel<<<(c.table_len + columns - 1) / columns + 1, 256, (size_t)c.slots * (columns + 1) * sizeof(int), st>>>(c, from, columns);
   return hipGetLastError();
 }
 
@@ -363,7 +374,7 @@ hipError_t launch_pages_copy(const Pages &c, int layers, const int *plan, int ma
 {
   const long page = (long)c.heads * c.page_tokens * c.head_dim;
   const long items = (long)max_pairs * layers * ((page + kPiece - 1) / kPiece);
-  copy_kernel<<<(unsigned)(items < 2048 ? items : 2048), 256, 0, st>>>(c, layers, plan, max_pairs);
+  copy_kernel<<<(unsigned)(items < 16384 ? items : 16384), 256, 0, st>>>(c, layers, plan, max_pairs);
   return hipGetLastError();
 }
 

@@ -898,7 +898,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(sum)) * 0.6931471805599453f;
 }
 
-// 32 columns of an item to a workgroup.
+// Eight columns of an item to a workgroup, eight shares on their way at a time.
+constexpr int kJoinColumns = 8;
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, long items, int splits)
 {
@@ -909,18 +910,34 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, l
   Rows rows;
   if (!columns_of(c, a, item % items, t, rows)) return;
   const float *base = a.parts + item * splits * wide_floats(D);
-  for (int i = threadIdx.x; i < 32 * (D / 2); i += 256) {
-    const int at = blockIdx.y * 32 + i / (D / 2), d = i % (D / 2) * 2, col = t.first + at;
+  for (int i = threadIdx.x; i < kJoinColumns * (D / 2); i += 256) {
+    const int at = blockIdx.y * kJoinColumns + i / (D / 2), d = i % (D / 2) * 2, col = t.first + at;
     if (col >= t.count) return;
-    float top = kLowest;
-    for (int k = 0; k < splits; ++k) top = fmaxf(top, base[(long)k * wide_floats(D) + kWide * D + at]);
-    float l = 0, x = 0, y = 0;
-    for (int k = 0; k < splits; ++k) {
-      const float *f = base + (long)k * wide_floats(D), m = f[kWide * D + at], e = exp2_fast(m - top);
-      if (m == kLowest) continue;                    // nothing seen there, nothing written
-      l = fmaf(f[kWide * (D + 1) + at], e, l);
-      x = fmaf(f[at * D + d], e, x);
-      y = fmaf(f[at * D + d + 1], e, y);
+    float top = kLowest, l = 0, x = 0, y = 0;
+    for (int k = 0; k < splits; k += 8) {
+      float m[8], u[8];
+      float2 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float *f = base + (long)min(k + j, splits - 1) * wide_floats(D);
+        m[j] = k + j < splits ? f[kWide * D + at] : kLowest;
+        u[j] = f[kWide * (D + 1) + at];
+        v[j] = *reinterpret_cast<const float2 *>(f + at * D + d);
+      }
+      float now = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) now = fmaxf(now, m[j]);
+      const float less = exp2_fast(top - now);
+      top = now;
+      l *= less; x *= less; y *= less;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (m[j] == kLowest) continue;               // nothing seen there, nothing written
+        const float e = exp2_fast(m[j] - top);
+        l = fmaf(u[j], e, l);
+        x = fmaf(v[j].x, e, x);
+        y = fmaf(v[j].y, e, y);
+      }
     }
     const float r = l == 0.f ? 0.f : 1.f / l;
     const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
@@ -938,7 +955,7 @@ hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
     const long items = wide_items(c.slots, c.q_per_kv, a.rows);
     const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
     wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits), 256, 0, st>>>(c, a, items, splits);
-    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / 32), 256, 0, st>>>(c, a, items, splits);
+    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, items, splits);
   }
   return hipGetLastError();
 }

@@ -61,6 +61,23 @@ __device__ inline unsigned four_codes(float a, float b, float c, float d)
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+typedef short s2 __attribute__((ext_vector_type(2)));
+// codes of four elements over a power of two, none of them beyond 448 times it
+template <bool BF16> __device__ inline unsigned four_codes(unsigned a, unsigned b, float scale)
+{
+  s2 w = {0, 0};
+  if constexpr (BF16) {
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(v2, a), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(v2, b), scale, true);
+  } else {
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(v2, a), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(v2, b), scale, true);
+  }
+  return __builtin_bit_cast(unsigned, w);
+}
 // four codes, rounded again for an exponent that is larger by shift (factor = 2^-shift)
 __device__ inline unsigned again(unsigned w, float factor)
 {
@@ -118,20 +135,33 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   }
   const unsigned was = off > 0 ? *exps : 0;
 
+  // The largest magnitude, on the elements' bits, two at a time; where one is not finite, once more without those.
+  constexpr unsigned kInf = BF16 ? 0x7f80u : 0x7c00u;
   int e[2], shift[2];
+  bool odd[2];                                       // a block with elements that are not finite, or beyond the largest exponent
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
-    unsigned m = 0;
+    us2 most = {0, 0};
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const unsigned word = (&x[which][h][i / 4].x)[i % 4];
-        const unsigned lo = magnitude(element<BF16>((unsigned short)word)), hi = magnitude(element<BF16>((unsigned short)(word >> 16)));
-        m = m > lo ? m : lo;
-        m = m > hi ? m : hi;
-      }
-    e[which] = exponent_of(wave_max(m));
+      for (int i = 0; i < 8; ++i)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, (&x[which][h][i / 4].x)[i % 4] & 0x7fff7fffu));
+    unsigned m = wave_max(most[0] > most[1] ? most[0] : most[1]);
+    odd[which] = m >= kInf;
+    if (odd[which]) {
+      m = 0;
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const unsigned y = (&x[which][h][i / 8].x)[i / 2 % 4] >> 16 * (i % 2) & 0x7fffu;
+          m = y < kInf && y > m ? y : m;
+        }
+      m = wave_max(m);
+    }
+    e[which] = exponent_of(__float_as_uint(element<BF16>((unsigned short)m)));
+    odd[which] |= e[which] == kTop;
     shift[which] = 0;
     if (off > 0) {
       int before = (signed char)(which ? was >> 8 : was);
@@ -146,6 +176,15 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   uint4 code[2][H];
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    if (!odd[which]) {
+      const float scale = pow2(e[which]);
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          (&code[which][h].x)[i] = four_codes<BF16>((&x[which][h][i / 2].x)[i % 2 * 2], (&x[which][h][i / 2].x)[i % 2 * 2 + 1], scale);
+      continue;
+    }
     const float inverse = pow2(-e[which]);
 #pragma unroll
     for (int h = 0; h < H; ++h)
