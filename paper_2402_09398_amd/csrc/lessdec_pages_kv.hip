@@ -85,6 +85,11 @@ __device__ inline unsigned again(unsigned w, float factor)
   return four_codes(a[0] * factor, a[1] * factor, b[0] * factor, b[1] * factor);
 }
 
+// whole lines of rows that are read, or written, once
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+__device__ inline uint4 load_once(const uint4 *p) { return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p))); }
+__device__ inline void store_once(uint4 *p, uint4 x) { __builtin_nontemporal_store(__builtin_bit_cast(u4, x), reinterpret_cast<u4 *>(p)); }
+
 constexpr int kRowPad = 16;                          // bytes behind a token's codes in the LDS: the four tokens of a group in other banks
 
 // Block b of a slot's new tokens: the wave's index less start[s] / 16 + 2 s, which leaves every slot as many waves as it can
@@ -111,12 +116,21 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   if (block < 0) return;
   const int off = begin > t0 ? begin - t0 : 0;                         // older tokens of the block
 
-  const int tok = lane & 15, g = lane >> 4;
-  const bool fresh = tok >= off && t0 + tok < len;
+  // A lane has eight channels of two tokens (of every 64 channels), eight lanes a line of a token's row; of the cache a piece of 16 bytes of
+  // every half block: of the values four channels of four tokens.
+  const int piece = lane & 7, g = lane >> 4;
+  int tok[2];
+  bool fresh[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    tok[i] = (lane >> 3) + 8 * i;
+    fresh[i] = tok[i] >= off && t0 + tok[i] < len;
+  }
   unsigned short *exps = reinterpret_cast<unsigned short *>(c.exps) + block;
-  uint4 *kb = reinterpret_cast<uint4 *>(c.k + block * ((long)kBlock * D)) + lane, *vb = reinterpret_cast<uint4 *>(c.v + block * ((long)kBlock * D)) + lane;
+  unsigned char *kb = c.k + block * ((long)kBlock * D);
+  uint4 *vb = reinterpret_cast<uint4 *>(c.v + block * ((long)kBlock * D)) + lane;
+  auto key_at = [&](int h, int i) { return reinterpret_cast<uint2 *>(kb + h * 1024 + ((piece >> 1) * 16 + tok[i]) * 16 + (piece & 1) * 8); };
   uint4 x[2][H][2];
-  const long row = (long)(row0 + t0 + tok - begin) * (a.stride / 8) + head * (D / 8);
 #pragma unroll
   for (int which = 0; which < 2; ++which)
 #pragma unroll
@@ -124,7 +138,8 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         x[which][h][i] = make_uint4(0, 0, 0, 0);
-        if (fresh) x[which][h][i] = reinterpret_cast<const uint4 *>(which ? a.v : a.k)[row + h * 8 + g * 2 + i];
+        if (fresh[i])
+          x[which][h][i] = load_once(reinterpret_cast<const uint4 *>(which ? a.v : a.k) + (long)(row0 + t0 + tok[i] - begin) * (a.stride / 8) + head * (D / 8) + h * 8 + piece);
       }
   uint4 old[H];
   const bool mixed = off > 0 && 4 * g + 3 >= off && t0 + 4 * g < len;  // the lane's four tokens of a value piece are not all older
@@ -172,50 +187,48 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   }
   if (lane == 0) *exps = (unsigned short)((e[0] & 255) | (e[1] & 255) << 8);
 
-  // codes of the lane's sixteen channels of a token
-  uint4 code[2][H];
+  // codes of the lane's eight channels of a token
+  uint2 code[2][H][2];
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
-    if (!odd[which]) {
-      const float scale = pow2(e[which]);
-#pragma unroll
-      for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          (&code[which][h].x)[i] = four_codes<BF16>((&x[which][h][i / 2].x)[i % 2 * 2], (&x[which][h][i / 2].x)[i % 2 * 2 + 1], scale);
-      continue;
-    }
-    const float inverse = pow2(-e[which]);
+    const float scale = pow2(e[which]), inverse = pow2(-e[which]);
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned p = (&x[which][h][i / 2].x)[i % 2 * 2], q = (&x[which][h][i / 2].x)[i % 2 * 2 + 1];
-        (&code[which][h].x)[i] = four_codes(scaled(element<BF16>((unsigned short)p), inverse), scaled(element<BF16>((unsigned short)(p >> 16)), inverse),
-                                            scaled(element<BF16>((unsigned short)q), inverse), scaled(element<BF16>((unsigned short)(q >> 16)), inverse));
-      }
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const unsigned p = (&x[which][h][i].x)[2 * j], q = (&x[which][h][i].x)[2 * j + 1];
+          unsigned &w = (&code[which][h][i].x)[j];
+          if (!odd[which])
+            w = four_codes<BF16>(p, q, scale);
+          else
+            w = four_codes(scaled(element<BF16>((unsigned short)p), inverse), scaled(element<BF16>((unsigned short)(p >> 16)), inverse),
+                           scaled(element<BF16>((unsigned short)q), inverse), scaled(element<BF16>((unsigned short)(q >> 16)), inverse));
+        }
   }
 
-  // keys: a lane's piece is one token's
-  if (fresh || off == 0) {                                             // (the rest of a new block: zeros)
 #pragma unroll
-    for (int h = 0; h < H; ++h) kb[h * kWave] = code[0][h];
-  } else if (shift[0] && tok < off) {
-    const float factor = pow2(-shift[0]);
+  for (int i = 0; i < 2; ++i) {
+    if (fresh[i] || off == 0) {                                        // (the rest of a new block: zeros)
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      uint4 k = kb[h * kWave];
+      for (int h = 0; h < H; ++h) *key_at(h, i) = code[0][h][i];
+    } else if (shift[0] && tok[i] < off) {
+      const float factor = pow2(-shift[0]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) (&k.x)[i] = again((&k.x)[i], factor);
-      kb[h * kWave] = k;
+      for (int h = 0; h < H; ++h) {
+        const uint2 k = *key_at(h, i);
+        *key_at(h, i) = make_uint2(again(k.x, factor), again(k.y, factor));
+      }
     }
   }
 
-  // values: a lane's piece is four channels of four tokens; the codes are turned in the LDS
+  // the values' codes are turned in the LDS
   unsigned char *mine = turned[wave];
 #pragma unroll
   for (int h = 0; h < H; ++h)
-    *reinterpret_cast<uint4 *>(mine + tok * (D + kRowPad) + h * 64 + g * 16) = code[1][h];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<uint2 *>(mine + tok[i] * (D + kRowPad) + h * 64 + piece * 8) = code[1][h][i];
   wave_lds_sync();
   const bool rescale = off > 0 && shift[1] > 0;
   if (off == 0 || mixed || rescale) {
@@ -258,50 +271,58 @@ __global__ __launch_bounds__(256) void read_kernel(Pages c, ReadArgs a)
   if (b * kBlock >= first + a.count) return;
   const long t0 = b * kBlock;
   const int block = t0 >= 0 && t0 < len ? block_index(c, s, head, (int)b) : -1;
-  uint4 k[H], v[H];
+  // of the cache and of the rows a lane has what it has when they are stored
+  const int piece = lane & 7, g = lane >> 4;
+  uint2 k[H][2], v[H][2];
+  uint4 turn[H];
   unsigned e = 0;
 #pragma unroll
-  for (int h = 0; h < H; ++h) k[h] = v[h] = make_uint4(0, 0, 0, 0);
+  for (int h = 0; h < H; ++h) {
+    turn[h] = make_uint4(0, 0, 0, 0);
+    k[h][0] = k[h][1] = make_uint2(0, 0);
+  }
   if (block >= 0) {
     e = reinterpret_cast<const unsigned short *>(c.exps)[block];
+    const unsigned char *kb = c.k + block * ((long)kBlock * D);
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      k[h] = reinterpret_cast<const uint4 *>(c.k + block * ((long)kBlock * D))[h * kWave + lane];
-      v[h] = reinterpret_cast<const uint4 *>(c.v + block * ((long)kBlock * D))[h * kWave + lane];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        k[h][i] = *reinterpret_cast<const uint2 *>(kb + h * 1024 + ((piece >> 1) * 16 + (lane >> 3) + 8 * i) * 16 + (piece & 1) * 8);
+      turn[h] = reinterpret_cast<const uint4 *>(c.v + block * ((long)kBlock * D))[h * kWave + lane];
     }
   }
   unsigned char *mine = turned[wave];
-  const int tok = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        mine[(4 * g + j) * (D + kRowPad) + h * 64 + t * 16 + (lane & 15)] = (unsigned char)((&v[h].x)[t] >> 8 * j);
+        mine[(4 * g + j) * (D + kRowPad) + h * 64 + t * 16 + (lane & 15)] = (unsigned char)((&turn[h].x)[t] >> 8 * j);
   wave_lds_sync();
-#pragma unroll
-  for (int h = 0; h < H; ++h) v[h] = *reinterpret_cast<const uint4 *>(mine + tok * (D + kRowPad) + h * 64 + g * 16);
-
-  const long at = t0 + tok - first;
-  if (at < 0 || at >= a.count) return;
-  const bool held = block >= 0 && t0 + tok < len;
-  const long row = (((long)i * c.heads + head) * a.count + at) * (D / 8);
   const float most = BF16 ? __uint_as_float(0x7f7f0000u) : 65504.f;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    int ex = (signed char)(which ? e >> 8 : e);
-    ex = ex < -kTop ? -kTop : ex < kTop ? ex : kTop;
-    const float scale = pow2(ex);
+  for (int half = 0; half < 2; ++half) {
+    const int tok = (lane >> 3) + 8 * half;
+    const long at = t0 + tok - first;
+    if (at < 0 || at >= a.count) continue;
+    const bool held = block >= 0 && t0 + tok < len;
+    const long row = (((long)i * c.heads + head) * a.count + at) * (D / 8);
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+    for (int h = 0; h < H; ++h) v[h][half] = *reinterpret_cast<const uint2 *>(mine + tok * (D + kRowPad) + h * 64 + piece * 8);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+    for (int which = 0; which < 2; ++which) {
+      int ex = (signed char)(which ? e >> 8 : e);
+      ex = ex < -kTop ? -kTop : ex < kTop ? ex : kTop;
+      const float scale = pow2(ex);
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
         uint4 out;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const uint4 &x = which ? v[h] : k[h];
-          const unsigned word = (&x.x)[half * 2 + n / 2];
+          const uint2 &x = which ? v[h][half] : k[h][half];
+          const unsigned word = (&x.x)[n / 2];
           const auto p = n % 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)word, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)word, false);
           unsigned pair = 0;
 #pragma unroll
@@ -312,8 +333,9 @@ __global__ __launch_bounds__(256) void read_kernel(Pages c, ReadArgs a)
           }
           (&out.x)[n] = pair;
         }
-        reinterpret_cast<uint4 *>(which ? a.v : a.k)[row + h * 8 + g * 2 + half] = out;
+        store_once(reinterpret_cast<uint4 *>(which ? a.v : a.k) + row + h * 8 + piece, out);
       }
+    }
   }
 }
 
