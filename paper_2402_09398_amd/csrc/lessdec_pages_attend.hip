@@ -588,7 +588,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   const int wave_last = min(t.first + wave * 32 + 31, last_col);
   const int wave_lo = before + (t.first + wave * 32) / G, wave_hi = before + wave_last / G;
   const bool have = t.first + wave * 32 <= last_col;
-  const int row = rows.first + col / G, q_head = head * G + col % G, p = col <= last_col ? before + col / G : -1;
+  const int row = rows.first + col / G, q_head = head * G + col % G;
+  // The row, at p, sees the tokens from_token .. from_token + seen_tokens - 1 and those before first_tokens: two compares a score (425
+  // us at 40 heads, 12288 tokens, a window of 4096, where four took 470).
+  const int p = col <= last_col ? before + col / G : -1;
+  const int from_token = c.window > 0 ? max(p - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
+  const unsigned seen_tokens = (unsigned)(p + 1 - from_token);
+  auto row_sees = [&](int token) { return (unsigned)(token - from_token) < seen_tokens || token < first_tokens; };
   u4 q[KK];
 #pragma unroll
   for (int k = 0; k < KK; ++k) {
@@ -738,10 +744,12 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   };
   auto mask = [&](int tile, int m) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int b = 2 * m + i / 8, token = span.block(tile * 4 + b) * kBlock + (i & 3) + 4 * h + 8 * (i >> 2 & 1);
-      const bool seen = at_of(tile, b) >= 0 && sees(c, p, token);
-      x[m][i] = seen ? x[m][i] : -__builtin_inff();
+    for (int b = 2 * m; b < 2 * m + 2; ++b) {
+      const int t0 = span.block(tile * 4 + b) * kBlock + 4 * h;
+      const bool there = at_of(tile, b) >= 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[m][b % 2 * 8 + i] = there && row_sees(t0 + (i & 3) + 8 * (i >> 2)) ? x[m][b % 2 * 8 + i] : -__builtin_inff();
     }
   };
   // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
@@ -802,6 +810,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   }
   for (int tile = from; tile < to; ++tile) {
     const int buf = tile & 1;
+    __builtin_amdgcn_s_setprio(0);
     keys_ahead(buf, 1);
     if (tile - chunk == kChunk / 2) place(chunk + kChunk);
     if (tile + 1 < to) {                             // (requested a round ago)
@@ -809,6 +818,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       request(tile + 2);
     }
     if (active) {
+      // products before the other workgroup's staging: 661 -> 621 us at 32 heads x 8192 tokens, clocks settled
+      __builtin_amdgcn_s_setprio(1);
       scores(buf, 1);
       weigh(0);
       values_ahead(buf, 0);
