@@ -19,6 +19,14 @@ __device__ inline int count_of(const int *refs, int p)
   return __hip_atomic_load(refs + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// The counts of the wave's next kSpan pages from `first` on, sixteen a lane.  Every load is made (of the last page behind the end): sixteen
+// conditional ones wait for one another (32k pages: the search took 8 us, now 2.5).
+__device__ inline void load_counts(const Pages &c, long first, int (&count)[16])
+{
+#pragma unroll
+  for (int k = 0; k < 16; ++k) count[k] = count_of(c.refs, (int)min(first + k * kWave + (long)(threadIdx.x & 63), (long)c.pages - 1));
+}
+
 // sum over the threads before this one; total: over all of them
 template <typename T>
 __device__ inline T scan_exclusive(T x, T *shared, T &total)
@@ -50,10 +58,10 @@ __global__ void reset_kernel(Pages c)
   for (long i = at; i < c.slots; i += stride) c.length[i] = 0;
 }
 
-// One workgroup.  free_list: [pages].
+// One workgroup.  free_list: [pages], the free pages from the kMaxSlots-th on (those before stay in the LDS).
 __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n_new, int *granted, int *plan, int *free_list)
 {
-  __shared__ __align__(16) int open_page[kMaxSlots]; // the shared page that the slot goes on filling, or -1
+  __shared__ __align__(16) int open_page[kMaxSlots]; // the page that the slot goes on filling, or -1; later the first of the free pages
   __shared__ int upto[kMaxSlots];                    // pages needed by the slots up to this one
   __shared__ int want[kMaxSlots];                    // pages needed by this one
   __shared__ long sums[kWaves];
@@ -79,8 +87,11 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
         if (__ballot(p < 0)) break;
       }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+  int counts[16];                                    // of the pages looked at first: on their way meanwhile
+  load_counts(c, (long)wave * kSpan, counts);
 
   // what each slot needs; a thread has the slots tid, tid + kThreads, ..
   int wanted[kTurns], length[kTurns], old_page[kTurns], pair[kTurns];
@@ -113,9 +124,15 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
         const int p = old_page[t], sharers = p >= 0 ? count_of(c.refs, p) : 0;
         if (sharers > 1) {
           int before = 0;                            // slots before this one that write to the same page
-          for (int i = 0; i < s; i += 4) {
-            const int4 o = *reinterpret_cast<const int4 *>(open_page + i);
-            before += (o.x == p) + (i + 1 < s && o.y == p) + (i + 2 < s && o.z == p) + (i + 3 < s && o.w == p);
+          for (int i = 0; i < s; i += 16) {
+            int4 o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = reinterpret_cast<const int4 *>(open_page + i)[q];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int at = i + 4 * q;
+              before += (at < s && o[q].x == p) + (at + 1 < s && o[q].y == p) + (at + 2 < s && o[q].z == p) + (at + 3 < s && o[q].w == p);
+            }
           }
           copies = sharers - before > 1;
         }
@@ -135,16 +152,14 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
   }
   const long total = before_turn & ((1L << 48) - 1);
 
-  // the first free pages, in order
-  int found = 0;
+  // the first free pages, in order (the scan above has synchronised: no one looks for an open page any more)
+  int *first_free = open_page, found = 0;
   for (long base = 0; base < c.pages && found < total; base += (long)kWaves * kSpan) {
-    unsigned long long free_of[16];
     int count = 0;
-    for (int k = 0; k < 16; ++k) {
-      const long p = base + (long)wave * kSpan + k * kWave + lane;
-      free_of[k] = __ballot(p < c.pages && count_of(c.refs, (int)(p < c.pages ? p : 0)) == 0);
-      count += __popcll(free_of[k]);
-    }
+    const long first = base + (long)wave * kSpan;
+    if (base) load_counts(c, first, counts);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) count += __popcll(__ballot(counts[k] == 0 && first + k * kWave + lane < c.pages));
     __syncthreads();
     if (lane == 0) page_sums[wave] = count;
     __syncthreads();
@@ -153,17 +168,21 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
       if (w < wave) at += page_sums[w];
       found += page_sums[w];
     }
-    for (int k = 0; k < 16; ++k) {
-      const int mine = at + __popcll(free_of[k] & ((1ull << lane) - 1));
-      if (free_of[k] >> lane & 1) free_list[mine] = (int)(base + (long)wave * kSpan + k * kWave + lane);
-      at += __popcll(free_of[k]);
-    }
+    if (at < total)                                  // (most waves are past the last page that is wanted)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const unsigned long long free_of = __ballot(counts[k] == 0 && first + k * kWave + lane < c.pages);
+        const int mine = at + __popcll(free_of & ((1ull << lane) - 1));
+        if ((free_of >> lane & 1) && mine < total) (mine < kMaxSlots ? first_free : free_list)[mine] = (int)(first + k * kWave + lane);
+        at += __popcll(free_of);
+      }
   }
-  __syncthreads();                                   // free_list and want, upto
+  __syncthreads();                                   // the free pages and want, upto
+  auto free_page = [&](int i) { return i < kMaxSlots ? first_free[i] : free_list[i]; };
 
   // tables: by the slot's thread where few pages are wanted, else by a wave
   auto take = [&](int s, int j, int need, int end) {
-    const int p = free_list[upto[s] - need + j];
+    const int p = free_page(upto[s] - need + j);
     c.table[(size_t)s * c.table_len + end - need + j] = p;
     c.refs[p] = 1;
   };
@@ -184,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
     if (pair[t] >= 0) {
       atomicSub(c.refs + old_page[t], 1);
       plan[1 + 2 * pair[t]] = old_page[t];
-      plan[2 + 2 * pair[t]] = free_list[upto[s] - need];
+      plan[2 + 2 * pair[t]] = free_page(upto[s] - need);
       atomicMax(&pairs, pair[t] + 1);
     }
   }
@@ -207,34 +226,48 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
   }
 }
 
-// A workgroup has some columns of the table, all slots of them, so that every old entry is read before one is written; the
-// last workgroup has the lengths.
-__global__ __launch_bounds__(256) void select_kernel(Pages c, const int *from, int columns)
+// A workgroup has 1 << shift columns of the table, all slots of them, so that every old entry is read before one is written; the
+// last workgroup has the lengths.  Loads are made four at a time, none of them conditional (64 slots of 133 entries: 4.2 us, 6.5 one by one).
+__global__ __launch_bounds__(256) void select_kernel(Pages c, const int *from, int shift)
 {
   extern __shared__ int shared[];
   const bool lengths = blockIdx.x == gridDim.x - 1;
-  const int wide = lengths ? 1 : columns, base = blockIdx.x * columns;
-  int *old = shared, *more = shared + c.slots * wide;                  // more[f]: slots that get slot f's entries, less f itself if it loses them
-  for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
-    const int s = i / wide, j = base + i % wide;
-    old[i] = lengths ? c.length[s] : j < c.table_len ? c.table[(size_t)s * c.table_len + j] : -1;
-  }
-  for (int s = threadIdx.x; s < c.slots; s += 256) more[s] = 0;
-  __syncthreads();
+  if (lengths) shift = 0;
+  const int base = blockIdx.x << shift, mask = (1 << shift) - 1, last = c.table_len - 1, n = c.slots << shift;
+  // more[f]: slots that get slot f's entries, less f itself if it loses them
+  int *old = shared, *source = shared + n, *more = source + c.slots;
   for (int s = threadIdx.x; s < c.slots; s += 256) {
     const int f = from[s];
-    if (f == s || f < -1 || f >= c.slots) continue;
+    source[s] = f < -1 || f >= c.slots ? s : f;
+    more[s] = 0;
+  }
+  for (int i = threadIdx.x; i < n; i += 4 * 256) {
+    int x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = min(i + k * 256, n - 1), s = e >> shift;
+      x[k] = *(lengths ? c.length + s : c.table + (size_t)s * c.table_len + min(base + (e & mask), last));
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * 256 < n) old[i + k * 256] = x[k];
+  }
+  __syncthreads();
+  for (int s = threadIdx.x; s < c.slots; s += 256) {
+    const int f = source[s];
+    if (f == s) continue;
     atomicSub(more + s, 1);
     if (f >= 0) atomicAdd(more + f, 1);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < c.slots * wide; i += 256) {
-    const int s = i / wide, j = base + i % wide, f = from[s], was = old[i];
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int s = i >> shift, j = base + (i & mask), f = source[s], was = old[i];
+    if (!lengths && j > last) continue;
     if (!lengths && more[s] && (unsigned)was < (unsigned)c.pages) atomicAdd(c.refs + was, more[s]);
-    if (f == s || f < -1 || f >= c.slots) continue;
-    const int now = f < 0 ? (lengths ? 0 : -1) : old[f * wide + i % wide];
+    if (f == s) continue;
+    const int now = f < 0 ? (lengths ? 0 : -1) : old[(f << shift) + (i & mask)];
     if (lengths) c.length[s] = now;
-    else if (j < c.table_len) c.table[(size_t)s * c.table_len + j] = now;
+    else c.table[(size_t)s * c.table_len + j] = now;
   }
 }
 
@@ -243,17 +276,23 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Pages c, int *plan, i
 {
   __shared__ int sums[kWaves], sums2[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int mine = 0;
-  for (long p = tid; p < c.pages; p += kThreads) mine += c.refs[p] != 0;
-  int used;
+  int mine = 0, count[16], used;
+  for (long base = 0; base < c.pages; base += (long)kWaves * kSpan) {
+    const long first = base + (long)wave * kSpan;
+    load_counts(c, first, count);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) mine += count[k] != 0 && first + k * kWave + lane < c.pages;
+  }
   scan_exclusive<int>(mine, sums, used);
   int sources = 0, places = 0;
   for (long base = 0; base < c.pages; base += (long)kWaves * kSpan) {
     unsigned long long in_use[16];
     int above = 0, below = 0;
+    load_counts(c, base + (long)wave * kSpan, count);
+#pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const long first = base + (long)wave * kSpan + k * kWave, p = first + lane;
-      in_use[k] = __ballot(p < c.pages && c.refs[p < c.pages ? p : 0] != 0);
+      const long p = base + (long)wave * kSpan + k * kWave + lane;
+      in_use[k] = __ballot(p < c.pages && count[k] != 0);
       const unsigned long long high = __ballot(p >= used), low = __ballot(p < used);
       above += __popcll(in_use[k] & high);
       below += __popcll(~in_use[k] & low);
@@ -267,6 +306,7 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Pages c, int *plan, i
       sources += sums[w];
       places += sums2[w];
     }
+#pragma unroll
     for (int k = 0; k < 16; ++k) {
       const long p = base + (long)wave * kSpan + k * kWave + lane;
       const unsigned long long from = in_use[k] & __ballot(p >= used), to = ~in_use[k] & __ballot(p < used);
@@ -358,8 +398,9 @@ hipError_t launch_pages_reserve(const Pages &c, const int *n_new, int *granted, 
 
 hipError_t launch_pages_select(const Pages &c, const int *from, hipStream_t st)
 {
-  const int columns = c.slots <= 960 ? 16 : 65536 / 4 / c.slots - 1;   // 64 KiB of LDS at most; 64 bytes of a row where they fit
-  select_kernel<<<(c.table_len + columns - 1) / columns + 1, 256, (size_t)c.slots * (columns + 1) * sizeof(int), st>>>(c, from, columns);
+  int shift = 4;                                     // 64 bytes of a row where 64 KiB of LDS hold them (of 4096 slots: two entries)
+  while ((size_t)c.slots * ((1 << shift) + 2) * sizeof(int) > 65536) --shift;
+  select_kernel<<<((c.table_len - 1) >> shift) + 2, 256, (size_t)c.slots * ((1 << shift) + 2) * sizeof(int), st>>>(c, from, shift);
   return hipGetLastError();
 }
 
