@@ -540,26 +540,57 @@ inline int wide_splits(long items, long tokens)
 }
 constexpr int wide_floats(int D) { return kWide * (D + 2); }
 
-// Column tile x of the list over all slots: floor(start[s] G / 128) + s leaves every slot as many as it can have.
-struct Columns { int slot, first, count, rows; };    // first column, columns of the slot in all; rows.count
-__device__ inline bool columns_of(const Pages &c, const AttendArgs &a, long x, Columns &t, Rows &rows)
+// Column tile x of the list over all slots, those of up to 16 columns left out (they are the other kernel's).  Up to 64 slots, and where
+// tiles are not split, every wave has all of them in its lanes, one load deep, and their tiles are listed longest slot first: the last
+// workgroups to begin are short ones (32 slots of 537 to 4096 tokens, 8 heads: 201 us, in the order of the slots 247; that many slots of one
+// length lose 3 us by it).  Else slot s has its tiles from floor(start[s] G / 128) + s on, which leaves each as many as it can have.
+struct Columns { int slot, first, count, len; };     // first column, columns of the slot in all; its tokens
+__device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bool sorted, Columns &t, Rows &rows)
 {
-  const int G = c.q_per_kv;
-  auto base = [&](int s) {
-    const int f = a.start[s];
-    return (long)(f < 0 ? 0 : f < a.rows ? f : a.rows) * G / kWide + s;
-  };
-  t.slot = __builtin_amdgcn_readfirstlane(last_slot_at(c.slots, x, base));
-  rows = slot_rows(a.start, t.slot, a.rows);
+  const int G = c.q_per_kv, lane = threadIdx.x & 63;
+  int i;
+  if (sorted) {
+    const int s = min(lane, c.slots - 1);
+    const Rows r = slot_rows(a.start, s, a.rows);
+    const int len = slot_length(c, s), n = lane < c.slots && r.count * G > kCols ? (r.count * G + kWide - 1) / kWide : 0;
+    const int seen = c.window > 0 ? min(len, min(c.window, len) + r.count) : len;
+    const int key = (seen / kTile << 6) + 63 - lane;   // tokens that a tile sees, in tiles; ties as the slots are
+    int before = 0;
+    for (int base = 0; base < c.slots; base += 8)
+#pragma unroll
+      for (int j = base; j < base + 8; ++j)
+        before += __builtin_amdgcn_readlane(n, j) & -(int)(__builtin_amdgcn_readlane(key, j) > key);
+    const unsigned long long found = __ballot((unsigned)(x - before) < (unsigned)n);
+    if (!found) return false;
+    t.slot = __ffsll(found) - 1;
+    rows.first = __builtin_amdgcn_readlane(r.first, t.slot);
+    rows.count = __builtin_amdgcn_readlane(r.count, t.slot);
+    t.len = __builtin_amdgcn_readlane(len, t.slot);
+    i = x - __builtin_amdgcn_readlane(before, t.slot);
+  } else {
+    auto base = [&](int s) {
+      const int f = a.start[s];
+      return (long)(f < 0 ? 0 : f < a.rows ? f : a.rows) * G / kWide + s;
+    };
+    t.slot = __builtin_amdgcn_readfirstlane(last_slot_at(c.slots, x, base));
+    rows = slot_rows(a.start, t.slot, a.rows);
+    t.len = slot_length(c, t.slot);
+    i = (int)(x - base(t.slot));
+  }
   t.count = rows.count * G;
-  const long i = x - base(t.slot), n = (t.count + kWide - 1) / kWide;
-  if (i >= n || t.count <= kCols) return false;      // (up to 16 columns: the other kernel's)
-  t.first = (int)(n - 1 - i) * kWide;                // the longest first
+  const int n = (t.count + kWide - 1) / kWide;
+  if (i >= n || t.count <= kCols) return false;
+  t.slot = __builtin_amdgcn_readfirstlane(t.slot);
+  t.count = __builtin_amdgcn_readfirstlane(t.count);
+  t.len = __builtin_amdgcn_readfirstlane(t.len);
+  rows.first = __builtin_amdgcn_readfirstlane(rows.first);
+  rows.count = __builtin_amdgcn_readfirstlane(rows.count);
+  t.first = __builtin_amdgcn_readfirstlane((n - 1 - i) * kWide);       // the longest first
   return true;
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, long items, int splits)
+__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
   __shared__ __align__(16) u4 keys[2][kTile * D / 8], values[2][kTile * D / 8];
@@ -567,16 +598,16 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int G = c.q_per_kv;
   // each die works through neighbouring items, head by head: what a (slot, head) has cached stays in its L2
-  const long total = items * c.heads * splits;
-  long id = blockIdx.x;
+  const unsigned total = gridDim.x;
+  unsigned id = blockIdx.x;
   if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
-  const int split = (int)(id % splits);
-  const long item = id / splits;
-  const int head = (int)(item / items);
+  const int split = id % (unsigned)splits;
+  const unsigned item = id / (unsigned)splits;
+  const int head = item / items;
   Columns t;
   Rows rows;
-  if (!columns_of(c, a, item % items, t, rows)) return;
-  const int len = slot_length(c, t.slot), before = len - rows.count;
+  if (!columns_of(c, a, item % items, splits == 1 && c.slots <= kWave, t, rows)) return;
+  const int len = t.len, before = len - rows.count;
   const int last_col = min(t.first + kWide, t.count) - 1;
   const int lo = before + t.first / G, hi = before + last_col / G;
   const Span span = span_of(c, lo, hi);
@@ -594,7 +625,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
   const int p = col <= last_col ? before + col / G : -1;
   const int from_token = c.window > 0 ? max(p - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
   const unsigned seen_tokens = (unsigned)(p + 1 - from_token);
-  auto row_sees = [&](int token) { return (unsigned)(token - from_token) < seen_tokens || token < first_tokens; };
+  auto row_sees = [&](int token) { return ((unsigned)(token - from_token) < seen_tokens) | (token < first_tokens); };
   u4 q[KK];
 #pragma unroll
   for (int k = 0; k < KK; ++k) {
@@ -749,7 +780,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
       const bool there = at_of(tile, b) >= 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        x[m][b % 2 * 8 + i] = there && row_sees(t0 + (i & 3) + 8 * (i >> 2)) ? x[m][b % 2 * 8 + i] : -__builtin_inff();
+        x[m][b % 2 * 8 + i] = there & row_sees(t0 + (i & 3) + 8 * (i >> 2)) ? x[m][b % 2 * 8 + i] : -__builtin_inff();
     }
   };
   // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
@@ -883,7 +914,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 
   sum += __shfl_xor(sum, 32, kWave);
   if (splits > 1) {
-    float *share = a.parts + (item * splits + split) * wide_floats(D);
+    float *share = a.parts + (long)id * wide_floats(D);
     const int mine = wave * 32 + n;
     if (from < to)
 #pragma unroll
@@ -912,15 +943,15 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, lon
 // Eight columns of an item to a workgroup, eight shares on their way at a time.
 constexpr int kJoinColumns = 8;
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, long items, int splits)
+__global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, unsigned items, int splits)
 {
   const int G = c.q_per_kv;
-  const long item = blockIdx.x;
-  const int head = (int)(item / items);
+  const unsigned item = blockIdx.x;
+  const int head = item / items;
   Columns t;
   Rows rows;
-  if (!columns_of(c, a, item % items, t, rows)) return;
-  const float *base = a.parts + item * splits * wide_floats(D);
+  if (!columns_of(c, a, item % items, false, t, rows)) return;
+  const float *base = a.parts + (long)item * splits * wide_floats(D);
   for (int i = threadIdx.x; i < kJoinColumns * (D / 2); i += 256) {
     const int at = blockIdx.y * kJoinColumns + i / (D / 2), d = i % (D / 2) * 2, col = t.first + at;
     if (col >= t.count) return;
@@ -965,8 +996,8 @@ hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
   if ((long)a.max_new * c.q_per_kv > kCols) {
     const long items = wide_items(c.slots, c.q_per_kv, a.rows);
     const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
-    wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits), 256, 0, st>>>(c, a, items, splits);
-    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, items, splits);
+    wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits), 256, 0, st>>>(c, a, (unsigned)items, splits);
+    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
   }
   return hipGetLastError();
 }
