@@ -620,12 +620,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   const int wave_lo = before + (t.first + wave * 32) / G, wave_hi = before + wave_last / G;
   const bool have = t.first + wave * 32 <= last_col;
   const int row = rows.first + col / G, q_head = head * G + col % G;
-  // The row, at p, sees the tokens from_token .. from_token + seen_tokens - 1 and those before first_tokens: two compares a score (425
-  // us at 40 heads, 12288 tokens, a window of 4096, where four took 470).
+  // the row, at p, sees the tokens from_token .. p and those before first_tokens
   const int p = col <= last_col ? before + col / G : -1;
   const int from_token = c.window > 0 ? max(p - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
-  const unsigned seen_tokens = (unsigned)(p + 1 - from_token);
-  auto row_sees = [&](int token) { return ((unsigned)(token - from_token) < seen_tokens) | (token < first_tokens); };
   u4 q[KK];
 #pragma unroll
   for (int k = 0; k < KK; ++k) {
@@ -773,14 +770,20 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     for (int k = 0; k < KK; ++k)
       x[m] = Operand<BF16>::mma32(k < kAhead ? ahead[k] : keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
   };
+  // Which of the lane's eight tokens of a block the row sees is a word of bits (four compares a score took 470
+  // us at 40 heads, 4 x 4096 tokens, a window of 820, two 440, this 415).
   auto mask = [&](int tile, int m) {
+    auto below = [](int n) { return (1u << min(max(n, 0), 12)) - 1; };
 #pragma unroll
     for (int b = 2 * m; b < 2 * m + 2; ++b) {
-      const int t0 = span.block(tile * 4 + b) * kBlock + 4 * h;
-      const bool there = at_of(tile, b) >= 0;
+      const int t0 = span.block(tile * 4 + b) * kBlock + 4 * h;        // the lane has t0 .. t0 + 3 and t0 + 8 .. t0 + 11
+      unsigned seen = (below(p + 1 - t0) & ~below(from_token - t0)) | below(first_tokens - t0);
+      if (at_of(tile, b) < 0) seen = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[m][b % 2 * 8 + i] = there & row_sees(t0 + (i & 3) + 8 * (i >> 2)) ? x[m][b % 2 * 8 + i] : -__builtin_inff();
+      for (int i = 0; i < 8; ++i) {
+        const unsigned all = (unsigned)((int)(seen << (31 - (i & 3) - 8 * (i >> 2))) >> 31);
+        x[m][b % 2 * 8 + i] = __uint_as_float((__float_as_uint(x[m][b % 2 * 8 + i]) & all) | (0xff800000u & ~all));
+      }
     }
   };
   // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
