@@ -925,7 +925,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *reinterpret_cast<f4 *>(share + mine * D + o * 32 + i * 8 + h * 4) = f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]};
-    if (h == 0) { share[kWide * D + mine] = top; share[kWide * (D + 1) + mine] = sum; }
+    if (h == 0) { share[kWide * D + mine] = from < to ? top : -__builtin_inff(); share[kWide * (D + 1) + mine] = sum; }
     return;
   }
   if (col > last_col) return;
@@ -965,7 +965,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float *f = base + (long)min(k + j, splits - 1) * wide_floats(D);
-        m[j] = k + j < splits ? f[kWide * D + at] : kLowest;
+        m[j] = k + j < splits ? f[kWide * D + at] : -__builtin_inff();
         u[j] = f[kWide * (D + 1) + at];
         v[j] = *reinterpret_cast<const float2 *>(f + at * D + d);
       }
@@ -977,7 +977,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
       l *= less; x *= less; y *= less;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (m[j] == kLowest) continue;               // nothing seen there, nothing written
+        if (m[j] == -__builtin_inff()) continue;     // no tiles, nothing written
         const float e = exp2_fast(m[j] - top);
         l = fmaf(u[j], e, l);
         x = fmaf(v[j].x, e, x);
