@@ -133,8 +133,9 @@ int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const vo
   const int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * desc->head_dim);
-  if (!k || !v || !start || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4) || step < 0 || rows < 0) return LESSDEC_EINVAL;
+  if (step < 0 || rows < 0) return LESSDEC_EINVAL;
   if (rows == 0) return LESSDEC_OK;
+  if (!k || !v || !start || !aligned(k, 16) || !aligned(v, 16) || !aligned(start, 4)) return LESSDEC_EINVAL;
   return result(launch_pages_append(c, desc->dtype, AppendArgs{k, v, step, start, rows}, (hipStream_t)hip_stream));
 }
 
@@ -145,11 +146,11 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
   int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
-  if (!q || !out || !start || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4)) return LESSDEC_EINVAL;
   if (step < 0 || rows < 0 || max_new < 0 || (long)rows * c.q_per_kv >= 1L << 31 || ((long)rows * c.q_per_kv / 128 + desc->slots) * desc->heads > 1L << 30) return LESSDEC_EINVAL;
   rc = check(desc, kWork, rows, layer, &c);
   if (rc) return rc;
   if (rows == 0 || max_new == 0) return LESSDEC_OK;
+  if (!q || !out || !start || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4)) return LESSDEC_EINVAL;
   AttendArgs a{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<int *>(desc->workspace),
                static_cast<float *>(scratch(desc))};
   return result(launch_pages_attend(c, desc->dtype, a, (hipStream_t)hip_stream));
@@ -161,9 +162,9 @@ int lessdec_pages_read(const lessdec_pages_desc *desc, int32_t layer, const int3
   Pages c;
   const int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
-  if (!slots || !K || !V || !aligned(slots, 4) || !aligned(K, 16) || !aligned(V, 16)) return LESSDEC_EINVAL;
   if (n < 0 || n > 65535 || count < 0) return LESSDEC_EINVAL;
   if (n == 0 || count == 0) return LESSDEC_OK;
+  if (!slots || !K || !V || !aligned(slots, 4) || !aligned(K, 16) || !aligned(V, 16)) return LESSDEC_EINVAL;
   return result(launch_pages_read(c, desc->dtype, ReadArgs{slots, n, first, count, K, V}, (hipStream_t)hip_stream));
 }
 

@@ -108,18 +108,19 @@ class PagedCache:
         self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)   # (zeros: lessdec.h)
         d.workspace, d.workspace_bytes = self.workspace.data_ptr(), need
         self.desc = d
+        self._pointer, self._lib, self._current = C.pointer(d), lib(), (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
         if buffers is None:
             self.reset()
 
     def _call(self, name, stream, *args):
-        torch, index = self.torch, self.device.index
-        s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-        f = getattr(lib(), name)
-        if torch.cuda.current_device() == index:
-            rc = f(self.desc, *args, s)
+        index, (raw_stream, device) = self.device.index, self._current
+        s = raw_stream(index) if stream is None else stream.cuda_stream
+        f = getattr(self._lib, name)
+        if device() == index:
+            rc = f(self._pointer, *args, s)
         else:
-            with torch.cuda.device(index):
-                rc = f(self.desc, *args, s)
+            with self.torch.cuda.device(index):
+                rc = f(self._pointer, *args, s)
         if rc:
             _check(rc, name)
 
@@ -130,12 +131,13 @@ class PagedCache:
 
     def _rows(self, t, heads, what):
         """(rows, elements from a row to the next) of a [rows, heads, D] tensor whose rows may lie apart."""
-        if t.dim() != 3 or t.dtype != self.tdtype or t.device != self.device or t.shape[1:] != (heads, self.D):
-            raise LessdecError(f"{what} must be [rows, {heads}, {self.D}] {self.tdtype} on {self.device}")
-        a, b, c = t.stride()
-        if t.shape[0] and (c != 1 or (b != self.D and heads > 1) or (t.shape[0] > 1 and (a < heads * self.D or a % 8)) or t.data_ptr() % 16):
+        shape, d = t.shape, self.D
+        if len(shape) != 3 or shape[1] != heads or shape[2] != d or t.dtype != self.tdtype or t.device != self.device:
+            raise LessdecError(f"{what} must be [rows, {heads}, {d}] {self.tdtype} on {self.device}")
+        rows, (a, b, c) = shape[0], t.stride()
+        if rows and (c != 1 or (b != d and heads > 1) or (rows > 1 and (a < heads * d or a % 8)) or t.data_ptr() % 16):
             raise LessdecError(f"{what}: heads of a row must be packed, rows 16-byte aligned and not overlap")
-        return t.shape[0], a if t.shape[0] > 1 else 0
+        return rows, a if rows > 1 else 0
 
     def reset(self, stream=None):
         """Every slot empty, every page free."""

@@ -203,3 +203,19 @@ def test_caches_beside_one_another():
         torch.cuda.synchronize()
         for want, outs in zip(alone, beside):
             assert all(torch.equal(want, out) for out in outs)
+
+
+def test_no_rows():
+    p = Pair(2, 8, 16, 4, 2, 64, q_per_kv=2)
+    fill(p, [5, 0])
+    none = p.t.empty(0, 2, 64, dtype=p.own.tdtype, device="cuda")
+    start = p.ints([0, 0, 0])
+    p.own.append(0, none, none, start)
+    p.own.attend(0, none.expand(0, 2, 64).repeat(1, 2, 1), p.t.empty(0, 4, 64, dtype=p.own.tdtype, device="cuda"), start, 0)
+    K = p.t.empty(0, 2, 3, 64, dtype=p.own.tdtype, device="cuda")
+    p.own.read(0, p.ints([]), 0, K, K.clone())
+    K = p.t.empty(1, 2, 0, 64, dtype=p.own.tdtype, device="cuda")
+    p.own.read(0, p.ints([0]), 0, K, K.clone())
+    p.reserve([0, 0])
+    p.own.copy(p.plan, 0)
+    p.held()

@@ -127,3 +127,15 @@ def test_the_oracles_bookkeeping():
     assert c.refs.tolist() == [1, 0, 0, 1, 0, 0, 0, 0] and c.compact() == [(3, 1)] and c.table[1].tolist() == [0, 1, -1, -1]
     assert c.reserve([16 * 5, 1, 0, 0])[0].tolist() == [0, 1, 0, 0]     # five pages: more than a table row holds
     assert c.reserve([16 * 4, 16, 64, 1])[0].tolist() == [64, 16, 0, 0] # two pages are left: the third gets none, nor does the last
+
+
+def test_nothing_to_do_needs_no_pointers():
+    """An empty tensor has no address."""
+    L, p = binding.lib(), C.byref(desc())
+    assert L.lessdec_pages_append(p, 0, None, None, 0, None, 0, None) == binding.OK
+    assert L.lessdec_pages_attend(p, 0, None, 0, None, None, None, 0, 1, None) == binding.OK
+    assert L.lessdec_pages_read(p, 0, None, 0, 0, 5, None, None, None) == L.lessdec_pages_read(p, 0, A, 1, 0, 0, None, None, None) == binding.OK
+    for layer, stride, rows in ((2, 0, 0), (0, 12, 0), (0, 0, -1)):
+        assert L.lessdec_pages_append(p, layer, None, None, stride, None, rows, None) == binding.EINVAL
+        assert L.lessdec_pages_attend(p, layer, None, stride, None, None, None, rows, 1, None) == binding.EINVAL
+    assert L.lessdec_pages_attend(p, 0, A, 0, B, None, B, 1 << 29, 1, None) == binding.EINVAL           # 2^31 query columns
