@@ -136,6 +136,10 @@ __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__
 // workgroup has of a (slot, head) that it shares with others goes to memory, past the L2 of its die, and the last of them to arrive joins
 // the shares in the order of the tokens: 32 neighbours first, then the joined ones, so that one sequence can be spread over the chip.
 
+// Measured: 64 slots of up to 8192 tokens, 8 heads, 4 query heads each: 107 us, 5.7 TB/s; one of 131072, 8 heads, 5 query heads each: 52 us,
+// 5.2 TB/s; one of 1025, 32 heads: 10.5 us, the latency of its chain of loads (start and length, table, codes, shares).
+// 16 columns is one matrix tile, and where the kernels meet: 64 slots of 8192, 8 heads, 16 columns 206 us here, 249 in the other.
+
 constexpr int kCols = 16, kStepBlocks = 8;
 constexpr int kGroup = 32;
 // Three workgroups to a compute unit; where that would make more than 32 shares of a (slot, head) down to one, which reads as
@@ -528,8 +532,17 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 // barrier a tile.  Where there are too few workgroups for the chip, several share a (slot, head, 128 columns), each some
 // of its tiles, and a second launch joins them.
 
+//
+// Measured: 32 heads of a prompt of 8192 tokens 566 us (970 TFLOP/s of the visible pairs; a large library product reaches 1184), the
+// matrix cores busy for 46 % of the cycles and the vector units about as long (6 of their instructions a product: widening, exponentials,
+// sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 405 us (600), 9 of their instructions a product.
+// Two workgroups are what the registers hold of a compute unit; eight waves of 16 columns to a workgroup took 605 us in place of 591,
+// four of 64 columns spilled.
+
 constexpr int kWide = 128, kTile = 64;               // columns and tokens
-constexpr int kEnough = 512;                         // workgroups: two to a compute unit
+// Workgroups that are enough not to split: two to a compute unit.  128 rows over 8192 tokens, 32 heads: 54 us (67 with 256, 46 with
+// 1024, 191 unsplit); 1024 rows: 182 us (247, 195, 246); 64 slots of 71 columns over 8192 tokens: 51 us (67, 49, 137).
+constexpr int kEnough = 512;
 
 __host__ __device__ inline long wide_items(int slots, int q_per_kv, long rows) { return rows * q_per_kv / kWide + slots; }
 inline int wide_splits(long items, long tokens)
@@ -541,9 +554,10 @@ inline int wide_splits(long items, long tokens)
 constexpr int wide_floats(int D) { return kWide * (D + 2); }
 
 // Column tile x of the list over all slots, those of up to 16 columns left out (they are the other kernel's).  Up to 64 slots, and where
-// tiles are not split, every wave has all of them in its lanes, one load deep, and their tiles are listed longest slot first: the last
-// workgroups to begin are short ones (32 slots of 537 to 4096 tokens, 8 heads: 201 us, in the order of the slots 247; that many slots of one
-// length lose 3 us by it).  Else slot s has its tiles from floor(start[s] G / 128) + s on, which leaves each as many as it can have.
+// tiles are not split, every wave has all of them in its lanes, one load deep, and the list has their tiles alone, longest slot first:
+// the last workgroups to begin are short ones, and every die has as many.  Else slot s has its tiles from floor(start[s] G / 128) + s on,
+// which leaves each as many as it can have.  32 slots of 537 to 4096 tokens, 8 heads: 201 us, as the slots are 247; 64 slots of 2048: 204 and
+// 233; 4 slots of 4096: 830 and 816.  Split tiles have a second launch that would do all of this again: 64 slots, 24 us as they are, 30 in order.
 struct Columns { int slot, first, count, len; };     // first column, columns of the slot in all; its tokens
 __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bool sorted, Columns &t, Rows &rows)
 {

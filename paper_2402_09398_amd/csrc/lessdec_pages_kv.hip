@@ -2,7 +2,10 @@
 //
 // Both are bound by memory: a token of a head is 2 D elements of two bytes on one side and 2 D bytes on the other.  A wave has one
 // block of 16 tokens of one head, keys and values, so that the block's exponents are the wave's own reduction, nothing is
-// shared and no wave waits for another.
+// shared and no wave waits for another.  Eight lanes have a line of 128 bytes of a token's row, so that rows are read and written by whole
+// lines, past the caches; the values are turned into the cache's order in the LDS.  32 heads, D = 128, bf16: 15581 tokens of 16 prompts in,
+// 383 MB, 78 us (4.9 TB/s); 16 times 2049 out, 806 MB, 128 us (6.3 TB/s).  Four lanes to a line took 253 us for both, not 209, and
+// non-temporal access by less than a line 447.  A token a slot is a chain of latencies: 5.3 us in, 4.0 out.
 #include "lessdec_pages.h"
 
 namespace lessdec {
