@@ -767,22 +767,23 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
       units[b] = read_lane(unit, i + b);
     }
   };
-  // The first operands of a product are read from the LDS ahead of what comes before it, so that it does not begin with a wait.
-  constexpr int kAhead = 4;
-  u4 ahead[kAhead];
+  // The operands of a product are read from the LDS ahead of what comes before it, so that it does not wait (8192 tokens, 32 heads, a call
+  // at a time: 624 us; with the first half of them ahead 631.  Each read as soon as the product before has used its registers: 628, and 657
+  // with the barrier before a tile's last product, which then meets no wait for the LDS at all).
+  static_assert(KK == 2 * OB, "as many operands of keys as of values");
+  u4 ahead[KK];
   auto keys_ahead = [&](int buf, int m) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) ahead[k] = keys[buf][(m * KK + k) * 64 + lane];
+    for (int k = 0; k < KK; ++k) ahead[k] = keys[buf][(m * KK + k) * 64 + lane];
   };
   auto values_ahead = [&](int buf, int m) {
 #pragma unroll
-    for (int o = 0; o < kAhead; ++o) ahead[o] = values[buf][(2 * m * OB + o) * 64 + lane];
+    for (int o = 0; o < KK; ++o) ahead[o] = values[buf][(m * KK + o) * 64 + lane];
   };
-  auto scores = [&](int buf, int m) {
+  auto scores = [&](int m) {
     x[m] = f16v{0};
 #pragma unroll
-    for (int k = 0; k < KK; ++k)
-      x[m] = Operand<BF16>::mma32(k < kAhead ? ahead[k] : keys[buf][(m * KK + k) * 64 + lane], q[k], x[m]);
+    for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(ahead[k], q[k], x[m]);
   };
   // Which of the lane's eight tokens of a block the row sees is a word of bits (four compares a score took 470
   // us at 40 heads, 4 x 4096 tokens, a window of 820, two 440, this 415).
@@ -838,12 +839,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
 #pragma unroll
     for (int b = 0; b < 2; ++b) sum = fmaf(part[b], units[2 * m + b], sum);
   };
-  auto gather = [&](int buf, int m, const u4 (&w)[2]) {
+  auto gather = [&](const u4 (&w)[2]) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int o = 0; o < OB; ++o)
-        acc[o] = Operand<false>::mma32(b * OB + o < kAhead ? ahead[b * OB + o] : values[buf][((2 * m + b) * OB + o) * 64 + lane], w[b], acc[o]);
+    for (int o = 0; o < KK; ++o) acc[o % OB] = Operand<false>::mma32(ahead[o], w[o / OB], acc[o % OB]);
   };
 #pragma unroll
   for (int k = 0; k < KK; ++k) asm volatile("" : "+v"(q[k]));          // the queries are waited for here, not (with all codes requested since) in the loop
@@ -852,7 +850,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     enter(from);
     if (active) {
       keys_ahead(from & 1, 0);
-      scores(from & 1, 0);
+      scores(0);
       if (!whole) mask(from, 0);
     }
   }
@@ -868,17 +866,17 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     if (active) {
       // products before the other workgroup's staging: 661 -> 621 us at 32 heads x 8192 tokens, clocks settled
       __builtin_amdgcn_s_setprio(1);
-      scores(buf, 1);
+      scores(1);
       weigh(0);
       values_ahead(buf, 0);
       settle(0);
       if (!whole) mask(tile, 1);
       const u4 first[2] = {weights[0], weights[1]};
-      gather(buf, 0, first);
+      gather(first);
       weigh(1);
       values_ahead(buf, 1);
       settle(1);
-      gather(buf, 1, weights);
+      gather(weights);
     }
     if (tile + 1 == to) break;
     if (tile + 1 - chunk == kChunk) {
@@ -890,7 +888,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     __syncthreads();
     if (active) {
       keys_ahead(buf ^ 1, 0);
-      scores(buf ^ 1, 0);
+      scores(0);
       if (!whole) mask(tile + 1, 0);
     }
   }
