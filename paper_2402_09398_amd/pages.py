@@ -6,15 +6,9 @@ from __future__ import annotations
 
 import ctypes as C
 
-from .binding import DTYPE_BF16, DTYPE_F16, LessdecError, PagesDesc, _check, _p, lib
+from .binding import DTYPE_BF16, DTYPE_F16, LessdecError, PagesDesc, _check, _p, _stream, lib
 
 BLOCK = 16
-
-
-def _stream(desc, stream):
-    import torch
-    s = torch.cuda.current_stream(getattr(desc, "device", None)) if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
 
 
 def lessdec_pages_workspace_bytes(desc: PagesDesc, max_rows: int) -> int:
@@ -22,37 +16,37 @@ def lessdec_pages_workspace_bytes(desc: PagesDesc, max_rows: int) -> int:
 
 
 def lessdec_pages_reset(desc: PagesDesc, stream=None):
-    _check(lib().lessdec_pages_reset(C.byref(desc), _stream(desc, stream)), "lessdec_pages_reset")
+    _check(lib().lessdec_pages_reset(C.byref(desc), _stream(stream)), "lessdec_pages_reset")
 
 
 def lessdec_pages_reserve(desc: PagesDesc, n_new, granted, plan, stream=None):
-    _check(lib().lessdec_pages_reserve(C.byref(desc), _p(n_new), _p(granted), _p(plan), _stream(desc, stream)), "lessdec_pages_reserve")
+    _check(lib().lessdec_pages_reserve(C.byref(desc), _p(n_new), _p(granted), _p(plan), _stream(stream)), "lessdec_pages_reserve")
 
 
 def lessdec_pages_select(desc: PagesDesc, source, stream=None):
-    _check(lib().lessdec_pages_select(C.byref(desc), _p(source), _stream(desc, stream)), "lessdec_pages_select")
+    _check(lib().lessdec_pages_select(C.byref(desc), _p(source), _stream(stream)), "lessdec_pages_select")
 
 
 def lessdec_pages_compact(desc: PagesDesc, plan, stream=None):
-    _check(lib().lessdec_pages_compact(C.byref(desc), _p(plan), _stream(desc, stream)), "lessdec_pages_compact")
+    _check(lib().lessdec_pages_compact(C.byref(desc), _p(plan), _stream(stream)), "lessdec_pages_compact")
 
 
 def lessdec_pages_copy(desc: PagesDesc, plan, max_pairs: int, stream=None):
-    _check(lib().lessdec_pages_copy(C.byref(desc), _p(plan), int(max_pairs), _stream(desc, stream)), "lessdec_pages_copy")
+    _check(lib().lessdec_pages_copy(C.byref(desc), _p(plan), int(max_pairs), _stream(stream)), "lessdec_pages_copy")
 
 
 def lessdec_pages_append(desc: PagesDesc, layer: int, k, v, row_stride: int, start, rows: int, stream=None):
-    _check(lib().lessdec_pages_append(C.byref(desc), layer, _p(k), _p(v), row_stride, _p(start), rows, _stream(desc, stream)),
+    _check(lib().lessdec_pages_append(C.byref(desc), layer, _p(k), _p(v), row_stride, _p(start), rows, _stream(stream)),
            "lessdec_pages_append")
 
 
 def lessdec_pages_attend(desc: PagesDesc, layer: int, q, q_stride: int, out, lse, start, rows: int, max_new: int, stream=None):
-    _check(lib().lessdec_pages_attend(C.byref(desc), layer, _p(q), q_stride, _p(out), _p(lse), _p(start), rows, max_new, _stream(desc, stream)),
+    _check(lib().lessdec_pages_attend(C.byref(desc), layer, _p(q), q_stride, _p(out), _p(lse), _p(start), rows, max_new, _stream(stream)),
            "lessdec_pages_attend")
 
 
 def lessdec_pages_read(desc: PagesDesc, layer: int, slots, n: int, first: int, count: int, K, V, stream=None):
-    _check(lib().lessdec_pages_read(C.byref(desc), layer, _p(slots), n, first, count, _p(K), _p(V), _stream(desc, stream)),
+    _check(lib().lessdec_pages_read(C.byref(desc), layer, _p(slots), n, first, count, _p(K), _p(V), _stream(stream)),
            "lessdec_pages_read")
 
 

@@ -219,3 +219,84 @@ def test_no_rows():
     p.reserve([0, 0])
     p.own.copy(p.plan, 0)
     p.held()
+
+
+@pytest.mark.parametrize("group,dim,rows", [(17, 64, [1, 0, 2]), (128, 128, [1, 2, 0]), (3, 64, [5, 6, 1])])
+def test_groups_at_the_edges_of_a_tile(group, dim, rows):
+    """Columns just past one matrix tile, exactly one workgroup's, 15 and 18."""
+    p = Pair(3, 40, 16, 12, 2, dim, "f16", q_per_kv=group)
+    fill(p, [150, 40, 7])
+    p.attend(rows)
+
+
+@pytest.mark.parametrize("scale", [0.3, 2.0 ** -40, 3.0])
+def test_scales(scale):
+    p = Pair(2, 30, 32, 8, 1, 64, "bf16", q_per_kv=2, scale=scale)
+    fill(p, [200, 50])
+    for rows in ([1, 1], [40, 50]):
+        p.attend(rows)
+
+
+def test_the_functions_of_the_library_by_name():
+    """The front end without PagedCache: its own descriptor, one call of each."""
+    from paper_2402_09398_amd import pages as lib
+    p = Pair(2, 12, 16, 4, 1, 64, "f16")
+    d, t = p.own.desc, p.t
+    assert lib.lessdec_pages_workspace_bytes(d, 4096) == d.workspace_bytes
+    lib.lessdec_pages_reset(d)
+    granted = p.ints([-1, -1])
+    lib.lessdec_pages_reserve(d, p.ints([20, 3]), granted, p.plan)
+    lib.lessdec_pages_copy(d, p.plan, 2)
+    p.ref.reserve([20, 3])
+    p.state()
+    start = np.array([0, 20, 23])
+    x = t.tensor(p.rng.standard_normal((3, 23, 1, 64))).half().cuda()
+    lib.lessdec_pages_append(d, 0, x[0], x[1], 0, p.ints(start), 23)
+    p.ref.append(0, x[0].double().cpu().numpy(), x[1].double().cpu().numpy(), start)
+    p.held()
+    out, lse = t.empty_like(x[2]), t.empty(23, 1, device="cuda")
+    lib.lessdec_pages_attend(d, 0, x[2], 0, out, lse, p.ints(start), 23, 20)
+    want, want_lse, tol, lse_tol = p.ref.attend(0, x[2].double().cpu().numpy(), start, HALF_STEP["f16"])
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all() and (np.abs(lse.double().cpu().numpy() - want_lse) <= lse_tol).all()
+    lib.lessdec_pages_select(d, p.ints([-1, 0]))
+    p.ref.select([-1, 0])
+    lib.lessdec_pages_compact(d, p.plan)
+    lib.lessdec_pages_copy(d, p.plan, 6)
+    p.ref.copy(p.ref.compact())
+    p.state()
+    K, V = (t.empty(1, 1, 20, 64, dtype=t.float16, device="cuda") for _ in range(2))
+    lib.lessdec_pages_read(d, 0, p.ints([1]), 1, 0, 20, K, V)
+    assert np.array_equal(V.double().cpu().numpy(), p.ref.read(0, [1], 0, 20, 65504.0)[1])
+
+
+def test_refusals():
+    import torch
+    from paper_2402_09398_amd import LessdecError, PagedCache
+    c = PagedCache(2, 8, 16, 4, 2, 64, "f16", q_per_kv=2, max_rows=8)
+    start, k, q = (torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, 64, dtype=torch.float16, device="cuda"),
+                   torch.zeros(4, 4, 64, dtype=torch.float16, device="cuda"))
+    ints = torch.zeros(64, dtype=torch.int32, device="cuda")
+    wide = torch.zeros(4, 2, 128, dtype=torch.float16, device="cuda")
+    bad = [
+        lambda: PagedCache(2, 8, 16, 4, 2, 64, "f32"), lambda: PagedCache(2, 8, 20, 4, 2, 64, "f16"), lambda: PagedCache(2, 8, 16, 4, 2, 96, "f16"),
+        lambda: PagedCache(2, 8, 16, 4, 2, 64, "f16", buffers={n: getattr(c, n)[:1] for n in c.STATE}),
+        lambda: c.append(0, k.float(), k, start), lambda: c.append(0, k, k.cpu(), start), lambda: c.append(0, k, k[:3], start),
+        lambda: c.append(1, k, k, start), lambda: c.append(-1, k, k, start), lambda: c.append(0, wide, wide, start),
+        lambda: c.append(0, wide[..., ::2], wide[..., ::2], start), lambda: c.append(0, k.transpose(0, 1), k.transpose(0, 1), start),
+        lambda: c.append(0, k[:1].expand(4, 2, 64), k[:1].expand(4, 2, 64), start),
+        lambda: c.append(0, k.view(-1)[4:260].view(2, 2, 64), k[:2], start), lambda: c.append(0, k, k, start[:2]),
+        lambda: c.append(0, k, k, start.long()), lambda: c.append(0, k, k, start.cpu()),
+        lambda: c.attend(0, k, k, start, 1), lambda: c.attend(0, q, q[:3], start, 1), lambda: c.attend(0, q, q.bfloat16(), start, 1),
+        lambda: c.attend(0, q, torch.zeros(4, 8, 64, dtype=torch.float16, device="cuda")[:, ::2], start, 1),
+        lambda: c.attend(0, q, torch.empty_like(q), start, 1, lse=torch.zeros(4, 2, device="cuda")), lambda: c.attend(0, q, torch.empty_like(q), start, -1),
+        lambda: c.attend(0, q.repeat(3, 1, 1), q.repeat(3, 1, 1), start, 1),
+        lambda: c.reserve(ints[:1], None, ints), lambda: c.reserve(ints[:2], None, ints[:4]), lambda: c.reserve(ints, ints, ints),
+        lambda: c.select(ints[:1]), lambda: c.select(c.length), lambda: c.compact(ints[:8]), lambda: c.copy(ints[:4], 2), lambda: c.copy(ints, -1),
+        lambda: c.read(0, ints[:1], 0, torch.zeros(1, 2, 4, 64, device="cuda"), torch.zeros(1, 2, 4, 64, device="cuda")),
+        lambda: c.read(0, ints[:1], 0, torch.zeros(2, 2, 4, 64, dtype=torch.float16, device="cuda"), torch.zeros(2, 2, 4, 64, dtype=torch.float16, device="cuda")),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(LessdecError):
+            call()
+            pytest.fail(f"call {i} was let through")
+    torch.cuda.synchronize()
