@@ -215,6 +215,7 @@ __device__ inline Part part_of(const Pages &c, const AttendArgs &a, int w, int w
 
 // A share: [columns][D] sums, maxima, totals.  Stored and loaded past the caches that other dies do not see.
 constexpr int part_floats(int D) { return kCols * (D + 2); }
+__host__ __device__ constexpr long few_floats(int G, int D) { return G <= kCols ? (long)kPagesWorkers * 2 * part_floats(D) : 0; }
 __device__ inline void put(float *p, float x, float y)
 {
   const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
@@ -283,15 +284,18 @@ __device__ inline void join(int n, int cols, Share share, Done done)
   }
 }
 
+template <int D> struct FewShared {
+  float sums[4][kCols][D + 4], tops[4][kCols], totals[4][kCols];
+};
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
+__device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, int worker, int workers, FewShared<D> &shared)
 {
-  constexpr int H = D / 64, T = D / 16, kRow = D + 4;
-  __shared__ float sums[4][kCols][kRow];
-  __shared__ float tops[4][kCols], totals[4][kCols];
+  constexpr int H = D / 64, T = D / 16;
+  auto &sums = shared.sums;
+  auto &tops = shared.tops, &totals = shared.totals;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int G = c.q_per_kv;
-  const Part part = part_of(c, a, blockIdx.x, gridDim.x);
+  const Part part = part_of(c, a, worker, workers);
   if (part.begin >= part.end) return;
   int s = part.slot;
   long in_slot = part.in_slot;
@@ -472,7 +476,7 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
     const bool whole = from == 0 && to == steps;
     // this share is number i of the (slot, head), which begins in worker w0; share 0 lies in that worker's second place, the others in the first
     const long first = pos - from;
-    const int w0 = (int)(first / part.per), shares = (int)((first + steps - 1) / part.per) - w0 + 1, i = (int)blockIdx.x - w0;
+    const int w0 = (int)(first / part.per), shares = (int)((first + steps - 1) / part.per) - w0 + 1, i = worker - w0;
     auto share = [&](int k) { return a.parts + ((long)(w0 + k) * 2 + (k == 0)) * part_floats(D); };
     auto store = [&](float *to_share) {
       return [=](int col, int d, float x, float y, float m, float l) {
@@ -524,6 +528,13 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
   }
 }
 
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
+{
+  __shared__ FewShared<D> shared;
+  few_rows<BF16, D>(c, a, blockIdx.x, gridDim.x, shared);
+}
+
 // ---- many rows a slot ---------------------------------------------------------------------------------------------------
 //
 // Bound by the matrix and vector instructions.  A workgroup has 128 query columns of a (slot, head), 32 to a wave, and goes through the
@@ -543,6 +554,10 @@ constexpr int kWide = 128, kTile = 64;               // columns and tokens
 // Workgroups that are enough not to split: two to a compute unit.  128 rows over 8192 tokens, 32 heads: 54 us (67 with 256, 46 with
 // 1024, 191 unsplit); 1024 rows: 182 us (247, 195, 246); 64 slots of 71 columns over 8192 tokens: 51 us (67, 49, 137).
 constexpr int kEnough = 512;
+// Slots of few rows in such a call: their steps are dealt out to this many workgroups behind the others of the launch, where they read memory
+// while the last tiles are multiplied.  32 slots, half of them prompts: 197 us (256 or 768 of them 195 and 196), 211 in front of the
+// others, 215 as a launch of their own, whose 4 us a call without such slots would pay as well.
+constexpr int kFewBeside = 512;
 
 __host__ __device__ inline long wide_items(int slots, int q_per_kv, long rows) { return rows * q_per_kv / kWide + slots; }
 inline int wide_splits(long items, long tokens)
@@ -607,12 +622,18 @@ template <bool BF16, int D>
 __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
-  __shared__ __align__(16) u4 keys[2][kTile * D / 8], values[2][kTile * D / 8];
+  __shared__ __align__(16) u4 tiles_of[4][kTile * D / 8];
   __shared__ int spoiled;
+  const unsigned total = items * c.heads * splits;
+  if (blockIdx.x >= total) {
+    static_assert(sizeof(FewShared<D>) <= sizeof tiles_of, "the slots of few rows work in the same LDS");
+    few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(tiles_of));
+    return;
+  }
+  auto keys = tiles_of, values = tiles_of + 2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int G = c.q_per_kv;
   // each die works through neighbouring items, head by head: what a (slot, head) has cached stays in its L2
-  const unsigned total = gridDim.x;
   unsigned id = blockIdx.x;
   if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
   const int split = id % (unsigned)splits;
@@ -929,7 +950,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
 
   sum += __shfl_xor(sum, 32, kWave);
   if (splits > 1) {
-    float *share = a.parts + (long)id * wide_floats(D);
+    float *share = a.parts + few_floats(G, D) + (long)id * wide_floats(D);
     const int mine = wave * 32 + n;
     if (from < to)
 #pragma unroll
@@ -966,7 +987,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
   Columns t;
   Rows rows;
   if (!columns_of(c, a, item % items, false, t, rows)) return;
-  const float *base = a.parts + (long)item * splits * wide_floats(D);
+  const float *base = a.parts + few_floats(G, D) + (long)item * splits * wide_floats(D);
   for (int i = threadIdx.x; i < kJoinColumns * (D / 2); i += 256) {
     const int at = blockIdx.y * kJoinColumns + i / (D / 2), d = i % (D / 2) * 2, col = t.first + at;
     if (col >= t.count) return;
@@ -1007,13 +1028,16 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
 template <bool BF16, int D>
 hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
 {
-  if (c.q_per_kv <= kCols) few_kernel<BF16, D><<<few_workers((long)c.slots * c.heads), 256, 0, st>>>(c, a);
-  if ((long)a.max_new * c.q_per_kv > kCols) {
-    const long items = wide_items(c.slots, c.q_per_kv, a.rows);
-    const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
-    wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits), 256, 0, st>>>(c, a, (unsigned)items, splits);
-    if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
+  const long pairs = (long)c.slots * c.heads;
+  if ((long)a.max_new * c.q_per_kv <= kCols) {
+    few_kernel<BF16, D><<<few_workers(pairs), 256, 0, st>>>(c, a);
+    return hipGetLastError();
   }
+  const long items = wide_items(c.slots, c.q_per_kv, a.rows);
+  const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
+  const int few = c.q_per_kv <= kCols ? min(few_workers(pairs), kFewBeside) : 0;
+  wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits + few), 256, 0, st>>>(c, a, (unsigned)items, splits);
+  if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
   return hipGetLastError();
 }
 
@@ -1021,15 +1045,14 @@ hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
 
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows)
 {
-  size_t n = q_per_kv <= kCols ? (size_t)kPagesWorkers * 2 * part_floats(head_dim) : 0;
+  size_t n = (size_t)few_floats(q_per_kv, head_dim);
   if ((long)rows * q_per_kv > kCols) {
     long items = wide_items(slots, q_per_kv, rows) * heads, fewest = wide_items(slots, q_per_kv, 0) * heads;
     if (fewest < kEnough) {
       // splits items: less than kEnough + items workgroups, for any number of rows up to this one
       const long most = wide_splits(fewest, tokens), now = items < kEnough ? items : kEnough - 1;
       long parts = now * most < kEnough + now ? now * most : kEnough + now;
-      const size_t wide = (size_t)parts * wide_floats(head_dim);
-      n = n > wide ? n : wide;
+      n += (size_t)parts * wide_floats(head_dim);
     }
   }
   return n;
