@@ -4,7 +4,7 @@
 // but the copy touches a few bytes a slot or page and is bound by the latency of its dependent loads.  What has an order
 // (which free page goes to which slot) is settled by prefix sums over slots and pages in one workgroup, never by the order in
 // which atomics arrive: the same state gives the same pages every time.  Counts change by integer atomics, which commute.
-// Measured: 64 beams of 2050 tokens on pages of 16: select 4.1 us, reserve 8.9, their 64 copies in four layers 3.8; compacting a pool of 5000 pages:
+// Measured: 64 beams of 2050 tokens on pages of 16: select 4.1 us, reserve 8.4, their 64 copies in four layers 3.8; compacting a pool of 5000 pages:
 // 11.6 us to find what moves, 4.5 to rename it, 56 for the copies (305 MB, 5.5 TB/s).
 #include "lessdec_pages.h"
 
@@ -22,11 +22,11 @@ __device__ inline int count_of(const int *refs, int p)
 }
 
 // The counts of the wave's next kSpan pages from `first` on, sixteen a lane.  Every load is made (of the last page behind the end): sixteen
-// conditional ones wait for one another (a pool of 17000 pages: the search took 8 us, now 2.5).
-__device__ inline void load_counts(const Pages &c, long first, int (&count)[16])
+// conditional ones wait for one another (a pool of 17000 pages: the search took 8 us, now 2.2).
+__device__ inline void load_counts(const Pages &c, int first, int (&count)[16])
 {
 #pragma unroll
-  for (int k = 0; k < 16; ++k) count[k] = count_of(c.refs, (int)min(first + k * kWave + (long)(threadIdx.x & 63), (long)c.pages - 1));
+  for (int k = 0; k < 16; ++k) count[k] = count_of(c.refs, min(first + k * kWave + (int)(threadIdx.x & 63), c.pages - 1));
 }
 
 // sum over the threads before this one; total: over all of them
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
     __syncthreads();
   }
   int counts[16];                                    // of the pages looked at first: on their way meanwhile
-  load_counts(c, (long)wave * kSpan, counts);
+  load_counts(c, wave * kSpan, counts);
 
   // what each slot needs; a thread has the slots tid, tid + kThreads, ..
   int wanted[kTurns], length[kTurns], old_page[kTurns], pair[kTurns];
@@ -152,13 +152,13 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
       want[s] = need;
     }
   }
-  const long total = before_turn & ((1L << 48) - 1);
+  const int total = (int)min(before_turn & ((1L << 48) - 1), (long)c.pages);           // (more than there are do not come)
 
   // the first free pages, in order (the scan above has synchronised: no one looks for an open page any more)
   int *first_free = open_page, found = 0;
-  for (long base = 0; base < c.pages && found < total; base += (long)kWaves * kSpan) {
+  for (int base = 0; base < c.pages && found < total; base += kWaves * kSpan) {
     int count = 0;
-    const long first = base + (long)wave * kSpan;
+    const int first = base + wave * kSpan;
     if (base) load_counts(c, first, counts);
 #pragma unroll
     for (int k = 0; k < 16; ++k) count += __popcll(__ballot(counts[k] == 0 && first + k * kWave + lane < c.pages));
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
       for (int k = 0; k < 16; ++k) {
         const unsigned long long free_of = __ballot(counts[k] == 0 && first + k * kWave + lane < c.pages);
         const int mine = at + __popcll(free_of & ((1ull << lane) - 1));
-        if ((free_of >> lane & 1) && mine < total) (mine < kMaxSlots ? first_free : free_list)[mine] = (int)(first + k * kWave + lane);
+        if ((free_of >> lane & 1) && mine < total) (mine < kMaxSlots ? first_free : free_list)[mine] = first + k * kWave + lane;
         at += __popcll(free_of);
       }
   }
@@ -279,21 +279,21 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Pages c, int *plan, i
   __shared__ int sums[kWaves], sums2[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int mine = 0, count[16], used;
-  for (long base = 0; base < c.pages; base += (long)kWaves * kSpan) {
-    const long first = base + (long)wave * kSpan;
+  for (int base = 0; base < c.pages; base += kWaves * kSpan) {
+    const int first = base + wave * kSpan;
     load_counts(c, first, count);
 #pragma unroll
     for (int k = 0; k < 16; ++k) mine += count[k] != 0 && first + k * kWave + lane < c.pages;
   }
   scan_exclusive<int>(mine, sums, used);
   int sources = 0, places = 0;
-  for (long base = 0; base < c.pages; base += (long)kWaves * kSpan) {
+  for (int base = 0; base < c.pages; base += kWaves * kSpan) {
     unsigned long long in_use[16];
     int above = 0, below = 0;
-    load_counts(c, base + (long)wave * kSpan, count);
+    load_counts(c, base + wave * kSpan, count);
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const long p = base + (long)wave * kSpan + k * kWave + lane;
+      const int p = base + wave * kSpan + k * kWave + lane;
       in_use[k] = __ballot(p < c.pages && count[k] != 0);
       const unsigned long long high = __ballot(p >= used), low = __ballot(p < used);
       above += __popcll(in_use[k] & high);
@@ -310,12 +310,12 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Pages c, int *plan, i
     }
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const long p = base + (long)wave * kSpan + k * kWave + lane;
+      const int p = base + wave * kSpan + k * kWave + lane;
       const unsigned long long from = in_use[k] & __ballot(p >= used), to = ~in_use[k] & __ballot(p < used);
       const unsigned long long below_me = (1ull << lane) - 1;
-      if (from >> lane & 1) plan[1 + 2 * (a + __popcll(from & below_me))] = (int)p;
+      if (from >> lane & 1) plan[1 + 2 * (a + __popcll(from & below_me))] = p;
       else if (p >= used && p < c.pages) moved[p] = -1;
-      if (to >> lane & 1) plan[2 + 2 * (b + __popcll(to & below_me))] = (int)p;
+      if (to >> lane & 1) plan[2 + 2 * (b + __popcll(to & below_me))] = p;
       a += __popcll(from);
       b += __popcll(to);
     }

@@ -544,9 +544,9 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 // of its tiles, and a second launch joins them.
 
 //
-// Measured: 32 heads of a prompt of 8192 tokens 566 us (970 TFLOP/s of the visible pairs; a large library product reaches 1184), the
+// Measured: 32 heads of a prompt of 8192 tokens 564 us (976 TFLOP/s of the visible pairs; a large library product reaches 1184), the
 // matrix cores busy for 46 % of the cycles and the vector units about as long (6 of their instructions a product: widening, exponentials,
-// sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 405 us (600), 9 of their instructions a product.
+// sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 404 us (616), 9 of their instructions a product.
 // Two workgroups are what the registers hold of a compute unit; eight waves of 16 columns to a workgroup took 605 us in place of 591,
 // four of 64 columns spilled.
 
