@@ -300,3 +300,27 @@ def test_refusals():
             call()
             pytest.fail(f"call {i} was let through")
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("slots,page,heads,dim,dtype,group,window,sinks", [
+    (3, 16, 3, 64, "f16", 1, 0, 0), (9, 48, 2, 128, "bf16", 4, 40, 3), (5, 256, 8, 64, "bf16", 17, 0, 0), (40, 32, 2, 64, "f16", 5, 7, 20),
+    (70, 16, 1, 128, "bf16", 20, 100, 3)])
+def test_sequences_that_come_and_go(slots, page, heads, dim, dtype, group, window, sinks):
+    """Twelve turns, chosen at random, of a program that adds tokens, attends, forks, ends sequences and compacts its pool."""
+    r = np.random.default_rng(slots * page)
+    wide = -(-150 // page) + 1
+    p = Pair(slots, slots * wide * 2 // 3 + 2, page, wide, heads, dim, dtype, seed=slots, q_per_kv=group, window=window, sinks=sinks)
+    for turn in range(12):
+        if turn % 4 == 2:
+            source = r.integers(-1, slots, slots)
+            stay = r.random(slots) < 0.5
+            source[stay] = np.arange(slots)[stay]
+            p.select(source.tolist())
+        elif turn % 4 == 3 and turn > 4:
+            p.compact()
+        else:
+            got = p.reserve(r.integers(0, [2, 6, 75][turn % 3], slots))
+            p.append(got, [1.0, 30.0][turn % 2])
+            rows = [int(min(n, r.integers(1, 40))) if r.random() < 0.4 else 0 for n in got]
+            p.attend(rows if any(rows) else [1] + [0] * (slots - 1), size=[1.0, 5.0][turn % 2])
+    p.held()
