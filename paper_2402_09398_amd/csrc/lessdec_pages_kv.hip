@@ -115,8 +115,7 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   const long b = begin / kBlock + w - base(s);
   if (r.count == 0 || b < 0 || b * kBlock >= len) return;
   const int t0 = (int)b * kBlock;
-  const int block = block_index(c, s, head, (int)b);
-  if (block < 0) return;
+  const int page = c.table[(size_t)s * c.table_len + entry_of(c, (int)b)];           // (on its way beside the rows)
   const int off = begin > t0 ? begin - t0 : 0;                         // older tokens of the block
 
   // A lane has eight channels of two tokens (of every 64 channels), eight lanes a line of a token's row; of the cache a piece of 16 bytes of
@@ -129,10 +128,6 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
     tok[i] = (lane >> 3) + 8 * i;
     fresh[i] = tok[i] >= off && t0 + tok[i] < len;
   }
-  unsigned short *exps = reinterpret_cast<unsigned short *>(c.exps) + block;
-  unsigned char *kb = c.k + block * ((long)kBlock * D);
-  uint4 *vb = reinterpret_cast<uint4 *>(c.v + block * ((long)kBlock * D)) + lane;
-  auto key_at = [&](int h, int i) { return reinterpret_cast<uint2 *>(kb + h * 1024 + ((piece >> 1) * 16 + tok[i]) * 16 + (piece & 1) * 8); };
   uint4 x[2][H][2];
 #pragma unroll
   for (int which = 0; which < 2; ++which)
@@ -144,6 +139,12 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
         if (fresh[i])
           x[which][h][i] = load_once(reinterpret_cast<const uint4 *>(which ? a.v : a.k) + (long)(row0 + t0 + tok[i] - begin) * (a.stride / 8) + head * (D / 8) + h * 8 + piece);
       }
+  const int block = block_in(c, page, head, (int)b);
+  if (block < 0) return;
+  unsigned short *exps = reinterpret_cast<unsigned short *>(c.exps) + block;
+  unsigned char *kb = c.k + block * ((long)kBlock * D);
+  uint4 *vb = reinterpret_cast<uint4 *>(c.v + block * ((long)kBlock * D)) + lane;
+  auto key_at = [&](int h, int i) { return reinterpret_cast<uint2 *>(kb + h * 1024 + ((piece >> 1) * 16 + tok[i]) * 16 + (piece & 1) * 8); };
   uint4 old[H];
   const bool mixed = off > 0 && 4 * g + 3 >= off && t0 + 4 * g < len;  // the lane's four tokens of a value piece are not all older
 #pragma unroll
