@@ -8,6 +8,12 @@
 // One pass over the tokens with the running maximum M and both sums (fp32).  M follows the maximum only where a weight would pass
 // 2^kSlack (a wave asks once per tile); until then the weights' range in fp16 above 1 takes it up and nothing is rescaled.
 //
+// M is held in two parts, the score S and the value exponent E of the token that M was taken from.  Far from 0 an fp32 holds neither the exact
+// product behind a score nor a score and an exponent in one, so there a weight is 2^((s_j - S) + (e_j - E)), with s_j rounded as S was: the largest
+// token's weight is 2^kBase, and tokens of one score have one weight, wherever the scores lie.  Up to |S| = kNear one fma in
+// place of the three operations is off by 2^-13 at most, less than the weights' rounding to fp16.  Sums that leave a wave's registers are taken times 2^E, so
+// that S alone goes with them.
+//
 // Both kernels form the scores transposed, S^T = K Q^T, with tokens along the rows of a matrix tile: a lane's accumulator
 // registers are then tokens of one query column, and just those tokens are what the lane has to bring to the second product, O^T = V^T P^T,
 // so the weights never leave their registers.  A query column is a (row, query head of the group) pair: the heads of a group share the
@@ -28,6 +34,8 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kSlack = 8.f, kBase = 6.f;           // weights reach 2^(kBase + kSlack) = 2^14 (fp16: below 2^16), normal down to 2^-14
 constexpr float kMost = 32768.f;                     // of a sum of weights: no one is more
+constexpr float kNear = 1024.f;                      // scores (base 2) for which fp32 holds a score and a value's exponent in one
+constexpr float kFirstE = 40.f - kBase;              // of M before its first token: no exponent is larger
 
 // A lane's 16 bytes at a scalar address.  The asm keeps the address from being added to the lane's offset in vector registers, which loads in
 // flight would then be waited for; the pointer says that it is global memory, which the compiler no longer sees.
@@ -89,6 +97,31 @@ __device__ inline unsigned code_nans(unsigned w)     // 0xff where one of four c
   return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
 }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float product(float a, float b)   // rounded by itself, not within an fma
+{
+#pragma clang fp contract(off)
+  return a * b;
+}
+
+// M: the score and the value exponent, less kBase, of the token with the largest t so far.
+struct Top {
+  float s, e;
+  __device__ inline float above(float score, float exponent) const { return (score - s) + (exponent - e); }
+  // of two, the larger; where they are equal the one with the larger score, so that lanes that exchange theirs agree
+  __device__ inline void raise(float score, float exponent)
+  {
+    const float d = above(score, exponent);
+    const bool more = d > 0 || (d == 0 && score > s);
+    s = more ? score : s;
+    e = more ? exponent : e;
+  }
+  __device__ inline void raise_by_lane(int distance)
+  {
+    const float score = __shfl_xor(s, distance, kWave), exponent = __shfl_xor(e, distance, kWave);
+    raise(score, exponent);
+  }
+  __device__ inline float unit() const { return pow2((int)e); }
+};
 
 // The blocks of 16 tokens that rows at positions lo .. hi see some token of, as a list: the first ones, then those of the window.
 struct Span {
@@ -352,7 +385,8 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
     f4 acc[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) acc[t] = f4{0, 0, 0, 0};
-    float top = kLowest, total = 0;
+    Top top = {kLowest, kFirstE};
+    float total = 0;
     bool spoiled = false;
     auto attend_to = [&](int step) {
       const int t0[2] = {tokens_of(step, 0), tokens_of(step, 1)};
@@ -393,19 +427,25 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
               }
           }
         }
-      // t = factor x + ve; the factor is positive, so a block's largest x gives its largest t
-      float most = kLowest, factor[2], ve[2];
+      // the factor is positive, so a block's largest x gives its largest score
+      float ve[2];
+      Top most;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        factor[b] = pow2((signed char)ex[b]) * c.scale_log2;
+        const float factor = pow2((signed char)ex[b]) * c.scale_log2;
         ve[b] = (float)(signed char)(ex[b] >> 8);
-        most = fmaxf(most, fmaf(fmaxf(fmaxf(x[b][0], x[b][1]), fmaxf(x[b][2], x[b][3])), factor[b], ve[b]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[b][i] = product(x[b][i], factor);
+        const float y = fmaxf(fmaxf(x[b][0], x[b][1]), fmaxf(x[b][2], x[b][3]));
+        if (b == 0) most = Top{y, ve[0] - kBase};
+        else most.raise(y, ve[1] - kBase);
       }
-      if (__ballot(most > top + kSlack)) {
-        most = fmaxf(most, __shfl_xor(most, 16, kWave));
-        most = fmaxf(most, __shfl_xor(most, 32, kWave));
-        const float now = fmaxf(top, most), f = exp2_fast(top - now);
-        top = now;
+      if (__ballot(top.above(most.s, most.e) > kSlack)) {
+        most.raise_by_lane(16);
+        most.raise_by_lane(32);
+        const Top was = top;
+        top.raise(most.s, most.e);
+        const float f = exp2_fast(top.above(was.s, was.e));
         total *= f;
 #pragma unroll
         for (int i = 0; i < T; ++i) acc[i] *= f;
@@ -414,9 +454,9 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         float w[4];
-        const float zero = ve[b] - (top - kBase);
+        const float zero = ve[b] - top.e;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = exp2_fast(fmaf(x[b][i], factor[b], zero));
+        for (int i = 0; i < 4; ++i) w[i] = exp2_fast((x[b][i] - top.s) + zero);
         total = fmaf((w[0] + w[1]) + (w[2] + w[3]), pow2(-(signed char)(ex[b] >> 8)), total);
         weights[2 * b] = half_pair(w[0], w[1]);
         weights[2 * b + 1] = half_pair(w[2], w[3]);
@@ -456,12 +496,12 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
           }
       }
 
-    // the four waves' sums, relative to the largest of their maxima
+    // the four waves' sums, relative to the largest of their scores
     total += __shfl_xor(total, 16, kWave);
     total += __shfl_xor(total, 32, kWave);
-    if (g == 0) { tops[wave][n] = top; totals[wave][n] = total; }
+    if (g == 0) { tops[wave][n] = top.s; totals[wave][n] = total * top.unit(); }
     __syncthreads();
-    const float largest = fmaxf(fmaxf(tops[0][n], tops[1][n]), fmaxf(tops[2][n], tops[3][n])), f = exp2_fast(top - largest);
+    const float largest = fmaxf(fmaxf(tops[0][n], tops[1][n]), fmaxf(tops[2][n], tops[3][n])), f = exp2_fast(top.s - largest) * top.unit();
     if (n < cols)
 #pragma unroll
       for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
@@ -471,7 +511,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
       const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
       reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
           (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
-      if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+      if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
     };
     const bool whole = from == 0 && to == steps;
     // this share is number i of the (slot, head), which begins in worker w0; share 0 lies in that worker's second place, the others in the first
@@ -751,7 +791,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   f16v acc[OB];
 #pragma unroll
   for (int o = 0; o < OB; ++o) acc[o] = f16v{0};
-  float top = kLowest, sum = 0;
+  Top top = {kLowest, kFirstE};
+  float level = kLowest;                             // M less kBase, in one
+  unsigned long long far = 0;                        // lanes whose M is beyond kNear (as a bool 587 us at 8192 tokens, 32 heads, so 571)
+  float sum = 0;
   if (threadIdx.x == 0) spoiled = 0;
   if (from < to) {
     look(from);
@@ -823,13 +866,13 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     }
   };
   // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
-  // only looked for where one is: then M is moved and the weights are computed again.
+  // only looked for where one is, or where scores are far from 0: then M is moved and the weights are computed again, each step rounded by itself.
   u4 weights[2];
   float part[2];
   auto weigh = [&](int m) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const float zero = add[2 * m + b] - (top - kBase);
+      const float zero = add[2 * m + b] - level;
       part[b] = 0;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
@@ -839,23 +882,41 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
       }
     }
   };
+  auto weigh_exactly = [&](int m) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float factor = f[2 * m + b], e = add[2 * m + b] - top.e;
+      part[b] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float y = exp2_fast((product(x[m][b * 8 + i], factor) - top.s) + e), z = exp2_fast((product(x[m][b * 8 + i + 1], factor) - top.s) + e);
+        part[b] += y + z;
+        weights[b][i / 2] = half_pair(y, z);
+      }
+    }
+  };
   auto settle = [&](int m) {
-    if (__ballot(fmaxf(part[0], part[1]) > kMost)) {
-      float most = kLowest;
+    if (far | __ballot(fmaxf(part[0], part[1]) > kMost)) {
+      Top most;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         float y = x[m][b * 8];
 #pragma unroll
         for (int i = 1; i < 8; ++i) y = fmaxf(y, x[m][b * 8 + i]);      // (the factor is positive)
-        most = fmaxf(most, fmaf(y, f[2 * m + b], add[2 * m + b]));
+        const float score = product(y, f[2 * m + b]), e = add[2 * m + b] - kBase;
+        if (b == 0) most = Top{score, e};
+        else most.raise(score, e);
       }
-      most = fmaxf(most, __shfl_xor(most, 32, kWave));
-      const float now = fmaxf(top, most), less = exp2_fast(top - now);
-      top = now;
+      most.raise_by_lane(32);
+      const Top was = top;
+      top.raise(most.s, most.e);
+      const float less = exp2_fast(top.above(was.s, was.e));
+      level = top.s + top.e;
+      far = __ballot(fabsf(top.s) > kNear && top.s > kLowest);
       sum *= less;
 #pragma unroll
       for (int o = 0; o < OB; ++o) acc[o] *= less;
-      weigh(m);
+      weigh_exactly(m);
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) sum = fmaf(part[b], units[2 * m + b], sum);
@@ -952,13 +1013,15 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   if (splits > 1) {
     float *share = a.parts + few_floats(G, D) + (long)id * wide_floats(D);
     const int mine = wave * 32 + n;
+    const float unit_of_e = top.unit();
     if (from < to)
 #pragma unroll
       for (int o = 0; o < OB; ++o)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f4 *>(share + mine * D + o * 32 + i * 8 + h * 4) = f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]};
-    if (h == 0) { share[kWide * D + mine] = from < to ? top : -__builtin_inff(); share[kWide * (D + 1) + mine] = sum; }
+          *reinterpret_cast<f4 *>(share + mine * D + o * 32 + i * 8 + h * 4) =
+              f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]} * unit_of_e;
+    if (h == 0) { share[kWide * D + mine] = from < to ? top.s : -__builtin_inff(); share[kWide * (D + 1) + mine] = sum * unit_of_e; }
     return;
   }
   if (col > last_col) return;
@@ -973,7 +1036,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
       y.y = (unsigned)Operand<BF16>::store(acc[o][4 * i + 2] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 3] * r) << 16;
       reinterpret_cast<uint2 *>(a.out)[to_row * (D / 4) + o * 8 + i * 2 + h] = y;
     }
-  if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(sum)) * 0.6931471805599453f;
+  if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top.s + (top.e + __builtin_log2f(sum))) * 0.6931471805599453f;
 }
 
 // Eight columns of an item to a workgroup, eight shares on their way at a time.
@@ -1021,7 +1084,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
     const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
     reinterpret_cast<unsigned *>(a.out)[to * (D / 2) + d / 2] =
         (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
-    if (a.lse && d == 0) a.lse[to] = l == 0.f ? -__builtin_inff() : (top - kBase + __builtin_log2f(l)) * 0.6931471805599453f;
+    if (a.lse && d == 0) a.lse[to] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.6931471805599453f;
   }
 }
 
