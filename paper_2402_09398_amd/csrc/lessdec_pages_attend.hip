@@ -727,8 +727,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   };
   auto turn = [&] {
     at = at_next;
-    factor = pow2((signed char)exps_next) * c.scale_log2;
-    const int e = (signed char)(exps_next >> 8);
+    const int ex = at < 0 ? 0 : exps_next;           // (of what is not there the load gave any block's: powers of two that are no numbers, perhaps)
+    factor = pow2((signed char)ex) * c.scale_log2;
+    const int e = (signed char)(ex >> 8);
     shift = (float)e;
     unit = pow2(-e);
   };

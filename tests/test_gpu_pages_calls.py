@@ -1,0 +1,24 @@
+"""The paged cache in calls that its description allows and that come up less often: rows that begin behind row 0, more rows than tokens, pages that
+no one has written yet, tokens counted from a slot's end, values in lengths and starts that are out of range."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_pages import HALF_STEP, Pair
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("exponent", [-128, -127, 127])
+@pytest.mark.parametrize("rows", [1, 20, 70])
+@pytest.mark.parametrize("dim,dtype", [(64, "f16"), (128, "bf16")])
+def test_a_pool_that_is_not_written_yet(exponent, rows, dim, dtype):
+    """The first page belongs to a slot that has its room and no tokens yet, and holds whatever the memory held: what lies behind another slot's
+    end, or on a page that is not there, is read from it and must not count."""
+    p = Pair(3, 60, 16, 30, 2, dim, dtype, q_per_kv=2)
+    p.own.exps.fill_(exponent)
+    p.reserve([16, 71, 400])
+    p.append([0, 71, 400])
+    p.attend([0, rows, rows])
+    p.own.table[2, 3] = p.ref.table[2, 3] = -1
+    p.own.table[2, 20] = p.ref.table[2, 20] = -1
+    p.attend([0, rows, rows])
