@@ -107,18 +107,23 @@ __device__ inline float product(float a, float b)   // rounded by itself, not wi
 struct Top {
   float s, e;
   __device__ inline float above(float score, float exponent) const { return (score - s) + (exponent - e); }
-  // of two, the larger; where they are equal the one with the larger score, so that lanes that exchange theirs agree
   __device__ inline void raise(float score, float exponent)
   {
-    const float d = above(score, exponent);
-    const bool more = d > 0 || (d == 0 && score > s);
+    const bool more = above(score, exponent) > 0;
     s = more ? score : s;
     e = more ? exponent : e;
   }
-  __device__ inline void raise_by_lane(int distance)
+  // the larger of two lanes' that lie Distance apart, in both; the swap has the lower lane's in one result and the upper one's in the other
+  template <int Distance> __device__ inline void raise_over()
   {
-    const float score = __shfl_xor(s, distance, kWave), exponent = __shfl_xor(e, distance, kWave);
-    raise(score, exponent);
+    auto swapped = [](float x) {
+      const unsigned bits = __float_as_uint(x);
+      return Distance == 32 ? __builtin_amdgcn_permlane32_swap(bits, bits, false, false) : __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    };
+    const auto scores = swapped(s), exponents = swapped(e);
+    s = __uint_as_float(scores[0]);
+    e = __uint_as_float(exponents[0]);
+    raise(__uint_as_float(scores[1]), __uint_as_float(exponents[1]));
   }
   __device__ inline float unit() const { return pow2((int)e); }
 };
@@ -428,21 +433,20 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
           }
         }
       // the factor is positive, so a block's largest x gives its largest score
-      float ve[2];
-      Top most;
+      float ve[2], y[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const float factor = pow2((signed char)ex[b]) * c.scale_log2;
         ve[b] = (float)(signed char)(ex[b] >> 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[b][i] = product(x[b][i], factor);
-        const float y = fmaxf(fmaxf(x[b][0], x[b][1]), fmaxf(x[b][2], x[b][3]));
-        if (b == 0) most = Top{y, ve[0] - kBase};
-        else most.raise(y, ve[1] - kBase);
+        y[b] = fmaxf(fmaxf(x[b][0], x[b][1]), fmaxf(x[b][2], x[b][3]));
       }
-      if (__ballot(top.above(most.s, most.e) > kSlack)) {
-        most.raise_by_lane(16);
-        most.raise_by_lane(32);
+      if (__ballot(fmaxf(top.above(y[0], ve[0]), top.above(y[1], ve[1])) > kBase + kSlack)) {
+        Top most = {y[0], ve[0] - kBase};
+        most.raise(y[1], ve[1] - kBase);
+        most.raise_over<16>();
+        most.raise_over<32>();
         const Top was = top;
         top.raise(most.s, most.e);
         const float f = exp2_fast(top.above(was.s, was.e));
@@ -587,8 +591,8 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 // Measured: 32 heads of a prompt of 8192 tokens 564 us (976 TFLOP/s of the visible pairs; a large library product reaches 1184), the
 // matrix cores busy for 46 % of the cycles and the vector units about as long (6 of their instructions a product: widening, exponentials,
 // sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 404 us (616), 9 of their instructions a product.
-// Two workgroups are what the registers hold of a compute unit; eight waves of 16 columns to a workgroup took 605 us in place of 591,
-// four of 64 columns spilled.
+// Two workgroups are what the registers hold of a compute unit at D = 128, three at 64 (8192 tokens, 32 heads: 350 us, 365 with two);
+// eight waves of 16 columns to a workgroup took 605 us in place of 591, four of 64 columns spilled.
 
 constexpr int kWide = 128, kTile = 64;               // columns and tokens
 // Workgroups that are enough not to split: two to a compute unit.  128 rows over 8192 tokens, 32 heads: 54 us (67 with 256, 46 with
@@ -659,7 +663,7 @@ __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bo
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
   __shared__ __align__(16) u4 tiles_of[4][kTile * D / 8];
@@ -908,7 +912,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
         if (b == 0) most = Top{score, e};
         else most.raise(score, e);
       }
-      most.raise_by_lane(32);
+      most.raise_over<32>();
       const Top was = top;
       top.raise(most.s, most.e);
       const float less = exp2_fast(top.above(was.s, was.e));
