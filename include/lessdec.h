@@ -329,7 +329,7 @@ int lessdec_pages_reset(const lessdec_pages_desc *desc, void *hip_stream);
  *  - with `window`: pages that hold only tokens which no row at position >= length[s] (as it was) sees are let go;
  *  - if its last page is partly filled and other slots still share it, the slot gets a page of its own in its place (the last of
  *    the sharers that write keeps the page if no one else has it) and the pair of pages goes on the plan;
- *  - pages for the new tokens.
+ *  - pages for the new tokens; none in the place of a partly filled one that the table does not name, as append passes over its tokens.
  * Free pages are handed out in ascending order to the slots in ascending order.  A slot that would outgrow its
  * table row is passed over; where the free pages do not suffice for a slot, neither it nor a later one gets any.
  * plan: [1 + 2 slots]: the number of pairs, then (from, to) by slot; to be carried out by

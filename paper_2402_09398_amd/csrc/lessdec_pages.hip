@@ -121,7 +121,6 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
     int need = 0, copies = 0;
     if (wanted[t]) {
       const int n = wanted[t], len = length[t];
-      int own = 0;                                   // a new page in the place of the partly filled one: shared, or not there
       if (len % pt) {
         const int p = old_page[t], sharers = p >= 0 ? count_of(c.refs, p) : 0;
         if (sharers > 1) {
@@ -138,9 +137,10 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(Pages c, const int *n
           }
           copies = sharers - before > 1;
         }
-        own = p < 0 || copies;
       }
-      need = (int)((len + (long)n + pt - 1) / pt) - (len + pt - 1) / pt + own;
+      // (`copies`: a new page in the place of the partly filled one.  None where the table names none there: what an earlier
+      // sequence left on it would be read as this one's older tokens.)
+      need = (int)((len + (long)n + pt - 1) / pt) - (len + pt - 1) / pt + copies;
     }
     long all;                                        // both sums in one word: 2^12 slots of less than 2^27 pages each
     const long x = scan_exclusive<long>(need | (long)copies << 48, sums, all) + before_turn;

@@ -22,3 +22,21 @@ def test_a_pool_that_is_not_written_yet(exponent, rows, dim, dtype):
     p.own.table[2, 3] = p.ref.table[2, 3] = -1
     p.own.table[2, 20] = p.ref.table[2, 20] = -1
     p.attend([0, rows, rows])
+
+
+def test_a_slot_whose_last_page_is_missing():
+    """Room for a slot whose partly filled page its table does not name: no page in its place (it would show what an earlier sequence left there);
+    its new tokens on that page are passed over, those behind it have theirs."""
+    for counts in ([1, 1, 1], [40, 3, 30]):
+        p = Pair(3, 20, 16, 8, 1, 64)
+        n = [21, 40, 16]
+        p.reserve(n)
+        p.append(n)
+        p.own.table[0, 1] = p.ref.table[0, 1] = -1
+        p.own.table[1, 2] = p.ref.table[1, 2] = -1
+        p.own.refs[:] = p.ints([1, 0, 1, 1, 0, 1] + [0] * 14)
+        p.ref.refs[:] = [1, 0, 1, 1, 0, 1] + [0] * 14
+        p.reserve(counts)
+        p.append(counts)
+        p.held()
+        p.attend(counts)
