@@ -96,6 +96,8 @@ __device__ inline unsigned code_nans(unsigned w)     // 0xff where one of four c
 {
   return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u;
 }
+// x / l as x * r, 0 for a row that sees nothing (whose x is NaN if values that it sees with weight 0 are)
+__device__ inline float share_of(float x, float l, float r) { return l == 0.f ? 0.f : x * r; }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float product(float a, float b)   // rounded by itself, not within an fma
 {
@@ -511,10 +513,10 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
       for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
     __syncthreads();
     auto finish = [&](int col, int d, float x, float y, float m, float l) {
-      const float r = l == 0.f ? 0.f : 1.f / l;
+      const float r = 1.f / l;
       const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
       reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
-          (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+          (unsigned)Operand<BF16>::store(share_of(x, l, r)) | (unsigned)Operand<BF16>::store(share_of(y, l, r)) << 16;
       if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_log2f(l)) * 0.6931471805599453f;
     };
     const bool whole = from == 0 && to == steps;
@@ -1030,15 +1032,14 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void wide_kernel(Pages c, Att
     return;
   }
   if (col > last_col) return;
-  const float r = sum == 0.f ? 0.f : 1.f / sum;
+  const float r = 1.f / sum;
   const long to_row = (long)row * c.heads * G + q_head;
 #pragma unroll
   for (int o = 0; o < OB; ++o)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint2 y;
-      y.x = (unsigned)Operand<BF16>::store(acc[o][4 * i] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 1] * r) << 16;
-      y.y = (unsigned)Operand<BF16>::store(acc[o][4 * i + 2] * r) | (unsigned)Operand<BF16>::store(acc[o][4 * i + 3] * r) << 16;
+      auto stored = [&](int j) { return (unsigned)Operand<BF16>::store(share_of(acc[o][4 * i + j], sum, r)); };
+      const uint2 y = make_uint2(stored(0) | stored(1) << 16, stored(2) | stored(3) << 16);
       reinterpret_cast<uint2 *>(a.out)[to_row * (D / 4) + o * 8 + i * 2 + h] = y;
     }
   if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top.s + (top.e + __builtin_log2f(sum))) * 0.6931471805599453f;
@@ -1085,10 +1086,10 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
         y = fmaf(v[j].y, e, y);
       }
     }
-    const float r = l == 0.f ? 0.f : 1.f / l;
+    const float r = 1.f / l;
     const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
     reinterpret_cast<unsigned *>(a.out)[to * (D / 2) + d / 2] =
-        (unsigned)Operand<BF16>::store(x * r) | (unsigned)Operand<BF16>::store(y * r) << 16;
+        (unsigned)Operand<BF16>::store(share_of(x, l, r)) | (unsigned)Operand<BF16>::store(share_of(y, l, r)) << 16;
     if (a.lse && d == 0) a.lse[to] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.6931471805599453f;
   }
 }

@@ -40,3 +40,19 @@ def test_a_slot_whose_last_page_is_missing():
         p.append(counts)
         p.held()
         p.attend(counts)
+
+
+@pytest.mark.parametrize("rows,length", [(1, 70), (4, 70), (70, 80), (12, 9000)])
+def test_scores_of_minus_infinity_over_values_that_are_no_numbers(rows, length):
+    """A row whose every score is -inf gives zeros whatever the values hold, NaN among them; a row with one other score sees them."""
+    p = Pair(1, length // 16 + 2, 16, length // 16 + 2, 1, 64, "bf16", q_per_kv=2)
+
+    def spoil(k, v, start):
+        k[:, 0, 0] = 1 + k[:, 0, 0].abs()
+        v[3, 0, 5], v[20, 0, 7], v[length - 1, 0, 9] = float("nan"), float("inf"), float("nan")
+    p.reserve([length])
+    p.append([length], spoil=spoil)
+    q = p.t.tensor(p.rng.standard_normal((rows + 2, 2, 64))).to(p.own.tdtype)
+    q[:, 0] = 0
+    q[:, 0, 0] = -float("inf")
+    p.attend([rows], queries=q)
