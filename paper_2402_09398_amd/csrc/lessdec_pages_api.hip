@@ -53,7 +53,8 @@ int check(const lessdec_pages_desc *d, int needs, int rows, int layer, Pages *c)
   c->heads = d->heads; c->head_dim = d->head_dim; c->q_per_kv = d->q_per_kv > 1 ? d->q_per_kv : 1;
   const unsigned per = (unsigned)(d->page_tokens / kBlock);
   c->inverse = per == 1 ? 0 : (unsigned)(((1ull << 32) + per - 1) / per);
-  c->sinks = d->sinks; c->window = d->window;
+  // a window that no sequence outgrows is none: positions less the window then stay within an int for any window allowed
+  c->sinks = d->sinks; c->window = d->window < d->table_len * d->page_tokens ? d->window : 0;
   const double scale = d->scale > 0.f ? (double)d->scale : d->head_dim == 64 ? 0.125 : 0.08838834764831845;
   c->scale_log2 = (float)(scale * 1.4426950408889634);
   const size_t blocks = (size_t)layer * d->pages * d->heads * (d->page_tokens / kBlock);

@@ -420,7 +420,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
           for (int i = 0; i < 4; ++i) {
             const int token = t0[b] + 4 * g + i;
             x[b][i] = t0[b] >= 0 && sees(c, p, token) ? x[b][i] : -__builtin_inff();
-            if (t0[b] >= 0 && token <= hi && (c.window == 0 || token > lo - c.window || token < c.sinks)) keep |= 255u << 8 * i;
+            if (t0[b] >= 0 && token <= hi && (c.window == 0 || token + c.window > lo || token < c.sinks)) keep |= 255u << 8 * i;
           }
 #pragma unroll
           for (int h = 0; h < H; ++h) {
@@ -703,7 +703,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void wide_kernel(Pages c, Att
   const int row = rows.first + col / G, q_head = head * G + col % G;
   // the row, at p, sees the tokens from_token .. p and those before first_tokens
   const int p = col <= last_col ? before + col / G : -1;
-  const int from_token = c.window > 0 ? max(p - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
+  const int from_token = c.window > 0 ? max(max(p, 0) - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
   u4 q[KK];
 #pragma unroll
   for (int k = 0; k < KK; ++k) {
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void wide_kernel(Pages c, Att
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int t0 = span.block(tile * 4 + b) * kBlock;
-        some |= at_of(tile, b) >= 0 && t0 <= wave_hi && (c.window == 0 || t0 + kBlock > wave_lo - c.window || t0 < c.sinks);
+        some |= at_of(tile, b) >= 0 && t0 <= wave_hi && (c.window == 0 || t0 + kBlock + c.window > wave_lo || t0 < c.sinks);
       }
       active &= some;
     }

@@ -56,3 +56,20 @@ def test_scores_of_minus_infinity_over_values_that_are_no_numbers(rows, length):
     q[:, 0] = 0
     q[:, 0, 0] = -float("inf")
     p.attend([rows], queries=q)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 16, 2 ** 30, 0, 5])
+@pytest.mark.parametrize("counts", [[3, 8, 2], [8, 0, 5], [40, 90, 3], [130, 33, 1]])
+def test_more_rows_than_tokens(window, counts):
+    """Rows whose position would be below 0 are not stored and see nothing; the others are as ever, with a window as large as the type allows, too."""
+    for sinks in (0, 2, 2 ** 31 - 1):
+        p = Pair(3, 12, 16, 4, 2, 64, "f16", q_per_kv=1 + len(set(counts)) % 2, window=window, sinks=sinks)
+        p.reserve([1, 33, 2])
+        p.append([1, 33, 2])
+        p.append(counts)
+        p.attend(counts)
+        p.held()
+        p.reserve([min(20, counts[0]), min(1, counts[1]), 0])
+        p.append(counts)
+        p.attend(counts)
+        p.held()
