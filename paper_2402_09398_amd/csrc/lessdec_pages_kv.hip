@@ -112,8 +112,8 @@ __global__ __launch_bounds__(256) void append_kernel(Pages c, AppendArgs a)
   const Rows r = slot_rows(a.start, s, a.rows);
   const int len = slot_length(c, s), begin = len > r.count ? len - r.count : 0;
   const int row0 = r.first + r.count - (len - begin);                  // row of the token at position begin
-  const long b = begin / kBlock + w - base(s);
-  if (r.count == 0 || b < 0 || b * kBlock >= len) return;
+  const long nth = w - base(s), b = begin / kBlock + nth;              // (below 0: a wave before the first slot's rows)
+  if (r.count == 0 || nth < 0 || b * kBlock >= len) return;
   const int t0 = (int)b * kBlock;
   const int page = c.table[(size_t)s * c.table_len + entry_of(c, (int)b)];           // (on its way beside the rows)
   const int off = begin > t0 ? begin - t0 : 0;                         // older tokens of the block

@@ -73,3 +73,37 @@ def test_more_rows_than_tokens(window, counts):
         p.append(counts)
         p.attend(counts)
         p.held()
+
+
+@pytest.mark.parametrize("slots,first", [(3, 1), (3, 100), (3, 1000), (70, 777), (300, 40)])
+def test_rows_that_begin_behind_the_first(slots, first):
+    """start[0] > 0: rows before it belong to no slot and blocks before the new tokens are left as they are, byte for byte."""
+    p = Pair(slots, 12 * slots, 16, 16, 1, 64, "bf16", q_per_kv=3)
+    n = [120 + s % 50 for s in range(slots)]
+    p.reserve(n)
+    p.append(n)
+    for counts in ([1 + s % 3 for s in range(slots)], [20 + s % 60 if slots < 100 else 3 + s % 20 for s in range(slots)]):
+        p.reserve(counts)
+        start = first + np.concatenate([[0], np.cumsum(counts)])
+        block = p.own.table.view(slots, -1).long()
+        begin = p.own.length.long() - p.ints(counts).long()
+        behind = p.t.arange(16, device="cuda") < (begin // 16)[:, None]          # pages of a block each that hold older tokens alone
+        older = block[behind & (block >= 0)]
+        saved = p.own.exps.clone()
+        p.own.exps[:, older] = 77                             # (which no append has written)
+        k, v = (p.t.tensor(p.rng.standard_normal((start[-1] + 2, 1, 64))).to(p.own.tdtype) for _ in range(2))
+        codes = [x.clone() for x in (p.own.k_codes, p.own.v_codes)]
+        p.own.append(0, k.cuda(), v.cuda(), p.ints(start))
+        assert (p.own.exps[:, older] == 77).all()
+        p.own.exps[:, older] = saved[:, older]
+        for now, was in zip((p.own.k_codes, p.own.v_codes), codes):
+            assert p.t.equal(now.view(p.ref.pages, -1)[older], was.view(p.ref.pages, -1)[older])
+        p.ref.append(0, k.double().numpy(), v.double().numpy(), start)
+        p.held()
+        q = p.t.tensor(p.rng.standard_normal((start[-1] + 2, 3, 64))).to(p.own.tdtype)
+        out = p.t.full(q.shape, 3.5, dtype=p.own.tdtype, device="cuda")
+        p.own.attend(0, q.cuda(), out, p.ints(start), max(counts))
+        want, _, tol, _ = p.ref.attend(0, q.double().numpy(), start, HALF_STEP["bf16"])
+        got = out.double().cpu().numpy()
+        assert (got[:first] == 3.5).all() and (got[start[-1]:] == 3.5).all()
+        assert (np.abs(got - want) <= tol)[first:start[-1]].all()
