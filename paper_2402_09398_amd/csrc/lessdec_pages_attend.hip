@@ -654,7 +654,7 @@ __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bo
   }
   t.count = rows.count * G;
   const int n = (t.count + kWide - 1) / kWide;
-  if (i >= n || t.count <= kCols) return false;
+  if (i < 0 || i >= n || t.count <= kCols) return false;               // (i < 0: before the first slot's rows)
   t.slot = __builtin_amdgcn_readfirstlane(t.slot);
   t.count = __builtin_amdgcn_readfirstlane(t.count);
   t.len = __builtin_amdgcn_readfirstlane(t.len);
