@@ -375,7 +375,8 @@ int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const vo
  * it, does not reach that row.
  * Scores, softmax statistics and sums are fp32; the weights are rounded to fp16 for the product with the values (a relative
  * error of 2^-11 at most in each, down to 2^-28 of the row's largest contribution); out is rounded once, to dtype (fp16: infinite
- * from 65520 on, which a value of 65504, held as 65536, reaches).  With rows = 0, as with nothing to append or read, no pointer is looked at.
+ * from 65520 on, which a value of 65504, held as 65536, reaches).  With rows = 0 or max_new = 0, as with nothing to append or read, no pointer argument and no
+ * workspace is looked at.
  */
 int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t q_stride, void *out, float *lse,
                          const int32_t *start, int32_t rows, int32_t max_new, void *hip_stream);

@@ -148,9 +148,9 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
   if (step < 0 || rows < 0 || max_new < 0 || (long)rows * c.q_per_kv >= 1L << 31 || ((long)rows * c.q_per_kv / 128 + desc->slots) * desc->heads > 1L << 30) return LESSDEC_EINVAL;
+  if (rows == 0 || max_new == 0) return LESSDEC_OK;
   rc = check(desc, kWork, rows, layer, &c);
   if (rc) return rc;
-  if (rows == 0 || max_new == 0) return LESSDEC_OK;
   if (!q || !out || !start || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4)) return LESSDEC_EINVAL;
   AttendArgs a{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<int *>(desc->workspace),
                static_cast<float *>(scratch(desc))};
