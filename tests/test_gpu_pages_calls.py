@@ -107,3 +107,64 @@ def test_rows_that_begin_behind_the_first(slots, first):
         got = out.double().cpu().numpy()
         assert (got[:first] == 3.5).all() and (got[start[-1]:] == 3.5).all()
         assert (np.abs(got - want) <= tol)[first:start[-1]].all()
+
+
+@pytest.mark.parametrize("heads,dim,page,dtype", [(2, 64, 16, "f16"), (1, 128, 48, "bf16")])
+def test_tokens_counted_from_a_slots_end(heads, dim, page, dtype):
+    """read with negative `first` (before the slot's beginning, too), in the middle of a block, past the end; the same slot twice; slots that do not exist."""
+    p = Pair(4, 40, page, 8, heads, dim, dtype)
+    n = [50, 0, 17, 100]
+    p.reserve(n)
+    p.append(n, size=30.0)
+    slots = [3, 0, -1, 2, 3, 4, 1, 2 ** 31 - 1, -2 ** 31]
+    for first, count in ((-1, 1), (-17, 17), (-33, 20), (-100, 100), (-120, 70), (-2 ** 31, 5), (1, 15), (19, 40), (48, 3), (99, 33), (100, 2), (2 ** 31 - 1, 4)):
+        K, V = (p.t.full((len(slots), heads, count, dim), 7.0, dtype=p.own.tdtype, device="cuda") for _ in range(2))
+        p.own.read(0, p.ints(slots), first, K, V)
+        want = p.ref.read(0, slots, first, count, float(p.t.finfo(p.own.tdtype).max))
+        for got, w in zip((K, V), want):
+            np.testing.assert_array_equal(got.double().cpu().numpy(), p.t.tensor(w).to(p.own.tdtype).double().numpy())
+
+
+@pytest.mark.parametrize("slots,group", [(4, 1), (4, 5), (70, 5)])
+def test_lengths_and_starts_out_of_range(slots, group):
+    """Lengths and entries of start beyond their range count as the nearer end, to the bit; rows out of order touch nothing but the arrays."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    bad, near = [-5, high, 40, low] * (slots // 4 + 1), [0, 8 * 16, 40, 0] * (slots // 4 + 1)
+    pairs = [Pair(slots, slots * 8, 16, 8, 2, 64, "f16", seed=3, q_per_kv=group) for _ in range(2)]
+    rows = 400
+    for p, length in zip(pairs, (bad, near)):
+        fill = [100 if s % 4 == 1 else 40 if s % 4 == 2 else 20 for s in range(slots)]
+        p.reserve(fill)
+        p.append(fill)
+        p.own.length.copy_(p.ints(length[:slots]))
+    t, ints = pairs[0].t, pairs[0].ints
+    k, v = (t.tensor(pairs[0].rng.standard_normal((rows, 2, 64))).half().cuda() for _ in range(2))
+    q = t.tensor(pairs[0].rng.standard_normal((rows, 2 * group, 64))).half().cuda()
+    tail = [390] * (slots - 3)
+    starts = [([-7, 3, 90] + tail[:-1] + [rows, high], [0, 3, 90] + tail[:-1] + [rows, rows]), ([low, 0, 200] + tail + [high], [0, 0, 200] + tail + [rows])]
+    for start, nearest in starts:
+        assert len(start) == len(nearest) == slots + 1
+        for most in (3, rows):
+            got = []
+            for p, at in zip(pairs, (start, nearest)):
+                p.own.append(0, k, v, ints(at))
+                out = t.full((rows + 64, 2 * group, 64), 3.5, dtype=t.float16, device="cuda")
+                p.own.attend(0, q, out[32:-32], ints(at), most)
+                assert (out[:32] == 3.5).all() and (out[-32:] == 3.5).all()
+                K, V = (t.full((slots, 2, 33, 64), 7.0, dtype=t.float16, device="cuda") for _ in range(2))
+                p.own.read(0, ints(range(slots)), -33, K, V)
+                got.append([out, K, V] + [getattr(p.own, n) for n in ("k_codes", "v_codes", "exps", "table", "refs")])
+            for a, b in zip(*got):
+                assert t.equal(a.view(t.uint8) if a.is_floating_point() else a, b.view(t.uint8) if b.is_floating_point() else b)
+    p = pairs[0]
+    r = np.random.default_rng(slots)
+    for _ in range(6):
+        at = r.integers(-50, rows + 50, slots + 1)
+        at[::5] = r.choice([low, high, 0, rows], len(at[::5]))
+        p.own.length.copy_(ints(r.choice([low, high, -1, 0, 1, 40, 128, 129], slots)))
+        for most in (1, 3, rows):
+            out = t.full((rows + 64, 2 * group, 64), 3.5, dtype=t.float16, device="cuda")
+            p.own.append(0, k, v, ints(at))
+            p.own.attend(0, q, out[32:-32], ints(at), most)
+            assert (out[:32] == 3.5).all() and (out[-32:] == 3.5).all()
+    t.cuda.synchronize()
