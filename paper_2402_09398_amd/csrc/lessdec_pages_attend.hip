@@ -593,7 +593,7 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 // Measured: 32 heads of a prompt of 8192 tokens 564 us (976 TFLOP/s of the visible pairs; a large library product reaches 1184), the
 // matrix cores busy for 46 % of the cycles and the vector units about as long (6 of their instructions a product: widening, exponentials,
 // sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 404 us (616), 9 of their instructions a product.
-// Two workgroups are what the registers hold of a compute unit at D = 128, three at 64 (8192 tokens, 32 heads: 350 us, 365 with two);
+// Two workgroups are what the registers hold of a compute unit at D = 128, three at 64 (167 registers; 8192 tokens, 32 heads: 351 us, 365 with two);
 // eight waves of 16 columns to a workgroup took 605 us in place of 591, four of 64 columns spilled.
 
 constexpr int kWide = 128, kTile = 64;               // columns and tokens
@@ -665,7 +665,7 @@ __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bo
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
+__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
   __shared__ __align__(16) u4 tiles_of[4][kTile * D / 8];
