@@ -168,3 +168,40 @@ def test_lengths_and_starts_out_of_range(slots, group):
             p.own.attend(0, q, out[32:-32], ints(at), most)
             assert (out[:32] == 3.5).all() and (out[-32:] == 3.5).all()
     t.cuda.synchronize()
+
+
+def test_plans_and_requests_out_of_range():
+    """copy passes over pairs outside the pool and carries out no more than it is told; requests of the ends of the type; counts that are no counts."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    p = Pair(4, 24, 32, 5, 2, 64, "f16", layers=2)
+    n = [100, 31, 0, 64]
+    p.reserve(n)
+    p.append(n)
+    pairs = [(0, 20), (24, 21), (1, -1), (low, 22), (2, high), (high, low), (3, 23)]
+    plan = p.ints([len(pairs)] + [x for pair in pairs for x in pair] + [7] * 32)
+    before = [x.clone() for x in (p.own.k_codes, p.own.v_codes, p.own.exps)]
+    for count, most in ((len(pairs), len(pairs)), (high, len(pairs)), (low, len(pairs)), (-1, 3), (len(pairs), 1)):
+        plan[0] = count
+        for x, was in zip((p.own.k_codes, p.own.v_codes, p.own.exps), before):
+            x.copy_(was)
+        p.own.copy(plan, most)
+        moved = pairs[:max(0, min(count, most))]
+        for x, was in zip((p.own.k_codes, p.own.v_codes, p.own.exps), before):
+            now, want = x.view(2, 24, -1), was.view(2, 24, -1).clone()
+            for a, b in moved:
+                if 0 <= a < 24 and 0 <= b < 24:
+                    want[:, b] = was.view(2, 24, -1)[:, a]
+            assert p.t.equal(now, want), (count, most)
+    p.reserve([high, low, 161, high - 31])
+    p.reserve([1, 129, high, low])
+    granted = p.ints([-9] * 4)
+    r = np.random.default_rng(4)
+    for _ in range(6):                                        # (nothing to compare: what is read stays in range, and the calls end)
+        p.own.refs.copy_(p.ints(r.choice([low, -1, 0, 1, 2, high], 24)))
+        p.own.table.copy_(p.ints(r.choice([low, -1, 0, 5, 23, 24, high], (4, 5))))
+        p.own.length.copy_(p.ints(r.choice([low, 0, 7, 32, 150, 160, 161, high], 4)))
+        p.own.reserve(p.ints(r.choice([low, 0, 1, 40, 160, high], 4)), granted, p.plan)
+        p.own.select(p.ints(r.choice([low, -1, 0, 1, 3, 4, high], 4)))
+        p.own.compact(p.plan)
+        p.own.copy(p.plan, 12)
+    p.t.cuda.synchronize()
