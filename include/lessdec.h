@@ -282,7 +282,8 @@ int lessdec_probe_stream_read(const void *buf, size_t bytes, int32_t waves, uint
  * Row arguments (q, k, v, out) are packed over the slots: rows start[s] .. start[s+1] - 1 belong to slot s, start
  * [slots+1] ascending; they are the slot's LAST start[s+1] - start[s] tokens, so row start[s] + i is the token at position
  * length[s] - (start[s+1] - start[s]) + i.  Rows behind the last slot's are neither read nor written; a row whose position would be
- * below 0 is not stored and sees nothing.
+ * below 0 is not stored and sees nothing.  Rows for a slot whose request for room was not granted would take the place of its last tokens, on a
+ * page that other slots may share, too: give none before it is.
  * length, table and refs change through lessdec_pages_reserve, _select, _compact and _reset alone; a slot ends, or starts again, by _select.
  * A generation step: lessdec_pages_reserve (which advances length), lessdec_pages_copy, then for every layer
  * lessdec_pages_append and lessdec_pages_attend.  All of it can be captured in a HIP graph: lengths, tables and plans are
@@ -373,8 +374,9 @@ int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const vo
  * max_new: no slot has more rows than this; rows of one that does may be left unwritten.
  * A row that sees nothing, or only scores of -inf, gives zeros and an lse of -inf.  What a token that a row does not see holds, NaN among
  * it, does not reach that row.
- * Scores, softmax statistics and sums are fp32; the weights are rounded to fp16 for the product with the values (a relative
- * error of 2^-11 at most in each, down to 2^-28 of the row's largest contribution); out is rounded once, to dtype (fp16: infinite
+ * Scores, softmax statistics and sums are fp32, and hold at any size that fp32 has (tokens of one score share alike); the weights are
+ * rounded to fp16 for the product with the values: an error in each of 2^-11 of it at most, or of 2^-31 of the row's largest, each weight times its value
+ * block's 2^e (so channels of a block that is 2^-31 of another lose their part); out is rounded once, to dtype (fp16: infinite
  * from 65520 on, which a value of 65504, held as 65536, reaches).  With rows = 0 or max_new = 0, as with nothing to append or read, no pointer argument and no
  * workspace is looked at.
  */
@@ -382,7 +384,8 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
                          const int32_t *start, int32_t rows, int32_t max_new, void *hip_stream);
 
 /*
- * The values that a layer of the cache holds, e.g. for lessdec_prefill, when a sequence goes over to the compressed cache.
+ * The values that a layer of the cache holds, e.g. for lessdec_prefill, when a sequence goes over to the compressed cache (an fp16 cache's as they
+ * are; lessdec_prefill takes no bfloat16).
  * slots: [n], n <= 65535.  K, V: [n][heads][count][D] dtype, 16-byte aligned: tokens first .. first + count - 1 of
  * slots[i], counted from the slot's end if first < 0 (-count: its last count tokens).  Tokens that the slot does not
  * have (or no longer has) and slots outside [0, slots) give zeros; what exceeds dtype's largest finite value gives that value.

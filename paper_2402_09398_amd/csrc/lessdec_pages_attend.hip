@@ -16,7 +16,8 @@
 //
 // Both kernels form the scores transposed, S^T = K Q^T, with tokens along the rows of a matrix tile: a lane's accumulator
 // registers are then tokens of one query column, and just those tokens are what the lane has to bring to the second product, O^T = V^T P^T,
-// so the weights never leave their registers.  A query column is a (row, query head of the group) pair: the heads of a group share the
+// so the weights never leave their registers.  They are rounded to fp16 for it, the sum's are not: fp16 outputs are off by 2.6e-4 of their size in place of the
+// 2.1e-4 of fp32 weights and the output's own rounding, bfloat16 ones by 1.7e-3 either way (the cases of perf/operators.py).  A query column is a (row, query head of the group) pair: the heads of a group share the
 // cached keys and values that a tile has loaded.
 #include "lessdec_pages.h"
 
@@ -183,7 +184,8 @@ __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__
 constexpr int kCols = 16, kStepBlocks = 8;
 constexpr int kGroup = 32;
 // Three workgroups to a compute unit; where that would make more than 32 shares of a (slot, head) down to one, which reads as
-// fast (one sequence of 131072 tokens, 8 heads: 54 us with 256 workgroups, 61 with 512, 64 with 768).
+// fast (one sequence of 131072 tokens, 8 heads: 54 us with 256 workgroups, 61 with 512, 64 with 768).  Counted are the slots that the cache
+// has, as lengths are on the device: the same sequence alone in a cache of 64 slots takes 60 us, in one of its own 52.
 inline int few_workers(long items) { return (int)(items * kGroup < 256 ? 256 : items * kGroup < kPagesWorkers ? items * kGroup : kPagesWorkers); }
 
 __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
@@ -588,17 +590,17 @@ __global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 // all four waves and put into the LDS in the order in which the matrix operands read them (whole lines, no padding), one
 // barrier a tile.  Where there are too few workgroups for the chip, several share a (slot, head, 128 columns), each some
 // of its tiles, and a second launch joins them.
-
 //
-// Measured: 32 heads of a prompt of 8192 tokens 564 us (976 TFLOP/s of the visible pairs; a large library product reaches 1184), the
+// Measured: 32 heads of a prompt of 8192 tokens 561 us (980 TFLOP/s of the visible pairs; a large library product reaches 1184), the
 // matrix cores busy for 46 % of the cycles and the vector units about as long (6 of their instructions a product: widening, exponentials,
-// sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 404 us (616), 9 of their instructions a product.
+// sums), half of it at the same time; 4 x 4096 tokens, 40 heads, a window of 820: 403 us (617), 10 of their instructions a product.
 // Two workgroups are what the registers hold of a compute unit at D = 128, three at 64 (167 registers; 8192 tokens, 32 heads: 351 us, 365 with two);
 // eight waves of 16 columns to a workgroup took 605 us in place of 591, four of 64 columns spilled.
 
 constexpr int kWide = 128, kTile = 64;               // columns and tokens
 // Workgroups that are enough not to split: two to a compute unit.  128 rows over 8192 tokens, 32 heads: 54 us (67 with 256, 46 with
-// 1024, 191 unsplit); 1024 rows: 182 us (247, 195, 246); 64 slots of 71 columns over 8192 tokens: 51 us (67, 49, 137).
+// 1024, 191 unsplit); 1024 rows: 182 us (247, 195, 246); 64 slots of 71 columns over 8192 tokens: 51 us (67, 49, 137).  The host counts a tile for every
+// slot that the cache has: 256 rows of one slot over 8192 tokens, 8 heads, take 35 us in a cache of one slot and, unsplit, 182 in one of 64.
 constexpr int kEnough = 512;
 // Slots of few rows in such a call: their steps are dealt out to this many workgroups behind the others of the launch, where they read memory
 // while the last tiles are multiplied.  32 slots, half of them prompts: 197 us (256 or 768 of them 195 and 196), 211 in front of the
@@ -616,7 +618,7 @@ constexpr int wide_floats(int D) { return kWide * (D + 2); }
 
 // Column tile x of the list over all slots, those of up to 16 columns left out (they are the other kernel's).  Up to 64 slots, and where
 // tiles are not split, every wave has all of them in its lanes, one load deep, and the list has their tiles alone, longest slot first:
-// the last workgroups to begin are short ones, and every die has as many.  Else slot s has its tiles from floor(start[s] G / 128) + s on,
+// the last workgroups to begin are short ones.  Else slot s has its tiles from floor(start[s] G / 128) + s on,
 // which leaves each as many as it can have.  32 slots of 537 to 4096 tokens, 8 heads: 201 us, as the slots are 247; 64 slots of 2048: 204 and
 // 233; 4 slots of 4096: 830 and 816.  Split tiles have a second launch that would do all of this again: 64 slots, 24 us as they are, 30 in order.
 struct Columns { int slot, first, count, len; };     // first column, columns of the slot in all; its tokens
@@ -679,7 +681,9 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   auto keys = tiles_of, values = tiles_of + 2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int G = c.q_per_kv;
-  // each die works through neighbouring items, head by head: what a (slot, head) has cached stays in its L2
+  // Where the workgroups divide by the dies, each die works through neighbouring items, head by head, and what a (slot, head) has cached stays in
+  // its L2: 32 heads of 8192 tokens 555 us, 684 in their order; 32 uneven slots, 8 heads 170 and 200; with 2 or 4 heads, which put long rows on one die
+  // and short ones on another, no slower: 8191 rows, 4 heads of 8 557 and 557, 4095 rows, 2 heads of 16 150 and 150.
   unsigned id = blockIdx.x;
   if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
   const int split = id % (unsigned)splits;

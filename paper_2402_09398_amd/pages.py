@@ -102,6 +102,7 @@ class PagedCache:
         self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)   # (zeros: lessdec.h)
         d.workspace, d.workspace_bytes = self.workspace.data_ptr(), need
         self.desc = d
+        # torch.cuda.current_stream and current_device, by what they call: 0.2 us of a call's 5.6, 1.4 by the public names
         self._pointer, self._lib, self._current = C.pointer(d), lib(), (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
         if buffers is None:
             self.reset()
