@@ -154,6 +154,15 @@ int lessdec_state_reset(const lessdec_desc *desc, void *hip_stream);
 int lessdec_state_sync(const lessdec_desc *desc, void *hip_stream);
 
 /*
+ * Sequences that go on from others (beams, samples of one prompt) and sequences that end: batch row b of all state buffers becomes
+ * what row from[b] was before the call ([batch]; b itself: stays; -1: becomes empty, as after lessdec_state_reset; any other
+ * value outside [0, batch): stays).  In place, a pending fold among the rest; outputs of the steps after it are those of the row
+ * that was copied.  Weights and workspace are not looked at; not to be called between lessdec_step_features and the
+ * lessdec_step_attend that belongs to it.  batch <= LESSDEC_MAX_SLOTS.  from must be none of the state buffers.
+ */
+int lessdec_state_select(const lessdec_desc *desc, const int32_t *from, void *hip_stream);
+
+/*
  * Prompt phase (remark after Eq. 3: with H_0 = z_0 = 0 it is regular attention).
  * Q, K, V: [B,Hh,P,D] dtype, the P prompt tokens of every unit.
  * out:     [B,Hh,P,D] dtype or NULL; causal softmax attention of the prompt.

@@ -20,7 +20,7 @@ FLAG_PROMPT_STEPWISE = 4
 OK, EINVAL, EWORKSPACE, EHIP, ESCRATCH = 0, -1, -2, -3, -4
 STATIC_SCRATCH_BYTES = 4 << 20
 
-EXPORTS = ("lessdec_workspace_bytes", "lessdec_state_reset", "lessdec_state_sync", "lessdec_prefill", "lessdec_step", "lessdec_step_features", "lessdec_step_attend", "lessdec_step_static",
+EXPORTS = ("lessdec_workspace_bytes", "lessdec_state_reset", "lessdec_state_sync", "lessdec_state_select", "lessdec_prefill", "lessdec_step", "lessdec_step_features", "lessdec_step_attend", "lessdec_step_static",
            "lessdec_probe_stream_read", "lessdec_step_launches",
            "lessdec_strerror", "lessdec_budget_tokens",
            "lessdec_pages_workspace_bytes", "lessdec_pages_reset", "lessdec_pages_reserve", "lessdec_pages_select",
@@ -77,6 +77,8 @@ def lib():
         L.lessdec_state_reset.argtypes = [C.POINTER(Desc), C.c_void_p]
         L.lessdec_state_sync.restype = C.c_int
         L.lessdec_state_sync.argtypes = [C.POINTER(Desc), C.c_void_p]
+        L.lessdec_state_select.restype = C.c_int
+        L.lessdec_state_select.argtypes = [C.POINTER(Desc), C.c_void_p, C.c_void_p]
         L.lessdec_prefill.restype = C.c_int
         L.lessdec_prefill.argtypes = [C.POINTER(Desc)] + [C.c_void_p] * 3 + [C.c_int32] + [C.c_void_p] * 2
         L.lessdec_step.restype = C.c_int
@@ -137,6 +139,10 @@ def lessdec_state_reset(desc: Desc, stream=None):
 
 def lessdec_state_sync(desc: Desc, stream=None):
     _check(lib().lessdec_state_sync(C.byref(desc), _stream(stream)), "lessdec_state_sync")
+
+
+def lessdec_state_select(desc: Desc, source, stream=None):
+    _check(lib().lessdec_state_select(C.byref(desc), _p(source), _stream(stream)), "lessdec_state_select")
 
 
 def lessdec_prefill(desc: Desc, Q, K, V, P: int, out=None, stream=None):
@@ -253,6 +259,12 @@ class LessDec:
 
     def state_sync(self, stream=None):
         lessdec_state_sync(self.desc, stream)
+
+    def state_select(self, source, stream=None):
+        """Batch row b becomes a copy of what row source[b] was (int32 [batch]; -1: becomes empty)."""
+        if source.dtype != self.torch.int32 or source.numel() != self.B or not source.is_contiguous() or source.device != self.k_cache.device:
+            raise LessdecError(f"state_select: source must be {self.B} contiguous int32 on {self.k_cache.device}")
+        lessdec_state_select(self.desc, source, stream)
 
     def prefill(self, Q, K, V, out=None, stream=None):
         """K, V: [B*Hh, P, D] (or [B,Hh,P,D]), Q, out: the same with an axis G before P if

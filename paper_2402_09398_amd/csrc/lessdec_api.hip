@@ -89,18 +89,25 @@ Workspace carve(const Shape &s, size_t P, unsigned flags)
   return w;
 }
 
-int check_desc(const lessdec_desc *d, Shape *s, size_t P)
+// shape and state buffers
+int check_state(const lessdec_desc *d, Shape *s)
 {
   if (!shape_ok(d, s)) return LESSDEC_EINVAL;
   if (!d->k_cache || !d->v_cache || !d->acc || !d->pos || !d->psi || !d->H || !d->z || !d->n_seen ||
       !d->pend_slot || !d->pend_v || !d->pend_psi)
     return LESSDEC_EINVAL;
-  if (!d->Wq1 || !d->Wq2 || !d->Wk1 || !d->Wk2 || !d->Wk3) return LESSDEC_EINVAL;
   if (!aligned(d->k_cache, 16) || !aligned(d->v_cache, 16) || !aligned(d->acc, 8) ||
       !aligned(d->z, 8) || !aligned(d->H, 16) || !aligned(d->psi, 16) || !aligned(d->pos, 4) ||
       !aligned(d->n_seen, 4) || !aligned(d->pend_slot, 4) || !aligned(d->pend_v, 16) ||
       !aligned(d->pend_psi, 4))
     return LESSDEC_EINVAL;
+  return LESSDEC_OK;
+}
+
+int check_desc(const lessdec_desc *d, Shape *s, size_t P)
+{
+  if (check_state(d, s)) return LESSDEC_EINVAL;
+  if (!d->Wq1 || !d->Wq2 || !d->Wk1 || !d->Wk2 || !d->Wk3) return LESSDEC_EINVAL;
   if (!aligned(d->Wq1, 16) || !aligned(d->Wq2, 16) || !aligned(d->Wk1, 16) ||
       !aligned(d->Wk2, 16) || !aligned(d->Wk3, d->dtype == LESSDEC_DTYPE_F16 ? 16 : 4))
     return LESSDEC_EINVAL;
@@ -223,6 +230,35 @@ int lessdec_state_sync(const lessdec_desc *desc, void *hip_stream)
   const StepArgs a = state_args(desc, s);
   return launch_state_sync(a, desc->dtype, desc->head_dim, (hipStream_t)hip_stream) == hipSuccess
              ? LESSDEC_OK : LESSDEC_EHIP;
+}
+
+int lessdec_state_select(const lessdec_desc *desc, const int32_t *from, void *hip_stream)
+{
+  Shape s;
+  const int rc = check_state(desc, &s);
+  if (rc) return rc;
+  if (desc->batch > LESSDEC_MAX_SLOTS || !from || !aligned(from, 4)) return LESSDEC_EINVAL;
+  const long Hh = desc->heads, C = (long)s.C, D = (long)s.D, R = (long)s.R, elem = s.f16 ? 2 : 4;
+  SelectArgs a;
+  int n = 0;
+  auto add = [&](void *p, long row_bytes, bool emptied, unsigned empty) {
+    a.array[n++] = SelectArray{static_cast<char *>(p), row_bytes, empty, emptied, aligned(p, 16) && row_bytes % 16 == 0};
+  };
+  // (a row that becomes empty has what lessdec_state_reset gives it)
+  add(desc->k_cache, Hh * C * D * elem, false, 0);
+  add(desc->v_cache, Hh * C * D * elem, false, 0);
+  add(desc->acc, Hh * C * 8, true, 0);
+  add(desc->pos, Hh * C * 4, true, ~0u);
+  add(desc->psi, Hh * C * R * 4, true, 0);
+  add(desc->H, Hh * R * D * 4, true, 0);
+  add(desc->z, Hh * R * 8, true, 0);
+  add(desc->n_seen, Hh * 4, true, 0);
+  add(desc->pend_slot, Hh * 4, true, ~0u);
+  add(desc->pend_v, Hh * D * elem, false, 0);
+  add(desc->pend_psi, Hh * R * 4, false, 0);
+  a.from = from;
+  a.batch = desc->batch;
+  return launch_state_select(a, (hipStream_t)hip_stream) == hipSuccess ? LESSDEC_OK : LESSDEC_EHIP;
 }
 
 }  // extern "C"

@@ -129,6 +129,22 @@ hipError_t launch_fill_empty(float *parts, size_t count, hipStream_t st);
 
 hipError_t launch_reset(const lessdec_desc *d, hipStream_t st);
 
+// Batch rows that become copies of others, in place (lessdec_states.hip).
+struct SelectArray {
+  char *p;
+  long row_bytes;           // a multiple of 4
+  unsigned empty;           // what a row that becomes empty holds, in every word
+  bool emptied;             // whether such a row of this array changes at all
+  bool wide;                // 16-byte aligned in every row
+};
+constexpr int kSelectArrays = 11;
+struct SelectArgs {
+  SelectArray array[kSelectArrays];
+  const int *from;          // [batch]
+  int batch;                // <= LESSDEC_MAX_SLOTS
+};
+hipError_t launch_state_select(const SelectArgs &s, hipStream_t st);
+
 // Digit planes of prompt keys: four bytes an element, a word per tile of 32 keys.  They live between the kernel that writes them
 // and the row pass, so units take turns in a part of the workspace of limited size: 352 MiB hold 0.7 million tokens of
 // D = 128 (a share of the work that fills the chip many times over), and a unit longer than that gets its own size.  Whole prompt
