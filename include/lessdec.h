@@ -402,6 +402,48 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
 int lessdec_pages_read(const lessdec_pages_desc *desc, int32_t layer, const int32_t *slots, int32_t n, int32_t first,
                        int32_t count, void *K, void *V, void *hip_stream);
 
+/*
+ * ---- Beams ------------------------------------------------------------------------------------
+ *
+ * What comes between the logits and the caches of a program that follows several continuations of a prompt at once.  Rows are beams: row
+ * g * beams + b is beam b of prompt g, a batch row of lessdec_desc or a slot of lessdec_pages_desc.  A generation step chooses the next
+ * beams by lessdec_beam_select, whose parents lessdec_state_select and lessdec_pages_select take as they are (with picks = beams).  The conventions
+ * at the top of this file hold here too; everything can be captured in a HIP graph.
+ */
+#define LESSDEC_MAX_BEAMS 64
+#define LESSDEC_MAX_PICKS 64
+
+typedef struct lessdec_beam_desc {
+  int32_t groups, beams;          /* prompts; beams of each <= LESSDEC_MAX_BEAMS; groups * beams <= 2^20 */
+  int32_t vocab;                  /* logits of a row, 1 to 2^28                                */
+  int32_t picks;                  /* chosen for each prompt, 1 to LESSDEC_MAX_PICKS            */
+  int32_t dtype;                  /* LESSDEC_DTYPE_*: the logits                              */
+  int32_t end_token;              /* of an ended beam, below vocab; -1: beams do not end      */
+  void *workspace;                /* >= lessdec_beam_workspace_bytes(), 256-byte aligned.  Scratch, filled with zeros once before its first
+                                     use (its first bytes count workgroups, and every call leaves them 0); it serves calls of one shape,
+                                     which must be ordered by a stream                         */
+  size_t workspace_bytes;
+} lessdec_beam_desc;
+
+/* Bytes of scratch.  Host only; 0 if the shape fields are invalid. */
+size_t lessdec_beam_workspace_bytes(const lessdec_beam_desc *desc);
+
+/*
+ * The `picks` best pairs (b, v) of beam and token of every prompt by
+ *   c = score[r] + (x[r][v] - ln sum_u e^{x[r][u]}),  r = g * beams + b.
+ * logits x: [rows][vocab] dtype, row_stride elements from a row to the next (0: packed; at least vocab), aligned to an element.
+ * score: [rows], the beams' own c.  ended: [rows] or NULL; a beam with a nonzero one offers a single pair instead, end_token at c = score, and its
+ * logits are not read.
+ * parent, token, next_score, next_ended: [groups][picks], the best first: r, v, c, and 1 where v is end_token, else 0 (next_ended may be NULL).
+ * With picks = beams, next_score may be score and next_ended may be ended.
+ * Pairs of one row come in the order of their logits, then of their tokens (the lower first), those of different rows in that of c, then of their
+ * beams.  What has no c above -inf is none: tokens with a logit of -inf, rows with a score of -inf, rows with a NaN among score and logits or with a
+ * logit of +inf.  Where a prompt has fewer than `picks`, the rest get parent -1, token -1, -inf and 0.
+ * c is formed in fp64 (its exponentials to 1.4e-13) and decides; next_score is c rounded once.
+ */
+int lessdec_beam_select(const lessdec_beam_desc *desc, const void *logits, int64_t row_stride, const float *score, const uint8_t *ended,
+                        int32_t *parent, int32_t *token, float *next_score, uint8_t *next_ended, void *hip_stream);
+
 /* Static message for a return code. */
 const char *lessdec_strerror(int code);
 

@@ -24,7 +24,8 @@ EXPORTS = ("lessdec_workspace_bytes", "lessdec_state_reset", "lessdec_state_sync
            "lessdec_probe_stream_read", "lessdec_step_launches",
            "lessdec_strerror", "lessdec_budget_tokens",
            "lessdec_pages_workspace_bytes", "lessdec_pages_reset", "lessdec_pages_reserve", "lessdec_pages_select",
-           "lessdec_pages_compact", "lessdec_pages_copy", "lessdec_pages_append", "lessdec_pages_attend", "lessdec_pages_read")
+           "lessdec_pages_compact", "lessdec_pages_copy", "lessdec_pages_append", "lessdec_pages_attend", "lessdec_pages_read",
+           "lessdec_beam_workspace_bytes", "lessdec_beam_select")
 
 
 class LessdecError(RuntimeError):
@@ -57,6 +58,14 @@ class PagesDesc(C.Structure):
         ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("exps", C.c_void_p),
         ("table", C.c_void_p), ("length", C.c_void_p), ("refs", C.c_void_p),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class BeamDesc(C.Structure):
+    """Mirror of struct lessdec_beam_desc."""
+    _fields_ = [
+        ("groups", C.c_int32), ("beams", C.c_int32), ("vocab", C.c_int32), ("picks", C.c_int32), ("dtype", C.c_int32),
+        ("end_token", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
 
@@ -106,6 +115,10 @@ def lib():
                            ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr])):
             f = getattr(L, "lessdec_pages_" + name)
             f.restype, f.argtypes = C.c_int, [C.POINTER(PagesDesc)] + args
+        L.lessdec_beam_workspace_bytes.restype = C.c_size_t
+        L.lessdec_beam_workspace_bytes.argtypes = [C.POINTER(BeamDesc)]
+        L.lessdec_beam_select.restype = C.c_int
+        L.lessdec_beam_select.argtypes = [C.POINTER(BeamDesc), ptr, C.c_int64] + [ptr] * 7
         _lib = L
     return _lib
 
