@@ -393,6 +393,27 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
                          const int32_t *start, int32_t rows, int32_t max_new, void *hip_stream);
 
 /*
+ * The same attention where slots share pages, as forks do that lessdec_pages_select has made: what neighbouring slots have in common is read and
+ * multiplied once for the rows of all of them, in place of once a slot.
+ *
+ * lessdec_pages_share finds it, once for all layers: runs of neighbouring slots whose table rows begin alike, nested (instructions that
+ * all requests begin with, a request's prompt, its samples), up to three deep; slots with rows in a call, start and rows as
+ * lessdec_pages_attend_shared gets them, and less than 128 query columns (rows * q_per_kv) each.  With `window` pages count as far as a slot sees them.
+ * plan: at least lessdec_pages_share_ints(desc, max_rows >= rows) ints, 16-byte aligned; what is in it is the library's own.  It
+ * holds until table or length change or rows of other sizes are given (a plan made for another number of rows counts as one in which
+ * nothing is shared).  Slots that share want neighbouring indices: what lies apart is read apart.
+ *
+ * lessdec_pages_attend_shared gives what lessdec_pages_attend gives, within the same bounds on its roundings (its sums are joined in another order).
+ * The workspace: lessdec_pages_shared_workspace_bytes(desc, max_rows) bytes.  Nothing shared, or a batch whose slots have
+ * 128 columns or more, costs one launch more than lessdec_pages_attend.
+ */
+size_t lessdec_pages_share_ints(const lessdec_pages_desc *desc, int32_t max_rows);
+size_t lessdec_pages_shared_workspace_bytes(const lessdec_pages_desc *desc, int32_t max_rows);
+int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, int32_t rows, int32_t *plan, void *hip_stream);
+int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t q_stride, void *out, float *lse,
+                                const int32_t *start, int32_t rows, int32_t max_new, const int32_t *plan, void *hip_stream);
+
+/*
  * The values that a layer of the cache holds, e.g. for lessdec_prefill, when a sequence goes over to the compressed cache (an fp16 cache's as they
  * are; lessdec_prefill takes no bfloat16).
  * slots: [n], n <= 65535.  K, V: [n][heads][count][D] dtype, 16-byte aligned: tokens first .. first + count - 1 of

@@ -9,5 +9,5 @@ from .binding import (LessDec, LessdecError, lessdec_budget_tokens, lessdec_pref
                       lessdec_state_reset, lessdec_state_select, lessdec_state_sync, lessdec_step, lessdec_step_attend,
                       lessdec_step_features, lessdec_step_static, lessdec_workspace_bytes, pack_weights)
 from .pages import (PagedCache, lessdec_pages_append, lessdec_pages_attend, lessdec_pages_compact, lessdec_pages_copy,  # noqa: F401
-                    lessdec_pages_read, lessdec_pages_reserve, lessdec_pages_reset, lessdec_pages_select,
-                    lessdec_pages_workspace_bytes)
+                    lessdec_pages_attend_shared, lessdec_pages_read, lessdec_pages_reserve, lessdec_pages_reset, lessdec_pages_select,
+                    lessdec_pages_share, lessdec_pages_share_ints, lessdec_pages_shared_workspace_bytes, lessdec_pages_workspace_bytes)

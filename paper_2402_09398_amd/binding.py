@@ -25,6 +25,7 @@ EXPORTS = ("lessdec_workspace_bytes", "lessdec_state_reset", "lessdec_state_sync
            "lessdec_strerror", "lessdec_budget_tokens",
            "lessdec_pages_workspace_bytes", "lessdec_pages_reset", "lessdec_pages_reserve", "lessdec_pages_select",
            "lessdec_pages_compact", "lessdec_pages_copy", "lessdec_pages_append", "lessdec_pages_attend", "lessdec_pages_read",
+           "lessdec_pages_share_ints", "lessdec_pages_shared_workspace_bytes", "lessdec_pages_share", "lessdec_pages_attend_shared",
            "lessdec_beam_workspace_bytes", "lessdec_beam_select")
 
 
@@ -112,9 +113,13 @@ def lib():
         for name, args in (("reset", [ptr]), ("reserve", [ptr] * 4), ("select", [ptr] * 2), ("compact", [ptr] * 2),
                            ("copy", [ptr, i32, ptr]), ("append", [i32, ptr, ptr, C.c_int64, ptr, i32, ptr]),
                            ("attend", [i32, ptr, C.c_int64, ptr, ptr, ptr, i32, i32, ptr]),
-                           ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr])):
+                           ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr]), ("share", [ptr, i32, ptr, ptr]),
+                           ("attend_shared", [i32, ptr, C.c_int64, ptr, ptr, ptr, i32, i32, ptr, ptr])):
             f = getattr(L, "lessdec_pages_" + name)
             f.restype, f.argtypes = C.c_int, [C.POINTER(PagesDesc)] + args
+        for name in ("share_ints", "shared_workspace_bytes"):
+            f = getattr(L, "lessdec_pages_" + name)
+            f.restype, f.argtypes = C.c_size_t, [C.POINTER(PagesDesc), i32]
         L.lessdec_beam_workspace_bytes.restype = C.c_size_t
         L.lessdec_beam_workspace_bytes.argtypes = [C.POINTER(BeamDesc)]
         L.lessdec_beam_select.restype = C.c_int

@@ -111,6 +111,59 @@ struct AttendArgs {
 };
 constexpr int kPagesWorkers = 768;                   // workgroups of the kernel of few rows: three to a compute unit
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
+
+// What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
+//  head  [8]: nodes, items, columns in all, rows that it was made for
+//  slot  [slots][2]: the node that its row begins with (-1: none), the first block that is its own
+//  node  [slots][kNodeInts]: slot whose table row to read, first row, rows, least and largest position of them, blocks [first, last), first column,
+//        node before it (-1: none), splits.  A node has splits times (rows * q_per_kv) columns
+//  pos   [rows]: positions of the rows
+//  item  [items][4]: node, tile of 128 columns | split << 16, tiles [from, to) of the node's blocks
+//  apart [kAgreeWorkers][slots]: scratch
+// A (head, column) of the plan has a sum of D floats, a maximum and a total in the workspace.
+constexpr int kPlanNodes = 0, kPlanItems = 1, kPlanColumns = 2, kPlanRows = 3, kPlanHead = 8, kNodeInts = 12, kAgreeWorkers = 64;
+constexpr int kTrunkWorkers = 512, kTrunkDepth = 3, kTrunkTile = 128;  // workgroups of the nodes; nodes on a slot's way; columns of a tile
+struct Plan {
+  int *head, *slot, *node, *pos, *item, *apart;
+};
+// Slots of up to 127 query columns share; a row is in kTrunkDepth nodes at most, a level has half as many nodes as slots.
+inline long shared_columns(int slots, int q_per_kv, long rows)
+{
+  const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
+  return n < most ? n : most;
+}
+inline long plan_items(int slots, int heads, int q_per_kv, long rows)
+{
+  return kTrunkDepth * (shared_columns(slots, q_per_kv, rows) / kTrunkTile + slots / 2 + 1) + kTrunkWorkers / heads + 1;
+}
+inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
+{
+  return kTrunkDepth * shared_columns(slots, q_per_kv, rows) + (long)kTrunkTile * (kTrunkWorkers / heads + 1);
+}
+inline long plan_ints(int slots, int heads, int q_per_kv, long rows)
+{
+  return kPlanHead + 4 * plan_items(slots, heads, q_per_kv, rows) + (long)slots * (2 + kNodeInts + kAgreeWorkers) + rows;
+}
+inline Plan plan_at(int *p, int slots, int heads, int q_per_kv, long rows)
+{
+  Plan x;
+  x.head = p;
+  x.item = x.head + kPlanHead;                       // (16-byte aligned, as the nodes are)
+  x.node = x.item + 4 * plan_items(slots, heads, q_per_kv, rows);
+  x.slot = x.node + (long)slots * kNodeInts;
+  x.apart = x.slot + 2L * slots;
+  x.pos = x.apart + (long)slots * kAgreeWorkers;
+  return x;
+}
+struct SharedArgs : AttendArgs {
+  Plan plan;
+  float *trunk;                                      // [heads][columns][D] sums, [heads][columns] maxima, [heads][columns] totals
+  long columns;
+  int items;                                         // that the plan has room for
+};
+hipError_t launch_pages_attend_shared(const Pages &c, int dtype, const SharedArgs &a, hipStream_t st);
+hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, int items, long columns, hipStream_t st);
+
 // floats of AttendArgs::parts for up to `rows` rows
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows);
 

@@ -38,6 +38,20 @@ size_t workspace_for(const lessdec_pages_desc *d, int rows)
   return kCounterBytes + (n + 255) / 256 * 256;
 }
 
+// .. and behind the shares of lessdec_pages_attend the sums of a plan's nodes
+size_t trunk_floats(const lessdec_pages_desc *d, int rows)
+{
+  const int G = d->q_per_kv > 1 ? d->q_per_kv : 1;
+  return (size_t)d->heads * plan_columns(d->slots, d->heads, G, rows) * (d->head_dim + 2);
+}
+size_t own_bytes(const lessdec_pages_desc *d, int rows) { return (floats_for(d, rows) * sizeof(float) + 255) / 256 * 256; }
+size_t shared_workspace_for(const lessdec_pages_desc *d, int rows)
+{
+  if (rows == 0) return workspace_for(d, 0);
+  const size_t n = kCounterBytes + own_bytes(d, rows) + (trunk_floats(d, rows) * sizeof(float) + 255) / 256 * 256, least = workspace_for(d, rows);
+  return n > least ? n : least;
+}
+
 enum Needs { kTables = 1, kPool = 2, kWork = 4 };
 
 // rows: of lessdec_pages_attend
@@ -72,6 +86,12 @@ long row_stride(int64_t stride, long packed)
 {
   if (stride == 0) return packed;
   return stride < packed || stride % 8 || stride > (int64_t)1 << 40 ? -1 : (long)stride;
+}
+
+// rows of an attention call
+bool rows_ok(const Pages &c, int rows)
+{
+  return rows >= 0 && (long)rows * c.q_per_kv < 1L << 31 && ((long)rows * c.q_per_kv / 128 + c.slots) * c.heads <= 1L << 30;
 }
 
 }  // namespace
@@ -140,6 +160,50 @@ int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const vo
   return result(launch_pages_append(c, desc->dtype, AppendArgs{k, v, step, start, rows}, (hipStream_t)hip_stream));
 }
 
+size_t lessdec_pages_share_ints(const lessdec_pages_desc *desc, int32_t max_rows)
+{
+  if (!shape_ok(desc) || max_rows < 0) return 0;
+  return (size_t)plan_ints(desc->slots, desc->heads, desc->q_per_kv > 1 ? desc->q_per_kv : 1, max_rows);
+}
+
+size_t lessdec_pages_shared_workspace_bytes(const lessdec_pages_desc *desc, int32_t max_rows)
+{
+  return !shape_ok(desc) || max_rows < 0 ? 0 : shared_workspace_for(desc, max_rows);
+}
+
+int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, int32_t rows, int32_t *plan, void *hip_stream)
+{
+  Pages c;
+  const int rc = check(desc, 0, 0, 0, &c);
+  if (rc) return rc;
+  if (!rows_ok(c, rows)) return LESSDEC_EINVAL;
+  if (rows == 0) return LESSDEC_OK;
+  if (!start || !plan || !aligned(start, 4) || !aligned(plan, 16) || plan == start || plan == desc->table || plan == desc->length) return LESSDEC_EINVAL;
+  return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots, c.heads, c.q_per_kv, rows), (int)plan_items(c.slots, c.heads, c.q_per_kv, rows),
+                                   plan_columns(c.slots, c.heads, c.q_per_kv, rows), (hipStream_t)hip_stream));
+}
+
+int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t stride, void *out, float *lse, const int32_t *start,
+                                int32_t rows, int32_t max_new, const int32_t *plan, void *hip_stream)
+{
+  Pages c;
+  const int rc = check(desc, kPool, 0, layer, &c);
+  if (rc) return rc;
+  const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
+  if (step < 0 || max_new < 0 || !rows_ok(c, rows)) return LESSDEC_EINVAL;
+  if (rows == 0 || max_new == 0) return LESSDEC_OK;
+  if (!desc->workspace || !aligned(desc->workspace, 256) || desc->workspace_bytes < shared_workspace_for(desc, rows)) return LESSDEC_EWORKSPACE;
+  if (!q || !out || !start || !plan || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4) || !aligned(plan, 16)) return LESSDEC_EINVAL;
+  SharedArgs a;
+  static_cast<AttendArgs &>(a) = AttendArgs{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<int *>(desc->workspace),
+                                            static_cast<float *>(scratch(desc))};
+  a.plan = plan_at(const_cast<int32_t *>(plan), c.slots, c.heads, c.q_per_kv, rows);
+  a.trunk = reinterpret_cast<float *>(static_cast<char *>(scratch(desc)) + own_bytes(desc, rows));
+  a.columns = plan_columns(c.slots, c.heads, c.q_per_kv, rows);
+  a.items = (int)plan_items(c.slots, c.heads, c.q_per_kv, rows);
+  return result(launch_pages_attend_shared(c, desc->dtype, a, (hipStream_t)hip_stream));
+}
+
 int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t stride, void *out, float *lse, const int32_t *start,
                          int32_t rows, int32_t max_new, void *hip_stream)
 {
@@ -147,7 +211,7 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
   int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
-  if (step < 0 || rows < 0 || max_new < 0 || (long)rows * c.q_per_kv >= 1L << 31 || ((long)rows * c.q_per_kv / 128 + desc->slots) * desc->heads > 1L << 30) return LESSDEC_EINVAL;
+  if (step < 0 || max_new < 0 || !rows_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0 || max_new == 0) return LESSDEC_OK;
   rc = check(desc, kWork, rows, layer, &c);
   if (rc) return rc;

@@ -134,11 +134,22 @@ struct Top {
 // The blocks of 16 tokens that rows at positions lo .. hi see some token of, as a list: the first ones, then those of the window.
 struct Span {
   int sinks, window, count;                          // blocks of the first tokens; the window's first block; blocks in all
-  __device__ inline int block(int i) const { return i < sinks ? i : i - sinks + window; }
+  int skip;                                          // blocks before the list's first, where it is cut
+  __device__ inline int block(int i) const
+  {
+    i += skip;
+    return i < sinks ? i : i - sinks + window;
+  }
+  __device__ inline int place(int block) const { return min(block, sinks) + max(block - window, 0); }       // blocks of the list (uncut) before this one
+  __device__ inline void cut(int first, int last)    // to blocks first .. last - 1
+  {
+    skip = min(place(first), count);
+    count = max(min(place(last), count) - skip, 0);
+  }
 };
 __device__ inline Span span_of(const Pages &c, int lo, int hi)
 {
-  Span s = {0, 0, 0};
+  Span s = {0, 0, 0, 0};
   if (hi < 0) return s;
   const int last = hi / kBlock;
   if (c.window > 0 && lo >= c.window) {
@@ -164,10 +175,63 @@ __device__ inline int inner_first(const Pages &c, const Span &s, int hi)
 {
   if (c.window == 0 || hi < c.window) return 0;
   const int block = (hi - c.window + kBlock) / kBlock;                 // the first whose tokens are all > hi - window
-  return (max(block - s.window, 0) + s.sinks + 3) / 4;
+  return (max(max(block - s.window, 0) + s.sinks - s.skip, 0) + 3) / 4;
 }
-__device__ inline int inner_last(const Span &s, int lo) { return max((lo + 1) / kBlock - s.window + s.sinks, 0) / 4; }
+__device__ inline int inner_last(const Span &s, int lo) { return max((lo + 1) / kBlock - s.window + s.sinks - s.skip, 0) / 4; }
 __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+
+// ---- slots that share pages --------------------------------------------------------------------------------------------
+//
+// What neighbouring slots have in common (a node of the plan) is gone through once, for the rows of all of them, by wide_kernel's work in a launch of
+// its own; the kernels of the slots begin behind it and take its sums in where they finish a row.  A sum lies at [head][column of the plan].
+template <typename Args> constexpr bool kShares = false;
+template <> constexpr bool kShares<SharedArgs> = true;
+
+// a slot's node (-1: none) and the first block of its own
+template <typename Args> __device__ inline int2 own_of(const Args &a, int s)
+{
+  if constexpr (kShares<Args>) {
+    const int2 x = reinterpret_cast<const int2 *>(a.plan.slot)[s];
+    return a.plan.head[kPlanRows] == a.rows ? make_int2(x.x, max(x.y, 0)) : make_int2(-1, 0);
+  }
+  return make_int2(-1, 0);
+}
+template <typename Args> __device__ inline void cut_own(const Args &a, int s, Span &span)
+{
+  if constexpr (kShares<Args>) span.cut(own_of(a, s).y, 1 << 30);
+}
+struct Node {
+  int slot, row, rows, lo, hi, first, last, base, parent, splits;      // last: the block behind its last one; base: its first column of the plan
+  int cols;
+};
+__device__ inline Node node_of(const Pages &c, const SharedArgs &a, int i)
+{
+  const int *f = a.plan.node + (long)i * kNodeInts;
+  Node n;
+  n.slot = min(max(f[0], 0), c.slots - 1);
+  n.row = min(max(f[1], 0), a.rows);
+  n.rows = min(max(f[2], 0), a.rows - n.row);
+  n.lo = f[3]; n.hi = f[4]; n.first = f[5]; n.last = f[6];
+  n.base = max(f[7], 0);
+  n.parent = f[8];
+  n.splits = max(f[9], 0);
+  n.cols = n.rows * c.q_per_kv;
+  return n;
+}
+// Calls take(index of the first share, from one to the next, how many) for every node that a slot's column belongs to, the nearest first.
+template <typename Take> __device__ inline void each_trunk(const Pages &c, const SharedArgs &a, int node, int row, int g, Take take)
+{
+  int upto = INT_MAX;
+  while ((unsigned)node < (unsigned)c.slots) {
+    const Node n = node_of(c, a, node);
+    const int col = (row - n.row) * c.q_per_kv + g;
+    // (a plan has its nodes end ever earlier, and its shares in their place; nothing else is followed)
+    if (n.last >= upto || (unsigned)col >= (unsigned)n.cols || (long)n.base + (long)n.splits * n.cols > a.columns) return;
+    upto = n.last;
+    take((long)n.base + col, (long)n.cols, n.splits);
+    node = n.parent;
+  }
+}
 
 // ---- few rows a slot: up to 16 query columns -----------------------------------------------------------------------------
 //
@@ -188,12 +252,14 @@ constexpr int kGroup = 32;
 // has, as lengths are on the device: the same sequence alone in a cache of 64 slots takes 60 us, in one of its own 52.
 inline int few_workers(long items) { return (int)(items * kGroup < 256 ? 256 : items * kGroup < kPagesWorkers ? items * kGroup : kPagesWorkers); }
 
-__device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
+template <typename Args> __device__ inline int steps_of(const Pages &c, const Args &a, int s)
 {
   const Rows r = slot_rows(a.start, s, a.rows);
   if (r.count == 0 || r.count * c.q_per_kv > kCols) return 0;
   const int len = slot_length(c, s);
-  const int n = (span_of(c, len - r.count, len - 1).count + kStepBlocks - 1) / kStepBlocks;
+  Span span = span_of(c, len - r.count, len - 1);
+  cut_own(a, s, span);
+  const int n = (span.count + kStepBlocks - 1) / kStepBlocks;
   return n > 0 ? n : 1;                              // (rows that see nothing are written too)
 }
 
@@ -203,7 +269,7 @@ struct Part {
   int slot;
   long in_slot;
 };
-__device__ inline Part part_of(const Pages &c, const AttendArgs &a, int w, int workers)
+template <typename Args> __device__ inline Part part_of(const Pages &c, const Args &a, int w, int workers)
 {
   __shared__ long sums[4], found_at;
   __shared__ int found;
@@ -326,11 +392,45 @@ __device__ inline void join(int n, int cols, Share share, Done done)
   }
 }
 
+// The sums of a slot's nodes at a column and two channels, added to its own.
+template <int D>
+__device__ inline void add_trunks(const Pages &c, const SharedArgs &a, int node, int head, int row, int g, int d, float &x, float &y, float &top, float &l)
+{
+  const float *sums = a.trunk + head * a.columns * D + d, *tops = a.trunk + c.heads * a.columns * D + head * a.columns, *totals = tops + c.heads * a.columns;
+  each_trunk(c, a, node, row, g, [&](long first, long step, int shares) {
+    for (int k = 0; k < shares; k += 8) {            // eight at a time on their way
+      float m[8], u[8];
+      float2 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const long at = first + min(k + j, shares - 1) * step;
+        m[j] = k + j < shares ? tops[at] : -__builtin_inff();
+        u[j] = totals[at];
+        v[j] = *reinterpret_cast<const float2 *>(sums + at * D);
+      }
+      float now = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) now = fmaxf(now, m[j]);
+      const float less = exp2_fast(top - now);
+      top = now;
+      l *= less; x *= less; y *= less;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (m[j] == -__builtin_inff()) continue;     // no tiles, nothing written
+        const float e = exp2_fast(m[j] - top);
+        l = fmaf(u[j], e, l);
+        x = fmaf(v[j].x, e, x);
+        y = fmaf(v[j].y, e, y);
+      }
+    }
+  });
+}
+
 template <int D> struct FewShared {
   float sums[4][kCols][D + 4], tops[4][kCols], totals[4][kCols];
 };
-template <bool BF16, int D>
-__device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, int worker, int workers, FewShared<D> &shared)
+template <bool BF16, int D, typename Args>
+__device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int worker, int workers, FewShared<D> &shared)
 {
   constexpr int H = D / 64, T = D / 16;
   auto &sums = shared.sums;
@@ -350,7 +450,9 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
 
     const Rows rows = slot_rows(a.start, s, a.rows);
     const int len = slot_length(c, s), lo = len - rows.count, hi = len - 1, cols = rows.count * G;
-    const Span span = span_of(c, lo, hi);
+    Span span = span_of(c, lo, hi);
+    cut_own(a, s, span);
+    const int node = own_of(a, s).x;
     const int p = lo + n / G;
     u4 q[H][2];
 #pragma unroll
@@ -515,6 +617,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
       for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
     __syncthreads();
     auto finish = [&](int col, int d, float x, float y, float m, float l) {
+      if constexpr (kShares<Args>) add_trunks<D>(c, a, node, head, rows.first + col / G, col % G, d, x, y, m, l);
       const float r = 1.f / l;
       const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
       reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
@@ -576,8 +679,8 @@ __device__ __forceinline__ void few_rows(const Pages &c, const AttendArgs &a, in
   }
 }
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
+template <bool BF16, int D, typename Args>
+__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, Args a)
 {
   __shared__ FewShared<D> shared;
   few_rows<BF16, D>(c, a, blockIdx.x, gridDim.x, shared);
@@ -666,47 +769,81 @@ __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bo
   return true;
 }
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, unsigned items, int splits)
+template <int D> struct WideShared {
+  __align__(16) u4 tiles[4][kTile * D / 8];
+  int spoiled, lo[4], hi[4];
+};
+
+// Item `id` of a launch.  kTrunk: of the plan's list, columns of all slots of a node; else of the slots' own.
+template <bool BF16, int D, bool kTrunk, typename Args>
+__device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigned id, unsigned items, int splits, WideShared<D> &shared)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
-  __shared__ __align__(16) u4 tiles_of[4][kTile * D / 8];
-  __shared__ int spoiled;
-  const unsigned total = items * c.heads * splits;
-  if (blockIdx.x >= total) {
-    static_assert(sizeof(FewShared<D>) <= sizeof tiles_of, "the slots of few rows work in the same LDS");
-    few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(tiles_of));
-    return;
-  }
-  auto keys = tiles_of, values = tiles_of + 2;
+  auto &spoiled = shared.spoiled;
+  auto keys = shared.tiles, values = shared.tiles + 2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int G = c.q_per_kv;
-  // Where the workgroups divide by the dies, each die works through neighbouring items, head by head, and what a (slot, head) has cached stays in
-  // its L2: 32 heads of 8192 tokens 555 us, 684 in their order; 32 uneven slots, 8 heads 170 and 200; with 2 or 4 heads, which put long rows on one die
-  // and short ones on another, no slower: 8191 rows, 4 heads of 8 557 and 557, 4095 rows, 2 heads of 16 150 and 150.
-  unsigned id = blockIdx.x;
-  if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
   const int split = id % (unsigned)splits;
   const unsigned item = id / (unsigned)splits;
   const int head = item / items;
   Columns t;
   Rows rows;
-  if (!columns_of(c, a, item % items, splits == 1 && c.slots <= kWave, t, rows)) return;
-  const int len = t.len, before = len - rows.count;
+  Span span;
+  Node trunk;
+  int node = -1, piece = 0, from, to, lo, hi, wave_lo, wave_hi, p;
+  if constexpr (kTrunk) {
+    const int4 f = reinterpret_cast<const int4 *>(a.plan.item)[item % items];
+    if ((unsigned)f.x >= (unsigned)c.slots) return;
+    trunk = node_of(c, a, f.x);
+    t = Columns{trunk.slot, f.y & 0xffff, trunk.cols, 0};
+    t.first *= kWide;
+    piece = (int)((unsigned)f.y >> 16);
+    if (t.first >= t.count || piece >= trunk.splits || (long)trunk.base + (long)trunk.splits * trunk.cols > a.columns) return;
+    rows = Rows{trunk.row, trunk.rows};
+    const int most = c.table_len * c.page_tokens;
+    span = span_of(c, min(max(trunk.lo, 0), most - 1), min(max(trunk.hi, 0), most - 1));
+    span.cut(max(trunk.first, 0), min(max(trunk.last, 0), c.table_len * page_blocks(c)));
+    from = max(f.z, 0);
+    to = min((span.count + 3) / 4, f.w);
+  } else {
+    if (!columns_of(c, a, item % items, splits == 1 && c.slots <= kWave, t, rows)) return;
+  }
+  const int before = t.len - rows.count;
   const int last_col = min(t.first + kWide, t.count) - 1;
-  const int lo = before + t.first / G, hi = before + last_col / G;
-  const Span span = span_of(c, lo, hi);
-  const int tiles = (span.count + 3) / 4, each = max(2, (tiles + splits - 1) / splits);
-  const int from = split * each, to = min(tiles, from + each);
-
   // this wave's columns
   const int col = t.first + wave * 32 + n;
-  const int wave_last = min(t.first + wave * 32 + 31, last_col);
-  const int wave_lo = before + (t.first + wave * 32) / G, wave_hi = before + wave_last / G;
   const bool have = t.first + wave * 32 <= last_col;
   const int row = rows.first + col / G, q_head = head * G + col % G;
-  // the row, at p, sees the tokens from_token .. p and those before first_tokens
-  const int p = col <= last_col ? before + col / G : -1;
+  if constexpr (kTrunk) {
+    // rows of several slots: their positions as the plan has them, in any order
+    p = col <= last_col ? min(max(a.plan.pos[row], -1), c.table_len * c.page_tokens - 1) : -1;
+    wave_lo = col <= last_col ? p : 1 << 30;
+    wave_hi = p;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      wave_lo = min(wave_lo, __shfl_xor(wave_lo, d, kWave));
+      wave_hi = max(wave_hi, __shfl_xor(wave_hi, d, kWave));
+    }
+    wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
+    wave_hi = __builtin_amdgcn_readfirstlane(wave_hi);
+    if (lane == 0) { shared.lo[wave] = wave_lo; shared.hi[wave] = wave_hi; }
+    __syncthreads();
+    lo = min(min(shared.lo[0], shared.lo[1]), min(shared.lo[2], shared.lo[3]));
+    hi = max(max(shared.hi[0], shared.hi[1]), max(shared.hi[2], shared.hi[3]));
+  } else {
+    lo = before + t.first / G;
+    hi = before + last_col / G;
+    span = span_of(c, lo, hi);
+    cut_own(a, t.slot, span);
+    node = own_of(a, t.slot).x;
+    const int tiles = (span.count + 3) / 4, each = max(2, (tiles + splits - 1) / splits);
+    from = split * each;
+    to = min(tiles, from + each);
+    wave_lo = before + (t.first + wave * 32) / G;
+    wave_hi = before + min(t.first + wave * 32 + 31, last_col) / G;
+    // the row, at p, sees the tokens from_token .. p and those before first_tokens
+    p = col <= last_col ? before + col / G : -1;
+  }
   const int from_token = c.window > 0 ? max(max(p, 0) - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
   u4 q[KK];
 #pragma unroll
@@ -719,6 +856,10 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   // slot is missing (which the look-ups below find before such a tile is reached).
   const int all_first = inner_first(c, span, hi), mine_first = inner_first(c, span, wave_hi);
   int all_last = inner_last(span, lo), mine_last = inner_last(span, wave_lo);
+  if constexpr (kTrunk) {                            // (a list that ends before the rows do)
+    all_last = min(all_last, span.count / 4);
+    mine_last = min(mine_last, span.count / 4);
+  }
 
   // Blocks are looked up for sixteen tiles at a time, a lane each: the table a chunk ahead, the exponents half a chunk ahead.
   constexpr int kChunk = kWave / 4;
@@ -1021,6 +1162,24 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     }
 
   sum += __shfl_xor(sum, 32, kWave);
+  if constexpr (kTrunk) {
+    if (col > last_col) return;
+    const long at = head * a.columns + trunk.base + (long)piece * trunk.cols + col;
+    const float unit_of_e = top.unit();
+    if (from < to)
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f4 *>(a.trunk + at * D + o * 32 + i * 8 + h * 4) =
+              f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]} * unit_of_e;
+    if (h == 0) {
+      float *tops = a.trunk + c.heads * a.columns * D;
+      tops[at] = from < to ? top.s : -__builtin_inff();
+      tops[c.heads * a.columns + at] = sum * unit_of_e;
+    }
+    return;
+  }
   if (splits > 1) {
     float *share = a.parts + few_floats(G, D) + (long)id * wide_floats(D);
     const int mine = wave * 32 + n;
@@ -1036,6 +1195,28 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
     return;
   }
   if (col > last_col) return;
+  if constexpr (kShares<Args> && !kTrunk) {
+    const float *sums = a.trunk + head * a.columns * D, *tops = a.trunk + c.heads * a.columns * D + head * a.columns, *totals = tops + c.heads * a.columns;
+    each_trunk(c, a, node, row, col % G, [&](long first, long step, int shares) {
+#pragma unroll 1
+      for (int k = 0; k < shares; ++k) {
+        const long at = first + k * step;
+        const float m = tops[at];
+        if (m == -__builtin_inff()) continue;
+        const float now = fmaxf(top.s, m), less = exp2_fast(top.s - now) * top.unit(), e = exp2_fast(m - now);
+        top = Top{now, 0.f};
+        sum = fmaf(totals[at], e, sum * less);
+#pragma unroll
+        for (int o = 0; o < OB; ++o)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f4 v = *reinterpret_cast<const f4 *>(sums + at * D + o * 32 + i * 8 + h * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[o][4 * i + j] = fmaf(v[j], e, acc[o][4 * i + j] * less);
+          }
+      }
+    });
+  }
   const float r = 1.f / sum;
   const long to_row = (long)row * c.heads * G + q_head;
 #pragma unroll
@@ -1049,10 +1230,43 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, AttendArgs a, uns
   if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top.s + (top.e + __builtin_log2f(sum))) * 0.6931471805599453f;
 }
 
+template <bool BF16, int D, typename Args>
+__global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned items, int splits)
+{
+  __shared__ WideShared<D> shared;
+  const unsigned total = items * c.heads * splits;
+  if (blockIdx.x >= total) {
+    static_assert(sizeof(FewShared<D>) <= sizeof shared.tiles, "the slots of few rows work in the same LDS");
+    few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(shared.tiles));
+    return;
+  }
+  // Where the workgroups divide by the dies, each die works through neighbouring items, head by head, and what a (slot, head) has cached stays in
+  // its L2: 32 heads of 8192 tokens 555 us, 684 in their order; 32 uneven slots, 8 heads 170 and 200; with 2 or 4 heads, which put long rows on one die
+  // and short ones on another, no slower: 8191 rows, 4 heads of 8 557 and 557, 4095 rows, 2 heads of 16 150 and 150.
+  unsigned id = blockIdx.x;
+  if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
+  wide_item<BF16, D, false>(c, a, id, items, splits, shared);
+}
+
+// The nodes' sums.  As many workgroups as the chip holds at once; how many items there are is known on the device alone.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 2) void trunk_kernel(Pages c, SharedArgs a)
+{
+  __shared__ WideShared<D> shared;
+  if (a.plan.head[kPlanRows] != a.rows) return;
+  const unsigned items = (unsigned)min(max(a.plan.head[kPlanItems], 0), a.items), total = items * c.heads;
+  for (unsigned at = blockIdx.x; at < total; at += gridDim.x) {
+    unsigned id = at;
+    if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
+    wide_item<BF16, D, true>(c, a, id, items, 1, shared);
+    __syncthreads();
+  }
+}
+
 // Eight columns of an item to a workgroup, eight shares on their way at a time.
 constexpr int kJoinColumns = 8;
-template <bool BF16, int D>
-__global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, unsigned items, int splits)
+template <bool BF16, int D, typename Args>
+__global__ __launch_bounds__(256) void wide_join_kernel(Pages c, Args a, unsigned items, int splits)
 {
   const int G = c.q_per_kv;
   const unsigned item = blockIdx.x;
@@ -1090,6 +1304,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
         y = fmaf(v[j].y, e, y);
       }
     }
+    if constexpr (kShares<Args>) add_trunks<D>(c, a, own_of(a, t.slot).x, head, rows.first + col / G, col % G, d, x, y, top, l);
     const float r = 1.f / l;
     const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
     reinterpret_cast<unsigned *>(a.out)[to * (D / 2) + d / 2] =
@@ -1098,19 +1313,20 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, AttendArgs a, u
   }
 }
 
-template <bool BF16, int D>
-hipError_t attend(const Pages &c, const AttendArgs &a, hipStream_t st)
+template <bool BF16, int D, typename Args>
+hipError_t attend(const Pages &c, const Args &a, hipStream_t st)
 {
   const long pairs = (long)c.slots * c.heads;
+  if constexpr (kShares<Args>) trunk_kernel<BF16, D><<<kTrunkWorkers, 256, 0, st>>>(c, a);
   if ((long)a.max_new * c.q_per_kv <= kCols) {
-    few_kernel<BF16, D><<<few_workers(pairs), 256, 0, st>>>(c, a);
+    few_kernel<BF16, D, Args><<<few_workers(pairs), 256, 0, st>>>(c, a);
     return hipGetLastError();
   }
   const long items = wide_items(c.slots, c.q_per_kv, a.rows);
   const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
   const int few = c.q_per_kv <= kCols ? min(few_workers(pairs), kFewBeside) : 0;
-  wide_kernel<BF16, D><<<(unsigned)(items * c.heads * splits + few), 256, 0, st>>>(c, a, (unsigned)items, splits);
-  if (splits > 1) wide_join_kernel<BF16, D><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
+  wide_kernel<BF16, D, Args><<<(unsigned)(items * c.heads * splits + few), 256, 0, st>>>(c, a, (unsigned)items, splits);
+  if (splits > 1) wide_join_kernel<BF16, D, Args><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
   return hipGetLastError();
 }
 
@@ -1131,11 +1347,13 @@ size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, lon
   return n;
 }
 
-hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st)
+template <typename Args> static hipError_t attend_any(const Pages &c, int dtype, const Args &a, hipStream_t st)
 {
   const bool bf16 = dtype == LESSDEC_DTYPE_BF16;
   if (c.head_dim == 128) return bf16 ? attend<true, 128>(c, a, st) : attend<false, 128>(c, a, st);
   return bf16 ? attend<true, 64>(c, a, st) : attend<false, 64>(c, a, st);
 }
+hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st) { return attend_any(c, dtype, a, st); }
+hipError_t launch_pages_attend_shared(const Pages &c, int dtype, const SharedArgs &a, hipStream_t st) { return attend_any(c, dtype, a, st); }
 
 }  // namespace lessdec

@@ -45,6 +45,23 @@ def lessdec_pages_attend(desc: PagesDesc, layer: int, q, q_stride: int, out, lse
            "lessdec_pages_attend")
 
 
+def lessdec_pages_share_ints(desc: PagesDesc, max_rows: int) -> int:
+    return int(lib().lessdec_pages_share_ints(C.byref(desc), int(max_rows)))
+
+
+def lessdec_pages_shared_workspace_bytes(desc: PagesDesc, max_rows: int) -> int:
+    return int(lib().lessdec_pages_shared_workspace_bytes(C.byref(desc), int(max_rows)))
+
+
+def lessdec_pages_share(desc: PagesDesc, start, rows: int, plan, stream=None):
+    _check(lib().lessdec_pages_share(C.byref(desc), _p(start), rows, _p(plan), _stream(stream)), "lessdec_pages_share")
+
+
+def lessdec_pages_attend_shared(desc: PagesDesc, layer: int, q, q_stride: int, out, lse, start, rows: int, max_new: int, plan, stream=None):
+    _check(lib().lessdec_pages_attend_shared(C.byref(desc), layer, _p(q), q_stride, _p(out), _p(lse), _p(start), rows, max_new, _p(plan),
+                                             _stream(stream)), "lessdec_pages_attend_shared")
+
+
 def lessdec_pages_read(desc: PagesDesc, layer: int, slots, n: int, first: int, count: int, K, V, stream=None):
     _check(lib().lessdec_pages_read(C.byref(desc), layer, _p(slots), n, first, count, _p(K), _p(V), _stream(stream)),
            "lessdec_pages_read")
@@ -54,7 +71,7 @@ class PagedCache:
     """Owns the device buffers of a paged cache (or takes a program's own, `buffers`) and its descriptor.
 
     Plumbing only: allocation with torch, checks of tensors, pointer marshalling, no arithmetic.  dtype: "f16" or "bf16", of the
-    rows that go in and come out.  max_rows: the most rows that an attend() gets in one call.  Calls run on the cache's device,
+    rows that go in and come out.  max_rows: the most rows that an attend() gets in one call.  shared: whether there is scratch for attend_shared(), too.  Calls run on the cache's device,
     on its current stream if none is given.
     """
 
@@ -62,7 +79,7 @@ class PagedCache:
     STATE = ("k_codes", "v_codes", "exps", "table", "length", "refs")
 
     def __init__(self, slots, pages, page_tokens, table_len, heads, head_dim, dtype, layers=1, q_per_kv=1, sinks=0, window=0,
-                 scale=0.0, max_rows=0, device="cuda:0", buffers=None):
+                 scale=0.0, max_rows=0, device="cuda:0", buffers=None, shared=False):
         import torch
         if not torch.cuda.is_available():
             raise LessdecError("no GPU visible: lessdec has no CPU path")
@@ -81,7 +98,8 @@ class PagedCache:
         d.heads, d.head_dim, d.q_per_kv, d.layers = heads, head_dim, q_per_kv, layers
         d.dtype = DTYPE_F16 if dtype == "f16" else DTYPE_BF16
         d.sinks, d.window, d.scale = sinks, window, scale
-        need = lessdec_pages_workspace_bytes(d, max_rows)
+        self.shared = shared
+        need = lessdec_pages_shared_workspace_bytes(d, max_rows) if shared else lessdec_pages_workspace_bytes(d, max_rows)
         if need == 0:
             raise LessdecError("lessdec_pages_workspace_bytes: invalid shape")
         blocks = layers * pages * heads * (page_tokens // BLOCK)
@@ -165,6 +183,10 @@ class PagedCache:
     def attend(self, layer, q, out, start, max_new, lse=None, stream=None):
         """q [rows, heads * q_per_kv, D] of the slots' last tokens, at most max_new of a slot; out the same, contiguous; lse fp32
         [rows, heads * q_per_kv] or None."""
+        n, args = self._attention(layer, q, out, start, max_new, lse)
+        self._call("lessdec_pages_attend", stream, *args, n, max_new)
+
+    def _attention(self, layer, q, out, start, max_new, lse):
         n, step = self._rows(q, self.heads * self.G, "q")
         if out.dtype != self.tdtype or out.device != self.device or out.shape != q.shape or not out.is_contiguous():
             raise LessdecError("attend: out must be contiguous, like q")
@@ -173,8 +195,27 @@ class PagedCache:
             raise LessdecError("attend: lse must be contiguous fp32 [rows, heads * q_per_kv]")
         if n > self.max_rows:
             raise LessdecError(f"attend: {n} rows exceed max_rows={self.max_rows} the workspace was sized for")
-        self._call("lessdec_pages_attend", stream, layer, q.data_ptr(), step, out.data_ptr(), None if lse is None else lse.data_ptr(),
-                   self._ints(start, self.slots + 1, "start"), n, max_new)
+        return n, (layer, q.data_ptr(), step, out.data_ptr(), None if lse is None else lse.data_ptr(), self._ints(start, self.slots + 1, "start"))
+
+    def share_plan(self):
+        """An int32 tensor for share(), for up to max_rows rows."""
+        return self.torch.zeros(lessdec_pages_share_ints(self.desc, self.max_rows), dtype=self.torch.int32, device=self.device)
+
+    def _plan(self, plan, rows):
+        if rows > self.max_rows:
+            raise LessdecError(f"share: {rows} rows exceed max_rows={self.max_rows} the workspace was sized for")
+        return self._ints(plan, lessdec_pages_share_ints(self.desc, rows), "plan")
+
+    def share(self, start, rows, plan, stream=None):
+        """What neighbouring slots have in common, for attend_shared() calls of `rows` rows; holds until slots, lengths or start change."""
+        self._call("lessdec_pages_share", stream, self._ints(start, self.slots + 1, "start"), rows, self._plan(plan, rows))
+
+    def attend_shared(self, layer, q, out, start, max_new, plan, lse=None, stream=None):
+        """attend() that reads what slots share once for all of them; plan: of share() for these rows."""
+        if not self.shared:
+            raise LessdecError("attend_shared: the cache was made without shared=True")
+        n, args = self._attention(layer, q, out, start, max_new, lse)
+        self._call("lessdec_pages_attend_shared", stream, *args, n, max_new, self._plan(plan, n))
 
     def read(self, layer, slots, first, K, V, stream=None):
         """K, V [n, heads, count, D]: tokens first .. first + count - 1 of slots (int32 [n]), from a slot's end if first < 0."""

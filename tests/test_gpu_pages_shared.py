@@ -1,0 +1,296 @@
+"""Attention that reads what slots share once, on the GPU, through PagedCache, against tests/pages_oracle.py, within the bounds that lessdec_pages_attend
+is held to; and the plan: every node's slots name its pages, and a slot's nodes and its own part are all that it sees."""
+import numpy as np
+import pytest
+
+from tests import pages_oracle as po
+from tests.test_gpu_pages import HALF_STEP, Pair
+
+pytestmark = pytest.mark.gpu
+
+
+class Shared(Pair):
+    def __init__(self, *args, **more):
+        super().__init__(*args, **more)
+        from paper_2402_09398_amd import lessdec_pages_shared_workspace_bytes
+        own = self.own
+        own.shared = True
+        need = lessdec_pages_shared_workspace_bytes(own.desc, own.max_rows)
+        own.workspace = self.t.zeros(need, dtype=self.t.uint8, device="cuda")
+        own.desc.workspace, own.desc.workspace_bytes = own.workspace.data_ptr(), need
+        self.sharing = own.share_plan()
+
+    def nodes(self):
+        """(slot's node, first own block) of every slot, and (row, rows, first block, last, node before, splits) of every node."""
+        r, plan = self.ref, self.sharing.cpu().numpy()
+        n, rows = plan[0], plan[3]
+        columns = min(rows * r.group, r.slots * 128)
+        items = 3 * (columns // 128 + r.slots // 2 + 1) + 512 // r.heads + 1
+        assert plan[1] <= items and plan[2] <= 3 * columns + 128 * (512 // r.heads + 1)
+        node = plan[8 + 4 * items:8 + 4 * items + 12 * r.slots].reshape(-1, 12)[:n]
+        slot = plan[8 + 4 * items + 12 * r.slots:][:2 * r.slots].reshape(-1, 2)
+        return slot, [(int(f[1]), int(f[2]), int(f[5]), int(f[6]), int(f[8]), int(f[9])) for f in node]
+
+    def share(self, counts, behind=2):
+        """The plan for these rows, looked over; the nodes."""
+        r, start = self.ref, np.concatenate([[0], np.cumsum(counts)])
+        self.sharing.fill_(-5)
+        self.own.share(self.ints(start), int(start[-1]) + behind, self.sharing)
+        slot, nodes = self.nodes()
+        per = r.page // 16
+        for row, rows, first, last, before, splits in nodes:
+            there = [s for s in range(r.slots) if counts[s] and row <= start[s] and start[s + 1] <= row + rows]
+            assert len(there) > 1 and sum(counts[s] for s in there) == rows and first % per == last % per == 0 and splits > 0
+            assert all(slot[s][0] >= 0 for s in there) and (before == -1 if first == 0 else nodes[before][3] == first)
+            for j in range(first // per, last // per):
+                named = set()
+                for s in there:
+                    p = r.length[s] - counts[s]
+                    seen = np.arange(j * r.page, (j + 1) * r.page)
+                    if (((seen > p - r.window) | (seen < r.sinks)) if r.window else seen >= 0).any():
+                        named.add(r.table[s, j])
+                assert len(named) <= 1
+        for s in range(r.slots):
+            at, own = slot[s]
+            if counts[s] == 0 or at < 0:
+                assert at == -1 and own == 0
+                continue
+            assert own == nodes[at][3]
+            while at >= 0:
+                row, rows, first, last, at, _ = nodes[at]
+                assert row <= start[s] and start[s + 1] <= row + rows
+                assert first == (nodes[at][3] if at >= 0 else 0)
+        return nodes
+
+    def attend_shared(self, counts, layer=0, size=1.0, queries=None, lse=True, stride=0):
+        start = np.concatenate([[0], np.cumsum(counts)])
+        hq = self.ref.heads * self.ref.group
+        q = self.t.tensor(self.rng.standard_normal((start[-1] + 2, hq, self.ref.dim)) * size).to(self.own.tdtype).cuda() if queries is None else queries
+        if stride:
+            q = self.t.cat([q, q], 1)[:, :hq]
+        out = self.t.full(q.shape, 3.5, dtype=self.own.tdtype, device="cuda")
+        stat = self.t.full(q.shape[:2], 3.5, device="cuda") if lse else None
+        self.own.attend_shared(layer, q, out, self.ints(start), int(max(counts)), self.sharing, stat)
+        want, want_lse, tol, lse_tol = self.ref.attend(layer, q.double().cpu().numpy(), start, HALF_STEP[self.dtype])
+        got, n = out.double().cpu().numpy(), start[-1]
+        assert (got[n:] == 3.5).all(), "rows behind the last slot"
+        np.testing.assert_array_equal(np.isnan(got[:n]), np.isnan(want[:n]))
+        fine = ~np.isnan(want[:n])
+        off = np.abs(got[:n] - want[:n])[fine] - tol[:n][fine]
+        assert off.size == 0 or off.max() <= 0, off.max()
+        if lse:
+            got = stat.double().cpu().numpy()
+            assert (got[n:] == 3.5).all()
+            np.testing.assert_array_equal(np.isneginf(got[:n]), np.isneginf(want_lse[:n]))
+            fine = np.isfinite(want_lse[:n])
+            assert (np.abs(got[:n] - want_lse[:n])[fine] <= lse_tol[:n][fine]).all()
+        return out
+
+    def room(self, n):
+        got = self.reserve(n)
+        assert list(got) == list(n)
+        self.append(n)
+
+
+def prompt(p, n, slots):
+    """A prompt of n tokens in slot 0, that slots become copies of."""
+    p.room([n] + [0] * (p.ref.slots - 1))
+    p.select([0 if s in slots else -1 for s in range(p.ref.slots)])
+
+
+SHAPES = [                                                    # slots, heads, group, dim, page, dtype, prompt, own tokens, rows a slot, sinks, window
+    (4, 2, 1, 64, 16, "f16", 200, [5, 1, 17, 40], [1, 1, 1, 1], 0, 0),
+    (4, 2, 4, 128, 16, "bf16", 130, [5, 1, 17, 40], [1, 1, 1, 1], 0, 0),
+    (5, 3, 5, 128, 32, "f16", 333, [1, 1, 1, 1, 1], [1, 1, 1, 1, 1], 0, 0),
+    (9, 1, 16, 64, 64, "bf16", 500, [3, 70, 9, 1, 1, 20, 33, 2, 8], [1] * 9, 0, 0),
+    (6, 2, 3, 64, 16, "f16", 401, [30, 2, 4, 16, 50, 9], [7, 2, 4, 5, 30, 1], 0, 0),
+    (3, 1, 71, 64, 32, "f16", 300, [4, 40, 1], [1, 1, 1], 0, 0),
+    (40, 1, 8, 128, 16, "bf16", 90, [1 + i % 5 for i in range(40)], [1] * 40, 0, 0),
+    (3, 2, 1, 128, 16, "f16", 150, [60, 200, 33], [60, 140, 33], 0, 0),
+    (6, 1, 2, 64, 16, "f16", 500, [30, 2, 4, 16, 50, 9], [3, 2, 4, 1, 8, 1], 0, 100),
+    (6, 2, 4, 128, 32, "bf16", 500, [30, 2, 4, 16, 50, 9], [1] * 6, 4, 200),
+    (5, 1, 30, 64, 16, "f16", 420, [3, 60, 1, 9, 33], [1, 3, 1, 2, 4], 40, 64),
+    (4, 1, 1, 128, 16, "f16", 300, [20, 1, 3, 8], [20, 1, 3, 8], 70, 1),
+]
+
+
+@pytest.mark.parametrize("slots,heads,group,dim,page,dtype,n,own,rows,sinks,window", SHAPES)
+def test_one_prompt(slots, heads, group, dim, page, dtype, n, own, rows, sinks, window):
+    pages = -(-n // page) + sum(2 + -(-x // page) for x in own) + 4
+    p = Shared(slots, pages, page, -(-(n + max(own)) // page) + 1, heads, dim, dtype, seed=slots + n, q_per_kv=group, sinks=sinks, window=window)
+    prompt(p, n, range(slots))
+    p.room(own)
+    nodes = p.share(rows)
+    assert nodes or window or max(rows) * group >= 128, "nothing is shared"      # (a slot of that many columns stands between the others)
+    p.attend_shared(rows)
+    p.attend_shared(rows, size=4.0, lse=False, stride=1)
+    order = [(3 * s + 1) % slots for s in range(slots)]
+    p.select(order)                                           # beams that go on from others
+    rows = [rows[s] for s in order]
+    p.share(rows)
+    p.attend_shared(rows, size=2.0)
+
+
+def test_all_is_shared():
+    """Forks that have no token of their own yet, a partly filled page among what they share; then one of them gets some."""
+    for group, rows in ((1, 1), (4, 3), (33, 1)):
+        p = Shared(6, 60, 16, 20, 2, 64, "f16", q_per_kv=group)
+        prompt(p, 203, range(6))
+        assert len(p.share([rows] * 6)) == 1
+        p.attend_shared([rows] * 6)
+        p.room([0, 0, 4, 0, 0, 1])
+        p.share([rows, 1, 3, 0, 0, 1])
+        p.attend_shared([rows, 1, 3, 0, 0, 1])
+
+
+def test_nested_prompts_and_slots_that_share_nothing():
+    """Instructions for all, prompts of their own behind them, samples of each; a slot without rows in between, one of another prompt, one with
+    many columns, one that is empty."""
+    p = Shared(14, 200, 16, 40, 2, 64, "bf16", q_per_kv=2)
+    p.room([150] + [0] * 13)
+    p.select([0] * 12 + [-1, -1])
+    p.room([100, 0, 0, 0, 64, 0, 0, 0, 33, 0, 0, 0, 90, 0])
+    p.select([0, 0, 0, 0, 4, 4, 4, 4, 8, 8, 8, 8, 12, -1])
+    p.room([3, 1, 20, 5, 1, 70, 2, 2, 1, 1, 1, 1, 2, 0])
+    for rows in ([1] * 13 + [0], [1, 1, 0, 2, 1, 70, 1, 2, 1, 1, 1, 1, 2, 0], [0, 1, 0, 0, 0, 1, 0, 0, 0, 0, 0, 1, 0, 0], [3, 1, 9, 4, 1, 5, 2, 2, 1, 1, 1, 1, 2, 0]):
+        nodes = p.share(rows)
+        assert len(nodes) >= 1
+        p.attend_shared(rows)
+    assert any(node[4] >= 0 for node in p.share([1] * 13 + [0])), "no node within another"
+
+
+def test_sharing_that_deepens_slot_by_slot():
+    """Every slot goes on from the one before it: nodes within nodes, more than are kept."""
+    p = Shared(8, 200, 16, 40, 1, 64, "f16")
+    p.room([300] + [0] * 7)
+    for s in range(1, 8):
+        p.select([i if i < s else s - 1 if i == s else -1 for i in range(8)])
+        p.room([0] * s + [48] + [0] * (7 - s))
+    nodes = p.share([1] * 8)
+    assert len(nodes) > 1
+    p.attend_shared([1] * 8)
+    p.select([7, 6, 5, 4, 3, 2, 1, 0])
+    p.share([1] * 8)
+    p.attend_shared([1] * 8)
+
+
+def test_many_slots():
+    for slots, group in ((70, 1), (300, 2), (1100, 1)):
+        p = Shared(slots, slots * 2 + 60, 16, 14, 1, 64, "f16", q_per_kv=group)
+        prompt(p, 100, range(slots))
+        p.room([1 + s % 3 for s in range(slots)])
+        assert len(p.share([1] * slots)) == 1
+        p.attend_shared([1] * slots)
+        p.select([s // 5 * 5 for s in range(slots)])
+        p.room([s % 2 for s in range(slots)])
+        rows = [s % 7 != 3 for s in range(slots)]
+        p.share(rows)
+        p.attend_shared(rows)
+
+
+def test_a_long_prefix_over_many_workgroups():
+    p = Shared(5, 1500, 16, 1400, 2, 64, "bf16", q_per_kv=3)
+    prompt(p, 20000, range(5))
+    p.room([1, 30, 7, 2, 500])
+    for rows in ([1] * 5, [1, 9, 7, 2, 30]):
+        nodes = p.share(rows)
+        assert nodes[0][5] > 20
+        p.attend_shared(rows)
+
+
+def test_what_a_row_does_not_see_does_not_reach_it():
+    """NaN and infinities among shared tokens, seen by some of the slots' rows; scores far apart."""
+    p = Shared(4, 60, 16, 20, 1, 64, "f16", q_per_kv=5, sinks=2, window=120)
+
+    def spoil(k, v, start):
+        nan, inf = float("nan"), float("inf")
+        v[75, 0, 3], v[40, 0, 5], v[130, 0, 9], v[1, 0, 60] = nan, inf, nan, nan
+        k[71, 0, 1] = nan
+        k[150] *= 50
+    p.reserve([200, 0, 0, 0])
+    p.append([200, 0, 0, 0], spoil=spoil)
+    p.select([0, 0, 0, 0])
+    p.room([1, 40, 9, 20])
+    for rows in ([1] * 4, [1, 3, 2, 12]):
+        p.share(rows)
+        p.attend_shared(rows)
+        p.attend_shared(rows, size=30.0)
+
+
+def test_plans_of_other_rows_and_other_contents():
+    """A plan for another number of rows counts as none; whatever a plan holds, nothing outside the arrays is touched and the call ends."""
+    p = Shared(6, 80, 16, 20, 2, 64, "f16", q_per_kv=4)
+    prompt(p, 200, range(6))
+    p.room([1, 2, 3, 4, 5, 6])
+    p.share([1] * 6)
+    p.attend_shared([1, 2, 3, 1, 1, 1])
+    p.sharing.zero_()
+    p.attend_shared([1] * 6)
+    p.share([1] * 6)
+    p.attend_shared([1] * 6)
+
+
+def test_a_captured_step():
+    """Forks, then steps of one graph: room, copies, the plan, append and attention in two layers; eager calls in between."""
+    import torch
+    slots = 6
+    p = Shared(slots, 120, 16, 24, 2, 64, "bf16", q_per_kv=2, layers=2)
+    prompt(p, 180, range(slots))
+    p.room([9, 1, 30, 4, 2, 16])
+    one, start = p.ints([1] * slots), p.ints(np.arange(slots + 1))
+    k, v = (torch.empty(slots, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, out = (torch.empty(slots, 4, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    outs = [torch.empty_like(out) for _ in range(2)]
+    plan = p.ints(np.zeros(1 + 2 * slots))
+
+    def step():
+        p.own.reserve(one, None, plan)
+        p.own.copy(plan, slots)
+        p.own.share(start, slots, p.sharing)
+        for layer in range(2):
+            p.own.append(layer, k, v, start)
+            p.own.attend_shared(layer, q, outs[layer], start, 1, p.sharing)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(6):
+        for x in (k, v, q):
+            x.copy_(torch.tensor(p.rng.standard_normal(tuple(x.shape))))
+        (step if i == 3 else graph.replay)()
+        torch.cuda.synchronize()
+        _, pairs = p.ref.reserve([1] * slots)
+        p.ref.copy(pairs)
+        p.state()
+        for layer in range(2):
+            p.ref.append(layer, k.double().cpu().numpy(), v.double().cpu().numpy(), np.arange(slots + 1))
+            want, _, tol, _ = p.ref.attend(layer, q.double().cpu().numpy(), np.arange(slots + 1), HALF_STEP["bf16"])
+            assert (np.abs(outs[layer].double().cpu().numpy() - want) <= tol).all()
+        p.share([1] * slots, behind=0)
+        p.attend([1] * slots)
+        if i == 1:
+            p.select([2, 2, 0, 3, 3, 1])
+
+
+def test_rows_of_another_stream_and_wrong_tensors():
+    import torch
+    from paper_2402_09398_amd import LessdecError, PagedCache
+    p = Shared(4, 60, 16, 16, 1, 128, "f16", q_per_kv=2)
+    prompt(p, 150, range(4))
+    p.room([1, 2, 3, 4])
+    side = torch.cuda.Stream()
+    q = torch.tensor(p.rng.standard_normal((4, 2, 128))).half().cuda()
+    out, out2 = torch.empty_like(q), torch.empty_like(q)
+    start = p.ints(np.arange(5))
+    side.wait_stream(torch.cuda.current_stream())
+    p.own.share(start, 4, p.sharing, stream=side)
+    p.own.attend_shared(0, q, out, start, 1, p.sharing, stream=side)
+    side.synchronize()
+    p.own.share(start, 4, p.sharing)
+    p.own.attend_shared(0, q, out2, start, 1, p.sharing)
+    assert torch.equal(out, out2)
+    bare = PagedCache(4, 60, 16, 16, 1, 128, "f16", q_per_kv=2, max_rows=4)
+    for call in (lambda: bare.attend_shared(0, q, out, start, 1, bare.share_plan()), lambda: p.own.attend_shared(0, q, out, start, 1, p.sharing[:100]),
+                 lambda: p.own.share(start[:4], 4, p.sharing), lambda: p.own.share(start, 4097, p.sharing), lambda: p.own.share(start, 4, p.sharing.float()),
+                 lambda: p.own.share(start, 4, p.sharing[1:])):
+        with pytest.raises(LessdecError):
+            call()
