@@ -51,6 +51,22 @@ __device__ inline int block_index(const Pages &c, int s, int head, int block)
   return block_in(c, c.table[(size_t)s * c.table_len + entry_of(c, block)], head, block);
 }
 
+// The last i in [0, n) whose base(i) is at most x, likewise, for any n.
+template <typename F>
+__device__ inline int last_at(int n, long x, F base)
+{
+  const int lane = threadIdx.x & 63;
+  int from = 0;
+  int step = 1;
+  while ((long)step * kWave < n) step *= kWave;
+  for (;; step /= kWave) {
+    const long i = from + (long)lane * step;
+    const int there = __popcll(__ballot(i < n && base((int)(i < n ? i : 0)) <= x));
+    from += (there > 0 ? there - 1 : 0) * step;
+    if (step == 1) return from;
+  }
+}
+
 // The last slot s in [0, slots) whose base(s) is at most x, for a base that does not fall with s: 64 lanes ask at a time, so that
 // up to 4096 slots cost two rounds of loads.  All lanes of a wave call it with the same x.
 template <typename F>
@@ -113,56 +129,69 @@ constexpr int kPagesWorkers = 768;                   // workgroups of the kernel
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 
 // What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
-//  head  [8]: nodes, items, columns in all, rows that it was made for
-//  slot  [slots][2]: the node that its row begins with (-1: none), the first block that is its own
-//  node  [slots][kNodeInts]: slot whose table row to read, first row, rows, least and largest position of them, blocks [first, last), first column,
-//        node before it (-1: none), splits.  A node has splits times (rows * q_per_kv) columns
+//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, log2 of the workers, tiles of a chunk
+//  node  [3 slots][kNodeInts]: slot whose table row is read, first row, rows, least and largest position of them, blocks [first, last), node before it
+//        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
+//        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
+//  few   [4 slots][2]: steps, slot (that shares nothing) or slots + node, of up to kFewColumns columns
+//  slot  [slots]: the node that is its own part (-1: it shares nothing)
 //  pos   [rows]: positions of the rows
-//  item  [items][4]: node, tile of 128 columns | split << 16, tiles [from, to) of the node's blocks
-//  apart [kAgreeWorkers][slots]: scratch
-// A (head, column) of the plan has a sum of D floats, a maximum and a total in the workspace.
-constexpr int kPlanNodes = 0, kPlanItems = 1, kPlanColumns = 2, kPlanRows = 3, kPlanHead = 8, kNodeInts = 12, kAgreeWorkers = 64;
-constexpr int kTrunkWorkers = 512, kTrunkDepth = 3, kTrunkTile = 128;  // workgroups of the nodes; nodes on a slot's way; columns of a tile
+//  apart [slots]: scratch
+// A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
+constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanShift = 4, kPlanChunk = 5, kPlanHead = 8, kNodeInts = 12, kEndless = 1 << 30;
+constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
+constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
+constexpr int kTrunkShift = 8, kTrunkLong = 14;      // 256 workers, one to a compute unit; two from so many tiles on that each of them then has
+constexpr int kTrunkWorkers = 2 << kTrunkShift, kFewWorkers = 256;     // workgroups of the launch
 struct Plan {
-  int *head, *slot, *node, *pos, *item, *apart;
+  int *head, *node, *few, *slot, *apart, *pos;
 };
-// Slots of up to 127 query columns share; a row is in kTrunkDepth nodes at most, a level has half as many nodes as slots.
-inline long shared_columns(int slots, int q_per_kv, long rows)
-{
-  const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
-  return n < most ? n : most;
-}
-inline long plan_items(int slots, int heads, int q_per_kv, long rows)
-{
-  return kTrunkDepth * (shared_columns(slots, q_per_kv, rows) / kTrunkTile + slots / 2 + 1) + kTrunkWorkers / heads + 1;
-}
+// The tiles of all heads and nodes, one behind the other, are dealt out evenly: worker w has [first(w), first(w + 1)).  Within a node and head
+// they are ordered by chunks of tokens, in a chunk by tiles of 128 columns, so that neighbouring workers read the same tokens at the same time.  A
+// chunk is no longer than any worker's part: what it has of 128 columns is cut into two pieces at most.
+struct Trunk {
+  int tiles, heads;                                  // of a head; all of them together are less than 2^31
+  int shift;                                         // log2 of the workers
+  int chunk;
+  __host__ __device__ inline unsigned total() const { return (unsigned)tiles * heads; }
+  __host__ __device__ inline unsigned first(unsigned w) const { return (unsigned)((unsigned long long)w * total() >> shift); }
+  __host__ __device__ inline int chunks(int n) const { return (n + chunk - 1) / chunk; }        // of n tiles of 128 columns
+  __host__ __device__ inline static Trunk of(int tiles, int heads)
+  {
+    Trunk t{tiles, heads, 0, 1};
+    const unsigned n = t.total();                    // (two tiles to a worker, at least)
+    while (t.shift < kTrunkShift && n >> (t.shift + 2)) ++t.shift;
+    if (t.shift == kTrunkShift && n >> (t.shift + 1) >= kTrunkLong) ++t.shift;
+    if (n >> t.shift) t.chunk = (int)(n >> t.shift);
+    return t;
+  }
+};
+// Slots of up to 127 query columns share.  A row is in kTrunkDepth nodes and one of its own at most, each of which has room for two pieces, and
+// for as many more as chunks are (n tiles have n / chunk + 1 at most, and a chunk is at least half of a worker's part).
 inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
 {
-  return kTrunkDepth * shared_columns(slots, q_per_kv, rows) + (long)kTrunkTile * (kTrunkWorkers / heads + 1);
+  const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
+  return 2 * (kTrunkDepth + 1) * (n < most ? n : most) + 4L * kTrunkTile * (kTrunkWorkers / heads + 1);
 }
-inline long plan_ints(int slots, int heads, int q_per_kv, long rows)
-{
-  return kPlanHead + 4 * plan_items(slots, heads, q_per_kv, rows) + (long)slots * (2 + kNodeInts + kAgreeWorkers) + rows;
-}
-inline Plan plan_at(int *p, int slots, int heads, int q_per_kv, long rows)
+inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (3 * kNodeInts + 8 + 2) + rows; }
+inline Plan plan_at(int *p, int slots)
 {
   Plan x;
   x.head = p;
-  x.item = x.head + kPlanHead;                       // (16-byte aligned, as the nodes are)
-  x.node = x.item + 4 * plan_items(slots, heads, q_per_kv, rows);
-  x.slot = x.node + (long)slots * kNodeInts;
-  x.apart = x.slot + 2L * slots;
-  x.pos = x.apart + (long)slots * kAgreeWorkers;
+  x.node = x.head + kPlanHead;                       // (16-byte aligned)
+  x.few = x.node + 3L * slots * kNodeInts;
+  x.slot = x.few + 8L * slots;
+  x.apart = x.slot + slots;
+  x.pos = x.apart + slots;
   return x;
 }
 struct SharedArgs : AttendArgs {
   Plan plan;
   float *trunk;                                      // [heads][columns][D] sums, [heads][columns] maxima, [heads][columns] totals
   long columns;
-  int items;                                         // that the plan has room for
 };
 hipError_t launch_pages_attend_shared(const Pages &c, int dtype, const SharedArgs &a, hipStream_t st);
-hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, int items, long columns, hipStream_t st);
+hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, long columns, hipStream_t st);
 
 // floats of AttendArgs::parts for up to `rows` rows
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows);

@@ -163,7 +163,7 @@ int lessdec_pages_append(const lessdec_pages_desc *desc, int32_t layer, const vo
 size_t lessdec_pages_share_ints(const lessdec_pages_desc *desc, int32_t max_rows)
 {
   if (!shape_ok(desc) || max_rows < 0) return 0;
-  return (size_t)plan_ints(desc->slots, desc->heads, desc->q_per_kv > 1 ? desc->q_per_kv : 1, max_rows);
+  return (size_t)plan_ints(desc->slots, max_rows);
 }
 
 size_t lessdec_pages_shared_workspace_bytes(const lessdec_pages_desc *desc, int32_t max_rows)
@@ -179,8 +179,7 @@ int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, in
   if (!rows_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0) return LESSDEC_OK;
   if (!start || !plan || !aligned(start, 4) || !aligned(plan, 16) || plan == start || plan == desc->table || plan == desc->length) return LESSDEC_EINVAL;
-  return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots, c.heads, c.q_per_kv, rows), (int)plan_items(c.slots, c.heads, c.q_per_kv, rows),
-                                   plan_columns(c.slots, c.heads, c.q_per_kv, rows), (hipStream_t)hip_stream));
+  return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots), plan_columns(c.slots, c.heads, c.q_per_kv, rows), (hipStream_t)hip_stream));
 }
 
 int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t stride, void *out, float *lse, const int32_t *start,
@@ -197,10 +196,9 @@ int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, c
   SharedArgs a;
   static_cast<AttendArgs &>(a) = AttendArgs{q, step, out, lse, start, rows, max_new < rows ? max_new : rows, static_cast<int *>(desc->workspace),
                                             static_cast<float *>(scratch(desc))};
-  a.plan = plan_at(const_cast<int32_t *>(plan), c.slots, c.heads, c.q_per_kv, rows);
+  a.plan = plan_at(const_cast<int32_t *>(plan), c.slots);
   a.trunk = reinterpret_cast<float *>(static_cast<char *>(scratch(desc)) + own_bytes(desc, rows));
   a.columns = plan_columns(c.slots, c.heads, c.q_per_kv, rows);
-  a.items = (int)plan_items(c.slots, c.heads, c.q_per_kv, rows);
   return result(launch_pages_attend_shared(c, desc->dtype, a, (hipStream_t)hip_stream));
 }
 

@@ -182,56 +182,47 @@ __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__
 
 // ---- slots that share pages --------------------------------------------------------------------------------------------
 //
-// What neighbouring slots have in common (a node of the plan) is gone through once, for the rows of all of them, by wide_kernel's work in a launch of
-// its own; the kernels of the slots begin behind it and take its sums in where they finish a row.  A sum lies at [head][column of the plan].
+// What neighbouring slots have in common (a node of the plan) is gone through once, for the rows of all of them, and what is behind it a slot at a
+// time, by the same two kernels' work in one launch; a second one joins a row's sums.  Sums lie at [head][column of the plan].
 template <typename Args> constexpr bool kShares = false;
 template <> constexpr bool kShares<SharedArgs> = true;
 
-// a slot's node (-1: none) and the first block of its own
-template <typename Args> __device__ inline int2 own_of(const Args &a, int s)
+// of a value that is the same in all lanes: in a scalar register, where loads from memory that the kernel also writes are not by themselves
+__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Work that a kernel does piece by piece: what depends on the thread alone is not to be kept in registers over all of them (it would be
+// computed before the first, and spilled).
+template <typename Args> __device__ inline int thread_of()
 {
-  if constexpr (kShares<Args>) {
-    const int2 x = reinterpret_cast<const int2 *>(a.plan.slot)[s];
-    return a.plan.head[kPlanRows] == a.rows ? make_int2(x.x, max(x.y, 0)) : make_int2(-1, 0);
-  }
-  return make_int2(-1, 0);
+  int x = threadIdx.x;
+  if constexpr (kShares<Args>) asm volatile("" : "+v"(x));
+  return x;
 }
-template <typename Args> __device__ inline void cut_own(const Args &a, int s, Span &span)
-{
-  if constexpr (kShares<Args>) span.cut(own_of(a, s).y, 1 << 30);
-}
+
 struct Node {
-  int slot, row, rows, lo, hi, first, last, base, parent, splits;      // last: the block behind its last one; base: its first column of the plan
+  int slot, row, rows, lo, hi, first, last, before, tile, tiles, base, shares;
   int cols;
 };
+// (i: the same in all lanes)
 __device__ inline Node node_of(const Pages &c, const SharedArgs &a, int i)
 {
-  const int *f = a.plan.node + (long)i * kNodeInts;
+  const int4 *f = reinterpret_cast<const int4 *>(a.plan.node + (long)i * kNodeInts);
+  const int4 x = f[0], y = f[1], z = f[2];
+  const int most = c.table_len * c.page_tokens;
   Node n;
-  n.slot = min(max(f[0], 0), c.slots - 1);
-  n.row = min(max(f[1], 0), a.rows);
-  n.rows = min(max(f[2], 0), a.rows - n.row);
-  n.lo = f[3]; n.hi = f[4]; n.first = f[5]; n.last = f[6];
-  n.base = max(f[7], 0);
-  n.parent = f[8];
-  n.splits = max(f[9], 0);
+  n.slot = min(max(same(x.x), 0), c.slots - 1);
+  n.row = min(max(same(x.y), 0), a.rows);
+  n.rows = min(max(same(x.z), 0), a.rows - n.row);
+  n.lo = min(max(same(x.w), 0), most - 1);
+  n.hi = min(max(same(y.x), -1), most - 1);
+  n.first = max(same(y.y), 0);
+  n.last = min(max(same(y.z), 0), c.table_len * page_blocks(c));
+  n.before = same(y.w);
+  n.tile = same(z.x); n.tiles = max(same(z.y), 0); n.base = same(z.z); n.shares = max(same(z.w), 0);
   n.cols = n.rows * c.q_per_kv;
   return n;
 }
-// Calls take(index of the first share, from one to the next, how many) for every node that a slot's column belongs to, the nearest first.
-template <typename Take> __device__ inline void each_trunk(const Pages &c, const SharedArgs &a, int node, int row, int g, Take take)
-{
-  int upto = INT_MAX;
-  while ((unsigned)node < (unsigned)c.slots) {
-    const Node n = node_of(c, a, node);
-    const int col = (row - n.row) * c.q_per_kv + g;
-    // (a plan has its nodes end ever earlier, and its shares in their place; nothing else is followed)
-    if (n.last >= upto || (unsigned)col >= (unsigned)n.cols || (long)n.base + (long)n.splits * n.cols > a.columns) return;
-    upto = n.last;
-    take((long)n.base + col, (long)n.cols, n.splits);
-    node = n.parent;
-  }
-}
+__device__ inline bool plan_holds(const SharedArgs &a) { return same(a.plan.head[kPlanRows]) == a.rows; }
 
 // ---- few rows a slot: up to 16 query columns -----------------------------------------------------------------------------
 //
@@ -252,31 +243,40 @@ constexpr int kGroup = 32;
 // has, as lengths are on the device: the same sequence alone in a cache of 64 slots takes 60 us, in one of its own 52.
 inline int few_workers(long items) { return (int)(items * kGroup < 256 ? 256 : items * kGroup < kPagesWorkers ? items * kGroup : kPagesWorkers); }
 
-template <typename Args> __device__ inline int steps_of(const Pages &c, const Args &a, int s)
+__device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
 {
   const Rows r = slot_rows(a.start, s, a.rows);
   if (r.count == 0 || r.count * c.q_per_kv > kCols) return 0;
   const int len = slot_length(c, s);
-  Span span = span_of(c, len - r.count, len - 1);
-  cut_own(a, s, span);
-  const int n = (span.count + kStepBlocks - 1) / kStepBlocks;
+  const int n = (span_of(c, len - r.count, len - 1).count + kStepBlocks - 1) / kStepBlocks;
   return n > 0 ? n : 1;                              // (rows that see nothing are written too)
 }
+// where slots share pages, entries of the plan: slots that share nothing, and nodes of few columns
+__device__ inline int steps_of(const Pages &c, const SharedArgs &a, int i)
+{
+  return plan_holds(a) ? min(max(a.plan.few[2L * i], 0), c.table_len * page_blocks(c) / kStepBlocks + 1) : steps_of(c, static_cast<const AttendArgs &>(a), i);
+}
+__device__ inline int few_entries(const Pages &c, const AttendArgs &) { return c.slots; }
+__device__ inline int few_entries(const Pages &c, const SharedArgs &a) { return plan_holds(a) ? min(max(same(a.plan.head[kPlanFew]), 0), 4 * c.slots) : c.slots; }
 
 // Worker w's part [begin, end) of the steps, and where it begins: slot, and step among the slot's (head by head).
 struct Part {
   long begin, end, per;
   int slot;
   long in_slot;
+  bool whole;                                        // the slots (by head) that begin in the part are all its own, to their end
 };
 template <typename Args> __device__ inline Part part_of(const Pages &c, const Args &a, int w, int workers)
 {
   __shared__ long sums[4], found_at;
-  __shared__ int found;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int found, most;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, entries = few_entries(c, a);
+  int largest = 0;
   auto scan = [&](int base, long &n, long &upto, long &at) {           // at: the sum before this chunk, then behind it
     const int s = base + tid;
-    n = s < c.slots ? (long)steps_of(c, a, s) * c.heads : 0;
+    const int steps = s < entries ? steps_of(c, a, s) : 0;
+    n = (long)steps * c.heads;
+    if constexpr (kShares<Args>) largest = max(largest, steps);
     upto = n;
     for (int d = 1; d < kWave; d <<= 1) {
       const long y = __shfl_up(upto, d, kWave);
@@ -294,8 +294,17 @@ template <typename Args> __device__ inline Part part_of(const Pages &c, const Ar
   };
   Part p;
   long total = 0, n, upto;
-  for (int base = 0; base < c.slots; base += 256) scan(base, n, upto, total);
+  for (int base = 0; base < entries; base += 256) scan(base, n, upto, total);
   p.per = (total + workers - 1) / workers;
+  p.whole = false;
+  if constexpr (kShares<Args>) {
+    // Where none is longer than a part, parts that meet at slots have nothing to join.
+    if (tid == 0) most = 0;
+    __syncthreads();
+    atomicMax(&most, largest);
+    __syncthreads();
+    p.whole = most <= p.per;
+  }
   p.begin = w * p.per;
   p.end = p.begin + p.per < total ? p.begin + p.per : total;
   if (p.begin >= p.end) return p;
@@ -305,11 +314,11 @@ template <typename Args> __device__ inline Part part_of(const Pages &c, const Ar
       found_at = p.begin - (upto - n);
     }
   };
-  if (c.slots <= 256) {
+  if (entries <= 256) {
     look(0);
   } else {
     long at = 0;
-    for (int base = 0; base < c.slots && at <= p.begin; base += 256) {
+    for (int base = 0; base < entries && at <= p.begin; base += 256) {
       __syncthreads();
       scan(base, n, upto, at);
       look(base);
@@ -392,40 +401,6 @@ __device__ inline void join(int n, int cols, Share share, Done done)
   }
 }
 
-// The sums of a slot's nodes at a column and two channels, added to its own.
-template <int D>
-__device__ inline void add_trunks(const Pages &c, const SharedArgs &a, int node, int head, int row, int g, int d, float &x, float &y, float &top, float &l)
-{
-  const float *sums = a.trunk + head * a.columns * D + d, *tops = a.trunk + c.heads * a.columns * D + head * a.columns, *totals = tops + c.heads * a.columns;
-  each_trunk(c, a, node, row, g, [&](long first, long step, int shares) {
-    for (int k = 0; k < shares; k += 8) {            // eight at a time on their way
-      float m[8], u[8];
-      float2 v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const long at = first + min(k + j, shares - 1) * step;
-        m[j] = k + j < shares ? tops[at] : -__builtin_inff();
-        u[j] = totals[at];
-        v[j] = *reinterpret_cast<const float2 *>(sums + at * D);
-      }
-      float now = top;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) now = fmaxf(now, m[j]);
-      const float less = exp2_fast(top - now);
-      top = now;
-      l *= less; x *= less; y *= less;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (m[j] == -__builtin_inff()) continue;     // no tiles, nothing written
-        const float e = exp2_fast(m[j] - top);
-        l = fmaf(u[j], e, l);
-        x = fmaf(v[j].x, e, x);
-        y = fmaf(v[j].y, e, y);
-      }
-    }
-  });
-}
-
 template <int D> struct FewShared {
   float sums[4][kCols][D + 4], tops[4][kCols], totals[4][kCols];
 };
@@ -435,25 +410,56 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
   constexpr int H = D / 64, T = D / 16;
   auto &sums = shared.sums;
   auto &tops = shared.tops, &totals = shared.totals;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(thread_of<Args>() >> 6), lane = thread_of<Args>() & 63, n = lane & 15, g = lane >> 4;
   const int G = c.q_per_kv;
   const Part part = part_of(c, a, worker, workers);
   if (part.begin >= part.end) return;
   int s = part.slot;
   long in_slot = part.in_slot;
   for (long pos = part.begin; pos < part.end;) {
-    const int steps = steps_of(c, a, s);
+    int steps = steps_of(c, a, s);
+    if constexpr (kShares<Args>) steps = same(steps);
     if (steps == 0) { ++s; in_slot = 0; continue; }
     const int head = (int)((unsigned long)in_slot >> 32 ? in_slot / steps : (unsigned)in_slot / (unsigned)steps);
     const int from = (int)(in_slot - (long)head * steps);
-    const int to = (int)min((long)steps, from + (part.end - pos));
+    const bool skip = kShares<Args> && part.whole && from > 0;         // (another worker's)
+    const int to = kShares<Args> && part.whole ? steps : (int)min((long)steps, from + (part.end - pos));
+    if (skip) {
+      pos += to - from;
+      in_slot += to - from;
+      if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
+      continue;
+    }
 
-    const Rows rows = slot_rows(a.start, s, a.rows);
-    const int len = slot_length(c, s), lo = len - rows.count, hi = len - 1, cols = rows.count * G;
-    Span span = span_of(c, lo, hi);
-    cut_own(a, s, span);
-    const int node = own_of(a, s).x;
-    const int p = lo + n / G;
+    Rows rows;
+    int lo, hi, p, read = s;
+    Span span;
+    Node node;
+    bool is_node = false;
+    if constexpr (kShares<Args>)
+      if (plan_holds(a)) {
+        const int i = same(a.plan.few[2L * s + 1]);
+        is_node = i >= c.slots;
+        if (is_node) node = node_of(c, a, min(i - c.slots, 3 * c.slots - 1));
+        else read = max(i, 0);
+      }
+    if (!is_node) {
+      rows = slot_rows(a.start, read, a.rows);
+      const int len = slot_length(c, read);
+      lo = len - rows.count;
+      hi = len - 1;
+      span = span_of(c, lo, hi);
+      p = lo + n / G;
+    } else if constexpr (kShares<Args>) {
+      rows = Rows{node.row, node.rows};
+      read = node.slot;
+      lo = node.lo;
+      hi = node.hi;
+      span = span_of(c, lo, hi);
+      span.cut(node.first, node.last);
+      p = n < node.cols ? min(max(a.plan.pos[node.row + n / G], -1), c.table_len * c.page_tokens - 1) : -1;
+    }
+    const int cols = min(rows.count * G, kCols);
     u4 q[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -467,7 +473,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     // A wave's blocks are looked up 64 at a time, a lane each: two of every step.  The next step's keys are requested as soon as this one's
     // are multiplied, its values likewise; every load is made (of the last step's blocks behind it, of the pool's first block where
     // there is none): with a branch around it the compiler would wait for all loads where it means to wait for the older ones.
-    const int *table = c.table + (size_t)s * c.table_len;
+    const int *table = c.table + (size_t)read * c.table_len;
     u4 k[2][H], v[2][H];
     int ats, exs, base, end;                         // the lane's block in the pool, or -1, and its exponents; steps [base, end)
     auto look = [&](int step) {
@@ -617,7 +623,15 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
       for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(&sums[wave][n][t * 16 + g * 4]) = acc[t] * f;
     __syncthreads();
     auto finish = [&](int col, int d, float x, float y, float m, float l) {
-      if constexpr (kShares<Args>) add_trunks<D>(c, a, node, head, rows.first + col / G, col % G, d, x, y, m, l);
+      if constexpr (kShares<Args>)
+        if (is_node) {
+          const long at = (long)head * a.columns + node.base + col;
+          if (node.base < 0 || (long)node.base + col >= a.columns) return;
+          *reinterpret_cast<float2 *>(a.trunk + at * D + d) = make_float2(x, y);
+          float *tops = a.trunk + c.heads * a.columns * D;
+          if (d == 0) { tops[at] = l == 0.f && m == kLowest ? -__builtin_inff() : m; tops[c.heads * a.columns + at] = l; }
+          return;
+        }
       const float r = 1.f / l;
       const long at = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
       reinterpret_cast<unsigned *>(a.out)[at * (D / 2) + d / 2] =
@@ -679,8 +693,8 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
   }
 }
 
-template <bool BF16, int D, typename Args>
-__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, Args a)
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 3) void few_kernel(Pages c, AttendArgs a)
 {
   __shared__ FewShared<D> shared;
   few_rows<BF16, D>(c, a, blockIdx.x, gridDim.x, shared);
@@ -725,14 +739,17 @@ constexpr int wide_floats(int D) { return kWide * (D + 2); }
 // which leaves each as many as it can have.  32 slots of 537 to 4096 tokens, 8 heads: 201 us, as the slots are 247; 64 slots of 2048: 204 and
 // 233; 4 slots of 4096: 830 and 816.  Split tiles have a second launch that would do all of this again: 64 slots, 24 us as they are, 30 in order.
 struct Columns { int slot, first, count, len; };     // first column, columns of the slot in all; its tokens
-__device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bool sorted, Columns &t, Rows &rows)
+// where slots share pages, those that share nothing are what is left to wide_kernel
+__device__ inline bool shares(const AttendArgs &, int) { return false; }
+__device__ inline bool shares(const SharedArgs &a, int s) { return plan_holds(a) && a.plan.slot[s] >= 0; }
+template <typename Args> __device__ inline bool columns_of(const Pages &c, const Args &a, int x, bool sorted, Columns &t, Rows &rows)
 {
   const int G = c.q_per_kv, lane = threadIdx.x & 63;
   int i;
   if (sorted) {
     const int s = min(lane, c.slots - 1);
     const Rows r = slot_rows(a.start, s, a.rows);
-    const int len = slot_length(c, s), n = lane < c.slots && r.count * G > kCols ? (r.count * G + kWide - 1) / kWide : 0;
+    const int len = slot_length(c, s), n = lane < c.slots && r.count * G > kCols && !shares(a, s) ? (r.count * G + kWide - 1) / kWide : 0;
     const int seen = c.window > 0 ? min(len, min(c.window, len) + r.count) : len;
     const int key = (seen / kTile << 6) + 63 - lane;   // tokens that a tile sees, in tiles; ties as the slots are
     int before = 0;
@@ -759,7 +776,7 @@ __device__ inline bool columns_of(const Pages &c, const AttendArgs &a, int x, bo
   }
   t.count = rows.count * G;
   const int n = (t.count + kWide - 1) / kWide;
-  if (i < 0 || i >= n || t.count <= kCols) return false;               // (i < 0: before the first slot's rows)
+  if (i < 0 || i >= n || t.count <= kCols || shares(a, t.slot)) return false;               // (i < 0: before the first slot's rows)
   t.slot = __builtin_amdgcn_readfirstlane(t.slot);
   t.count = __builtin_amdgcn_readfirstlane(t.count);
   t.len = __builtin_amdgcn_readfirstlane(t.len);
@@ -773,38 +790,36 @@ template <int D> struct WideShared {
   __align__(16) u4 tiles[4][kTile * D / 8];
   int spoiled, lo[4], hi[4];
 };
+// A piece of the nodes' tiles: 128 columns of a node by one head, tiles [from, to), the piece-th of these columns.
+struct Piece {
+  Node node;
+  int column, head, from, to, piece;
+  bool only;                                         // the chunk has no second piece
+};
 
-// Item `id` of a launch.  kTrunk: of the plan's list, columns of all slots of a node; else of the slots' own.
+// Item `id` of a launch, or with kTrunk a piece of the plan's.
 template <bool BF16, int D, bool kTrunk, typename Args>
-__device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigned id, unsigned items, int splits, WideShared<D> &shared)
+__device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigned id, unsigned items, int splits, const Piece &trunk, WideShared<D> &shared)
 {
   constexpr int H = D / 64, KK = D / 16, OB = D / 32;
   auto &spoiled = shared.spoiled;
   auto keys = shared.tiles, values = shared.tiles + 2;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(thread_of<Args>() >> 6), lane = thread_of<Args>() & 63, n = lane & 31, h = lane >> 5;
   const int G = c.q_per_kv;
-  const int split = id % (unsigned)splits;
-  const unsigned item = id / (unsigned)splits;
-  const int head = item / items;
+  const int split = kTrunk ? 0 : id % (unsigned)splits;
+  const unsigned item = kTrunk ? 0 : id / (unsigned)splits;
+  const int head = kTrunk ? trunk.head : item / items;
   Columns t;
   Rows rows;
   Span span;
-  Node trunk;
-  int node = -1, piece = 0, from, to, lo, hi, wave_lo, wave_hi, p;
+  int from, to, lo, hi, wave_lo, wave_hi, p;
   if constexpr (kTrunk) {
-    const int4 f = reinterpret_cast<const int4 *>(a.plan.item)[item % items];
-    if ((unsigned)f.x >= (unsigned)c.slots) return;
-    trunk = node_of(c, a, f.x);
-    t = Columns{trunk.slot, f.y & 0xffff, trunk.cols, 0};
-    t.first *= kWide;
-    piece = (int)((unsigned)f.y >> 16);
-    if (t.first >= t.count || piece >= trunk.splits || (long)trunk.base + (long)trunk.splits * trunk.cols > a.columns) return;
-    rows = Rows{trunk.row, trunk.rows};
-    const int most = c.table_len * c.page_tokens;
-    span = span_of(c, min(max(trunk.lo, 0), most - 1), min(max(trunk.hi, 0), most - 1));
-    span.cut(max(trunk.first, 0), min(max(trunk.last, 0), c.table_len * page_blocks(c)));
-    from = max(f.z, 0);
-    to = min((span.count + 3) / 4, f.w);
+    t = Columns{trunk.node.slot, trunk.column, trunk.node.cols, 0};
+    rows = Rows{trunk.node.row, trunk.node.rows};
+    span = span_of(c, trunk.node.lo, trunk.node.hi);
+    span.cut(trunk.node.first, trunk.node.last);
+    from = trunk.from;
+    to = min((span.count + 3) / 4, trunk.to);
   } else {
     if (!columns_of(c, a, item % items, splits == 1 && c.slots <= kWave, t, rows)) return;
   }
@@ -828,14 +843,12 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
     wave_hi = __builtin_amdgcn_readfirstlane(wave_hi);
     if (lane == 0) { shared.lo[wave] = wave_lo; shared.hi[wave] = wave_hi; }
     __syncthreads();
-    lo = min(min(shared.lo[0], shared.lo[1]), min(shared.lo[2], shared.lo[3]));
-    hi = max(max(shared.hi[0], shared.hi[1]), max(shared.hi[2], shared.hi[3]));
+    lo = same(min(min(shared.lo[0], shared.lo[1]), min(shared.lo[2], shared.lo[3])));
+    hi = same(max(max(shared.hi[0], shared.hi[1]), max(shared.hi[2], shared.hi[3])));
   } else {
     lo = before + t.first / G;
     hi = before + last_col / G;
     span = span_of(c, lo, hi);
-    cut_own(a, t.slot, span);
-    node = own_of(a, t.slot).x;
     const int tiles = (span.count + 3) / 4, each = max(2, (tiles + splits - 1) / splits);
     from = split * each;
     to = min(tiles, from + each);
@@ -1164,7 +1177,8 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
   sum += __shfl_xor(sum, 32, kWave);
   if constexpr (kTrunk) {
     if (col > last_col) return;
-    const long at = head * a.columns + trunk.base + (long)piece * trunk.cols + col;
+    const long in_head = trunk.node.base + (long)trunk.piece * trunk.node.cols + col, at = head * a.columns + in_head;
+    if (trunk.node.base < 0 || in_head >= a.columns) return;
     const float unit_of_e = top.unit();
     if (from < to)
 #pragma unroll
@@ -1176,6 +1190,7 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
     if (h == 0) {
       float *tops = a.trunk + c.heads * a.columns * D;
       tops[at] = from < to ? top.s : -__builtin_inff();
+      if (trunk.only && in_head + trunk.node.cols < a.columns) tops[at + trunk.node.cols] = -__builtin_inff();
       tops[c.heads * a.columns + at] = sum * unit_of_e;
     }
     return;
@@ -1195,28 +1210,6 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
     return;
   }
   if (col > last_col) return;
-  if constexpr (kShares<Args> && !kTrunk) {
-    const float *sums = a.trunk + head * a.columns * D, *tops = a.trunk + c.heads * a.columns * D + head * a.columns, *totals = tops + c.heads * a.columns;
-    each_trunk(c, a, node, row, col % G, [&](long first, long step, int shares) {
-#pragma unroll 1
-      for (int k = 0; k < shares; ++k) {
-        const long at = first + k * step;
-        const float m = tops[at];
-        if (m == -__builtin_inff()) continue;
-        const float now = fmaxf(top.s, m), less = exp2_fast(top.s - now) * top.unit(), e = exp2_fast(m - now);
-        top = Top{now, 0.f};
-        sum = fmaf(totals[at], e, sum * less);
-#pragma unroll
-        for (int o = 0; o < OB; ++o)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f4 v = *reinterpret_cast<const f4 *>(sums + at * D + o * 32 + i * 8 + h * 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[o][4 * i + j] = fmaf(v[j], e, acc[o][4 * i + j] * less);
-          }
-      }
-    });
-  }
   const float r = 1.f / sum;
   const long to_row = (long)row * c.heads * G + q_head;
 #pragma unroll
@@ -1237,7 +1230,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
   const unsigned total = items * c.heads * splits;
   if (blockIdx.x >= total) {
     static_assert(sizeof(FewShared<D>) <= sizeof shared.tiles, "the slots of few rows work in the same LDS");
-    few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(shared.tiles));
+    if constexpr (!kShares<Args>) few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(shared.tiles));
     return;
   }
   // Where the workgroups divide by the dies, each die works through neighbouring items, head by head, and what a (slot, head) has cached stays in
@@ -1245,22 +1238,120 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
   // and short ones on another, no slower: 8191 rows, 4 heads of 8 557 and 557, 4095 rows, 2 heads of 16 150 and 150.
   unsigned id = blockIdx.x;
   if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
-  wide_item<BF16, D, false>(c, a, id, items, splits, shared);
+  wide_item<BF16, D, false>(c, a, id, items, splits, Piece(), shared);
 }
 
-// The nodes' sums.  As many workgroups as the chip holds at once; how many items there are is known on the device alone.
+// Worker w's pieces of the nodes' tiles.
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void trunk_kernel(Pages c, SharedArgs a)
+__device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, WideShared<D> &shared)
+{
+  if (!plan_holds(a)) return;
+  const Trunk all{max(same(a.plan.head[kPlanTiles]), 0), c.heads, same(a.plan.head[kPlanShift]) & 15, max(same(a.plan.head[kPlanChunk]), 1)};
+  const int nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
+  if (all.tiles == 0 || nodes == 0 || w >> all.shift) return;
+  if (all.shift >= kTrunkShift) w = (w & 7) << (all.shift - 3) | w >> 3;                 // (neighbours on one die)
+  const unsigned end = all.first(w + 1);
+  for (unsigned at = all.first(w); at < end;) {
+    Piece x;
+    x.head = same((int)(at / (unsigned)all.tiles));
+    const int in_head = (int)(at - (unsigned)x.head * all.tiles);
+    const int i = last_at(nodes, in_head, [&](int k) { return (long)a.plan.node[(long)k * kNodeInts + 8]; });
+    x.node = node_of(c, a, same(i));
+    const int in_node = in_head - x.node.tile, tall = (x.node.cols + kWide - 1) / kWide, wide_chunk = all.chunk * tall;
+    if (x.head >= c.heads || in_node < 0 || x.node.tiles == 0 || (long)in_node >= (long)tall * x.node.tiles) return;       // (no plan is like this)
+    const int k = same(in_node / wide_chunk), in_chunk = in_node - k * wide_chunk, len = min(all.chunk, x.node.tiles - k * all.chunk);
+    const int column = same(in_chunk / len), done = in_chunk - column * len;
+    x.column = column * kWide;
+    x.from = k * all.chunk + done;
+    x.to = x.from + min(len - done, (int)(end - at));
+    x.piece = 2 * k + (done > 0);
+    x.only = done == 0 && x.to == x.from + len;
+    wide_item<BF16, D, true>(c, a, 0, 0, 1, x, shared);
+    __syncthreads();
+    at += x.to - x.from;
+  }
+}
+
+// The plan's work: entries of few columns by the first workgroups, nodes by those behind them.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a, int few)
 {
   __shared__ WideShared<D> shared;
-  if (a.plan.head[kPlanRows] != a.rows) return;
-  const unsigned items = (unsigned)min(max(a.plan.head[kPlanItems], 0), a.items), total = items * c.heads;
-  for (unsigned at = blockIdx.x; at < total; at += gridDim.x) {
-    unsigned id = at;
-    if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
-    wide_item<BF16, D, true>(c, a, id, items, 1, shared);
-    __syncthreads();
+  if ((int)blockIdx.x < few) few_rows<BF16, D>(c, a, blockIdx.x, few, reinterpret_cast<FewShared<D> &>(shared.tiles));
+  else trunk_pieces<BF16, D>(c, a, blockIdx.x - few, shared);
+}
+
+// A wave joins a row's sums by one query head: those of its slot's own part, then of the nodes around it.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(Pages c, SharedArgs a)
+{
+  constexpr int E = D / kWave;                       // channels of a lane
+  const int G = c.q_per_kv, heads = c.heads * G, lane = threadIdx.x & 63;
+  const int slot = blockIdx.y, id = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / kWave));
+  const Rows rows = slot_rows(a.start, slot, a.rows);
+  const int row = rows.first + id / heads, q_head = id % heads, head = q_head / G, g = q_head - head * G;
+  if (row >= rows.first + rows.count || !plan_holds(a)) return;
+  int i = __builtin_amdgcn_readfirstlane(a.plan.slot[slot]);
+  if ((unsigned)i >= (unsigned)(3 * c.slots)) return;                  // (shares nothing)
+  const float *sums = a.trunk + (long)head * a.columns * D + lane * E, *tops = a.trunk + c.heads * a.columns * D + (long)head * a.columns;
+  const float *totals = tops + c.heads * a.columns;
+  float top = kLowest, l = 0, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0;
+  for (int upto = INT_MAX; (unsigned)i < (unsigned)(3 * c.slots);) {
+    const Node n = node_of(c, a, i);
+    const int col = (row - n.row) * G + g;
+    if (n.last >= upto || (unsigned)col >= (unsigned)n.cols) break;    // (nodes end ever earlier)
+    upto = n.last;
+    i = n.before;
+    if (n.base < 0 || n.base + (long)n.shares * n.cols > a.columns) continue;
+    for (int from = 0; from < n.shares; from += kWave) {
+      const bool there = from + lane < n.shares;
+      const long first = n.base + (long)from * n.cols + col, mine = first + (there ? (long)lane * n.cols : 0);
+      float m = tops[mine], u = totals[mine];
+      if (!there) m = -__builtin_inff();
+      float now = fmaxf(top, m);
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) now = fmaxf(now, __shfl_xor(now, d, kWave));
+      const bool some = m != -__builtin_inff();      // (no tiles, nothing written)
+      const float less = exp2_fast(top - now), f = some ? exp2_fast(m - now) : 0.f;
+      top = now;
+      u = some ? u * f : 0.f;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) u += __shfl_xor(u, d, kWave);
+      l = fmaf(l, less, u);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] *= less;
+      for (unsigned long long left = __ballot(some); left;) {          // sixteen on their way at a time
+        int at[16];
+        float v[16][E];
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          at[j] = left ? __ffsll(left) - 1 : at[0];
+          count += left != 0;
+          left &= left - 1;
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[j][e] = sums[(first + (long)at[j] * n.cols) * D + e];
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float w = j < count ? read_lane(f, at[j]) : 0.f;
+          if (j >= count) v[j][0] = v[j][E - 1] = 0;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = fmaf(v[j][e], w, x[e]);
+        }
+      }
+    }
   }
+  const float r = 1.f / l;
+  const long to = (long)row * heads + q_head;
+  if constexpr (E == 2)
+    reinterpret_cast<unsigned *>(a.out)[to * kWave + lane] =
+        (unsigned)Operand<BF16>::store(share_of(x[0], l, r)) | (unsigned)Operand<BF16>::store(share_of(x[1], l, r)) << 16;
+  else
+    reinterpret_cast<unsigned short *>(a.out)[to * kWave + lane] = Operand<BF16>::store(share_of(x[0], l, r));
+  if (a.lse && lane == 0) a.lse[to] = l == 0.f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 // Eight columns of an item to a workgroup, eight shares on their way at a time.
@@ -1304,7 +1395,6 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, Args a, unsigne
         y = fmaf(v[j].y, e, y);
       }
     }
-    if constexpr (kShares<Args>) add_trunks<D>(c, a, own_of(a, t.slot).x, head, rows.first + col / G, col % G, d, x, y, top, l);
     const float r = 1.f / l;
     const long to = (long)(rows.first + col / G) * c.heads * G + head * G + col % G;
     reinterpret_cast<unsigned *>(a.out)[to * (D / 2) + d / 2] =
@@ -1317,14 +1407,19 @@ template <bool BF16, int D, typename Args>
 hipError_t attend(const Pages &c, const Args &a, hipStream_t st)
 {
   const long pairs = (long)c.slots * c.heads;
-  if constexpr (kShares<Args>) trunk_kernel<BF16, D><<<kTrunkWorkers, 256, 0, st>>>(c, a);
-  if ((long)a.max_new * c.q_per_kv <= kCols) {
-    few_kernel<BF16, D, Args><<<few_workers(pairs), 256, 0, st>>>(c, a);
+  if constexpr (kShares<Args>) {
+    const int few = c.q_per_kv <= kCols ? kFewWorkers : 0;
+    shared_kernel<BF16, D><<<few + kTrunkWorkers, 256, 0, st>>>(c, a, few);
+    const long columns = (long)a.max_new * c.q_per_kv < kTrunkTile ? (long)a.max_new * c.q_per_kv : kTrunkTile - 1;
+    shared_join_kernel<BF16, D><<<dim3((unsigned)((columns * c.heads + 3) / 4), (unsigned)c.slots), 256, 0, st>>>(c, a);
+    if ((long)a.max_new * c.q_per_kv <= kCols) return hipGetLastError();
+  } else if ((long)a.max_new * c.q_per_kv <= kCols) {
+    few_kernel<BF16, D><<<few_workers(pairs), 256, 0, st>>>(c, a);
     return hipGetLastError();
   }
   const long items = wide_items(c.slots, c.q_per_kv, a.rows);
   const int splits = wide_splits(items * c.heads, (long)c.table_len * c.page_tokens);
-  const int few = c.q_per_kv <= kCols ? min(few_workers(pairs), kFewBeside) : 0;
+  const int few = c.q_per_kv <= kCols && !kShares<Args> ? min(few_workers(pairs), kFewBeside) : 0;
   wide_kernel<BF16, D, Args><<<(unsigned)(items * c.heads * splits + few), 256, 0, st>>>(c, a, (unsigned)items, splits);
   if (splits > 1) wide_join_kernel<BF16, D, Args><<<dim3((unsigned)(items * c.heads), kWide / kJoinColumns), 256, 0, st>>>(c, a, (unsigned)items, splits);
   return hipGetLastError();
