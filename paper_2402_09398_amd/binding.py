@@ -113,7 +113,7 @@ def lib():
         for name, args in (("reset", [ptr]), ("reserve", [ptr] * 4), ("select", [ptr] * 2), ("compact", [ptr] * 2),
                            ("copy", [ptr, i32, ptr]), ("append", [i32, ptr, ptr, C.c_int64, ptr, i32, ptr]),
                            ("attend", [i32, ptr, C.c_int64, ptr, ptr, ptr, i32, i32, ptr]),
-                           ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr]), ("share", [ptr, i32, ptr, ptr]),
+                           ("read", [i32, ptr, i32, i32, i32, ptr, ptr, ptr]), ("share", [ptr, i32, C.c_int64, ptr, ptr]),
                            ("attend_shared", [i32, ptr, C.c_int64, ptr, ptr, ptr, i32, i32, ptr, ptr])):
             f = getattr(L, "lessdec_pages_" + name)
             f.restype, f.argtypes = C.c_int, [C.POINTER(PagesDesc)] + args

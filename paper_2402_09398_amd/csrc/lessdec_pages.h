@@ -134,17 +134,18 @@ hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, h
 //        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
 //        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
 //  few   [4 slots][2]: steps, slot (that shares nothing) or slots + node, of up to kFewColumns columns
-//  slot  [slots]: the node that is its own part (-1: it shares nothing)
+//  chain [slots][kTrunkDepth + 1][4]: of its own node and those around it, the first column of the plan that is its first row's, columns from a share to
+//        the next, shares (0: no more nodes; with -1 in the first the slot is not in any, and an entry of few or of 128 columns and more)
 //  pos   [rows]: positions of the rows
 //  apart [slots]: scratch
 // A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
 constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanShift = 4, kPlanChunk = 5, kPlanHead = 8, kNodeInts = 12, kEndless = 1 << 30;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
 constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
-constexpr int kTrunkShift = 8, kTrunkLong = 14;      // 256 workers, one to a compute unit; two from so many tiles on that each of them then has
+constexpr int kTrunkShift = 8, kTrunkLong = 4;       // 256 workers, one to a compute unit; two from so many tiles on that each of them then has
 constexpr int kTrunkWorkers = 2 << kTrunkShift, kFewWorkers = 256;     // workgroups of the launch
 struct Plan {
-  int *head, *node, *few, *slot, *apart, *pos;
+  int *head, *node, *chain, *few, *apart, *pos;
 };
 // The tiles of all heads and nodes, one behind the other, are dealt out evenly: worker w has [first(w), first(w + 1)).  Within a node and head
 // they are ordered by chunks of tokens, in a chunk by tiles of 128 columns, so that neighbouring workers read the same tokens at the same time.  A
@@ -173,15 +174,21 @@ inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
   const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
   return 2 * (kTrunkDepth + 1) * (n < most ? n : most) + 4L * kTrunkTile * (kTrunkWorkers / heads + 1);
 }
-inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (3 * kNodeInts + 8 + 2) + rows; }
+// tiles of all heads and nodes, at most
+inline double plan_tiles(int slots, int heads, int q_per_kv, long rows, long tokens)
+{
+  const double n = (double)rows * q_per_kv, most = (double)slots * kTrunkTile;
+  return heads * ((kTrunkDepth + 1) * (n < most ? n : most) / kTrunkTile + 2.0 * slots) * (tokens / 64 + 1);
+}
+inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (3 * kNodeInts + 4 * (kTrunkDepth + 1) + 8 + 1) + rows; }
 inline Plan plan_at(int *p, int slots)
 {
   Plan x;
   x.head = p;
   x.node = x.head + kPlanHead;                       // (16-byte aligned)
-  x.few = x.node + 3L * slots * kNodeInts;
-  x.slot = x.few + 8L * slots;
-  x.apart = x.slot + slots;
+  x.chain = x.node + 3L * slots * kNodeInts;
+  x.few = x.chain + 4L * (kTrunkDepth + 1) * slots;
+  x.apart = x.few + 8L * slots;
   x.pos = x.apart + slots;
   return x;
 }
@@ -191,7 +198,7 @@ struct SharedArgs : AttendArgs {
   long columns;
 };
 hipError_t launch_pages_attend_shared(const Pages &c, int dtype, const SharedArgs &a, hipStream_t st);
-hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, long columns, hipStream_t st);
+hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, long columns, long least_bytes, hipStream_t st);
 
 // floats of AttendArgs::parts for up to `rows` rows
 size_t pages_attend_floats(int slots, int heads, int q_per_kv, int head_dim, long tokens, int rows);

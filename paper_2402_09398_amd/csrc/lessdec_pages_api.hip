@@ -94,6 +94,11 @@ bool rows_ok(const Pages &c, int rows)
   return rows >= 0 && (long)rows * c.q_per_kv < 1L << 31 && ((long)rows * c.q_per_kv / 128 + c.slots) * c.heads <= 1L << 30;
 }
 
+bool tiles_ok(const Pages &c, int rows)
+{
+  return plan_tiles(c.slots, c.heads, c.q_per_kv, rows, (long)c.table_len * c.page_tokens) < 0x1p31;
+}
+
 }  // namespace
 
 extern "C" {
@@ -171,15 +176,16 @@ size_t lessdec_pages_shared_workspace_bytes(const lessdec_pages_desc *desc, int3
   return !shape_ok(desc) || max_rows < 0 ? 0 : shared_workspace_for(desc, max_rows);
 }
 
-int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, int32_t rows, int32_t *plan, void *hip_stream)
+int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, int32_t rows, int64_t least_bytes, int32_t *plan, void *hip_stream)
 {
   Pages c;
   const int rc = check(desc, 0, 0, 0, &c);
   if (rc) return rc;
-  if (!rows_ok(c, rows)) return LESSDEC_EINVAL;
+  if (!rows_ok(c, rows) || !tiles_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0) return LESSDEC_OK;
   if (!start || !plan || !aligned(start, 4) || !aligned(plan, 16) || plan == start || plan == desc->table || plan == desc->length) return LESSDEC_EINVAL;
-  return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots), plan_columns(c.slots, c.heads, c.q_per_kv, rows), (hipStream_t)hip_stream));
+  return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots), plan_columns(c.slots, c.heads, c.q_per_kv, rows), least_bytes,
+                                   (hipStream_t)hip_stream));
 }
 
 int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, const void *q, int64_t stride, void *out, float *lse, const int32_t *start,
@@ -189,7 +195,7 @@ int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, c
   const int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
-  if (step < 0 || max_new < 0 || !rows_ok(c, rows)) return LESSDEC_EINVAL;
+  if (step < 0 || max_new < 0 || !rows_ok(c, rows) || !tiles_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0 || max_new == 0) return LESSDEC_OK;
   if (!desc->workspace || !aligned(desc->workspace, 256) || desc->workspace_bytes < shared_workspace_for(desc, rows)) return LESSDEC_EWORKSPACE;
   if (!q || !out || !start || !plan || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4) || !aligned(plan, 16)) return LESSDEC_EINVAL;

@@ -254,10 +254,10 @@ __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
 // where slots share pages, entries of the plan: slots that share nothing, and nodes of few columns
 __device__ inline int steps_of(const Pages &c, const SharedArgs &a, int i)
 {
-  return plan_holds(a) ? min(max(a.plan.few[2L * i], 0), c.table_len * page_blocks(c) / kStepBlocks + 1) : steps_of(c, static_cast<const AttendArgs &>(a), i);
+  return min(max(a.plan.few[2L * i], 0), c.table_len * page_blocks(c) / kStepBlocks + 1);
 }
 __device__ inline int few_entries(const Pages &c, const AttendArgs &) { return c.slots; }
-__device__ inline int few_entries(const Pages &c, const SharedArgs &a) { return plan_holds(a) ? min(max(same(a.plan.head[kPlanFew]), 0), 4 * c.slots) : c.slots; }
+__device__ inline int few_entries(const Pages &c, const SharedArgs &a) { return min(max(same(a.plan.head[kPlanFew]), 0), 4 * c.slots); }
 
 // Worker w's part [begin, end) of the steps, and where it begins: slot, and step among the slot's (head by head).
 struct Part {
@@ -436,13 +436,12 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     Span span;
     Node node;
     bool is_node = false;
-    if constexpr (kShares<Args>)
-      if (plan_holds(a)) {
-        const int i = same(a.plan.few[2L * s + 1]);
-        is_node = i >= c.slots;
-        if (is_node) node = node_of(c, a, min(i - c.slots, 3 * c.slots - 1));
-        else read = max(i, 0);
-      }
+    if constexpr (kShares<Args>) {
+      const int i = same(a.plan.few[2L * s + 1]);
+      is_node = i >= c.slots;
+      if (is_node) node = node_of(c, a, min(i - c.slots, 3 * c.slots - 1));
+      else read = max(i, 0);
+    }
     if (!is_node) {
       rows = slot_rows(a.start, read, a.rows);
       const int len = slot_length(c, read);
@@ -739,9 +738,8 @@ constexpr int wide_floats(int D) { return kWide * (D + 2); }
 // which leaves each as many as it can have.  32 slots of 537 to 4096 tokens, 8 heads: 201 us, as the slots are 247; 64 slots of 2048: 204 and
 // 233; 4 slots of 4096: 830 and 816.  Split tiles have a second launch that would do all of this again: 64 slots, 24 us as they are, 30 in order.
 struct Columns { int slot, first, count, len; };     // first column, columns of the slot in all; its tokens
-// where slots share pages, those that share nothing are what is left to wide_kernel
-__device__ inline bool shares(const AttendArgs &, int) { return false; }
-__device__ inline bool shares(const SharedArgs &a, int s) { return plan_holds(a) && a.plan.slot[s] >= 0; }
+// (where slots share pages, those of 128 columns and more are what is left to wide_kernel)
+template <typename Args> constexpr int kLeast = kShares<Args> ? kTrunkTile : kCols + 1;
 template <typename Args> __device__ inline bool columns_of(const Pages &c, const Args &a, int x, bool sorted, Columns &t, Rows &rows)
 {
   const int G = c.q_per_kv, lane = threadIdx.x & 63;
@@ -749,7 +747,7 @@ template <typename Args> __device__ inline bool columns_of(const Pages &c, const
   if (sorted) {
     const int s = min(lane, c.slots - 1);
     const Rows r = slot_rows(a.start, s, a.rows);
-    const int len = slot_length(c, s), n = lane < c.slots && r.count * G > kCols && !shares(a, s) ? (r.count * G + kWide - 1) / kWide : 0;
+    const int len = slot_length(c, s), n = lane < c.slots && r.count * G >= kLeast<Args> ? (r.count * G + kWide - 1) / kWide : 0;
     const int seen = c.window > 0 ? min(len, min(c.window, len) + r.count) : len;
     const int key = (seen / kTile << 6) + 63 - lane;   // tokens that a tile sees, in tiles; ties as the slots are
     int before = 0;
@@ -776,7 +774,7 @@ template <typename Args> __device__ inline bool columns_of(const Pages &c, const
   }
   t.count = rows.count * G;
   const int n = (t.count + kWide - 1) / kWide;
-  if (i < 0 || i >= n || t.count <= kCols || shares(a, t.slot)) return false;               // (i < 0: before the first slot's rows)
+  if (i < 0 || i >= n || t.count < kLeast<Args>) return false;               // (i < 0: before the first slot's rows)
   t.slot = __builtin_amdgcn_readfirstlane(t.slot);
   t.count = __builtin_amdgcn_readfirstlane(t.count);
   t.len = __builtin_amdgcn_readfirstlane(t.len);
@@ -916,6 +914,17 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
       kc[j] = *(Pieces)(k + (unsigned)(half * kWave + lane) * 16);
       vc[j] = *(Pieces)(v + (unsigned)(half * kWave + lane) * 16);
     }
+  };
+  // A node's tokens are in no L2 yet: a word of every line of the tile that comes kAhead later is read, so that they are when it is requested (a
+  // wave has a block: sixteen lines of 16 D / 128 keys each, and as many of values).
+  constexpr int kAhead = 5;
+  unsigned touched = 0, touching = 0;
+  auto touch = [&](int tile) {
+    const int block = max(at_of(min(tile, to - 1), wave), 0);
+    constexpr int kLines = kBlock * D / 128;
+    const unsigned char *line = ((lane & kLines) ? c.v : c.k) + block * ((long)kBlock * D) + (unsigned)(lane % kLines) * 128;
+    touched |= touching;                             // (the one before is waited for here, a tile later)
+    touching = *reinterpret_cast<const unsigned *>(line);
   };
   // where a word of four tokens' codes of channel 64 half + 16 i + (lane & 15) goes: [block][32 channels][which eight of the 16
   // tokens][channel], tokens 0-3 and 8-11, or 4-7 and 12-15
@@ -1110,6 +1119,7 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
       stage(tile + 1, buf ^ 1);
       request(tile + 2);
     }
+    if constexpr (kTrunk) touch(tile + kAhead);
     if (active) {
       // products before the other workgroup's staging: 661 -> 621 us at 32 heads x 8192 tokens, clocks settled
       __builtin_amdgcn_s_setprio(1);
@@ -1140,6 +1150,7 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
     }
   }
 
+  if constexpr (kTrunk) asm volatile("" :: "v"(touched));
   if (mine_spoiled) spoiled = 1;
   __syncthreads();
   if (spoiled)                                       // the NaN that were taken out, counted for the rows that see them
@@ -1227,6 +1238,8 @@ template <bool BF16, int D, typename Args>
 __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned items, int splits)
 {
   __shared__ WideShared<D> shared;
+  if constexpr (kShares<Args>)
+    if (!plan_holds(a)) return;
   const unsigned total = items * c.heads * splits;
   if (blockIdx.x >= total) {
     static_assert(sizeof(FewShared<D>) <= sizeof shared.tiles, "the slots of few rows work in the same LDS");
@@ -1245,7 +1258,6 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
 template <bool BF16, int D>
 __device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, WideShared<D> &shared)
 {
-  if (!plan_holds(a)) return;
   const Trunk all{max(same(a.plan.head[kPlanTiles]), 0), c.heads, same(a.plan.head[kPlanShift]) & 15, max(same(a.plan.head[kPlanChunk]), 1)};
   const int nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
   if (all.tiles == 0 || nodes == 0 || w >> all.shift) return;
@@ -1277,75 +1289,81 @@ template <bool BF16, int D>
 __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a, int few)
 {
   __shared__ WideShared<D> shared;
+  if (!plan_holds(a)) return;
   if ((int)blockIdx.x < few) few_rows<BF16, D>(c, a, blockIdx.x, few, reinterpret_cast<FewShared<D> &>(shared.tiles));
   else trunk_pieces<BF16, D>(c, a, blockIdx.x - few, shared);
 }
 
-// A wave joins a row's sums by one query head: those of its slot's own part, then of the nodes around it.
+// A wave joins a row's sums by one query head: those of its slot's own part and of the nodes around it, a lane a share.
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(Pages c, SharedArgs a)
 {
-  constexpr int E = D / kWave;                       // channels of a lane
+  constexpr int E = D / kWave, kNodes = kTrunkDepth + 1;               // channels of a lane
   const int G = c.q_per_kv, heads = c.heads * G, lane = threadIdx.x & 63;
-  const int slot = blockIdx.y, id = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / kWave));
+  const int slot = blockIdx.y, id = same((int)(blockIdx.x * 4 + threadIdx.x / kWave));
   const Rows rows = slot_rows(a.start, slot, a.rows);
-  const int row = rows.first + id / heads, q_head = id % heads, head = q_head / G, g = q_head - head * G;
-  if (row >= rows.first + rows.count || !plan_holds(a)) return;
-  int i = __builtin_amdgcn_readfirstlane(a.plan.slot[slot]);
-  if ((unsigned)i >= (unsigned)(3 * c.slots)) return;                  // (shares nothing)
-  const float *sums = a.trunk + (long)head * a.columns * D + lane * E, *tops = a.trunk + c.heads * a.columns * D + (long)head * a.columns;
-  const float *totals = tops + c.heads * a.columns;
+  int4 chain[kNodes];
+#pragma unroll
+  for (int d = 0; d < kNodes; ++d) chain[d] = reinterpret_cast<const int4 *>(a.plan.chain)[(long)kNodes * slot + d];
+  const int in_slot = id / heads, q_head = id - in_slot * heads, head = q_head / G, g = q_head - head * G;
+  if (in_slot >= rows.count || !plan_holds(a) || chain[0].x < 0) return;
+  int upto[kNodes];                                  // shares of the nodes so far
+#pragma unroll
+  for (int d = 0; d < kNodes; ++d) {
+    const long last = (long)max(chain[d].x, 0) + (long)max(chain[d].y, 0) * max(chain[d].z - 1, 0) + in_slot * G + g;
+    upto[d] = (d ? upto[d - 1] : 0) + (last < a.columns ? max(chain[d].z, 0) : 0);
+  }
+  const float *tops = a.trunk + c.heads * a.columns * D + (long)head * a.columns, *totals = tops + c.heads * a.columns;
+  const float *sums = a.trunk + (long)head * a.columns * D + lane * E;
   float top = kLowest, l = 0, x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0;
-  for (int upto = INT_MAX; (unsigned)i < (unsigned)(3 * c.slots);) {
-    const Node n = node_of(c, a, i);
-    const int col = (row - n.row) * G + g;
-    if (n.last >= upto || (unsigned)col >= (unsigned)n.cols) break;    // (nodes end ever earlier)
-    upto = n.last;
-    i = n.before;
-    if (n.base < 0 || n.base + (long)n.shares * n.cols > a.columns) continue;
-    for (int from = 0; from < n.shares; from += kWave) {
-      const bool there = from + lane < n.shares;
-      const long first = n.base + (long)from * n.cols + col, mine = first + (there ? (long)lane * n.cols : 0);
-      float m = tops[mine], u = totals[mine];
-      if (!there) m = -__builtin_inff();
-      float now = fmaxf(top, m);
+  for (int from = 0; from < upto[kNodes - 1]; from += kWave) {
+    const int k = from + lane;
+    int column = max(chain[0].x, 0) + k * chain[0].y;
 #pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) now = fmaxf(now, __shfl_xor(now, d, kWave));
-      const bool some = m != -__builtin_inff();      // (no tiles, nothing written)
-      const float less = exp2_fast(top - now), f = some ? exp2_fast(m - now) : 0.f;
-      top = now;
-      u = some ? u * f : 0.f;
+    for (int d = 1; d < kNodes; ++d)
+      if (k >= upto[d - 1]) column = max(chain[d].x, 0) + (k - upto[d - 1]) * chain[d].y;
+    const bool there = k < upto[kNodes - 1];
+    column = there ? column + in_slot * G + g : 0;
+    float m = tops[column], u = totals[column];
+    if (!there) m = -__builtin_inff();
+    float now = fmaxf(top, m);
 #pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) u += __shfl_xor(u, d, kWave);
-      l = fmaf(l, less, u);
+    for (int d = 1; d < kWave; d <<= 1) now = fmaxf(now, __shfl_xor(now, d, kWave));
+    const bool some = m != -__builtin_inff();        // (no tiles, nothing written)
+    const float less = exp2_fast(top - now), f = some ? exp2_fast(m - now) : 0.f;
+    top = now;
+    u = some ? u * f : 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] *= less;
-      for (unsigned long long left = __ballot(some); left;) {          // sixteen on their way at a time
-        int at[16];
-        float v[16][E];
-        int count = 0;
+    for (int d = 1; d < kWave; d <<= 1) u += __shfl_xor(u, d, kWave);
+    l = fmaf(l, less, u);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          at[j] = left ? __ffsll(left) - 1 : at[0];
-          count += left != 0;
-          left &= left - 1;
+    for (int e = 0; e < E; ++e) x[e] *= less;
+    for (unsigned long long left = __ballot(some); left;) {            // sixteen on their way at a time
+      int at[16];
+      float v[16][E];
+      int count = 0;
 #pragma unroll
-          for (int e = 0; e < E; ++e) v[j][e] = sums[(first + (long)at[j] * n.cols) * D + e];
-        }
+      for (int j = 0; j < 16; ++j) {
+        at[j] = left ? __ffsll(left) - 1 : at[0];
+        count += left != 0;
+        left &= left - 1;
+        const float *p = sums + (long)__builtin_amdgcn_readlane(column, at[j]) * D;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float w = j < count ? read_lane(f, at[j]) : 0.f;
-          if (j >= count) v[j][0] = v[j][E - 1] = 0;
+        for (int e = 0; e < E; ++e) v[j][e] = p[e];
+      }
 #pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = fmaf(v[j][e], w, x[e]);
-        }
+      for (int j = 0; j < 16; ++j) {
+        const float w = j < count ? read_lane(f, at[j]) : 0.f;
+        if (j >= count) v[j][0] = v[j][E - 1] = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(v[j][e], w, x[e]);
       }
     }
   }
   const float r = 1.f / l;
-  const long to = (long)row * heads + q_head;
+  const long to = (long)(rows.first + in_slot) * heads + q_head;
   if constexpr (E == 2)
     reinterpret_cast<unsigned *>(a.out)[to * kWave + lane] =
         (unsigned)Operand<BF16>::store(share_of(x[0], l, r)) | (unsigned)Operand<BF16>::store(share_of(x[1], l, r)) << 16;
@@ -1364,6 +1382,8 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, Args a, unsigne
   const int head = item / items;
   Columns t;
   Rows rows;
+  if constexpr (kShares<Args>)
+    if (!plan_holds(a)) return;
   if (!columns_of(c, a, item % items, false, t, rows)) return;
   const float *base = a.parts + few_floats(G, D) + (long)item * splits * wide_floats(D);
   for (int i = threadIdx.x; i < kJoinColumns * (D / 2); i += 256) {
@@ -1412,7 +1432,7 @@ hipError_t attend(const Pages &c, const Args &a, hipStream_t st)
     shared_kernel<BF16, D><<<few + kTrunkWorkers, 256, 0, st>>>(c, a, few);
     const long columns = (long)a.max_new * c.q_per_kv < kTrunkTile ? (long)a.max_new * c.q_per_kv : kTrunkTile - 1;
     shared_join_kernel<BF16, D><<<dim3((unsigned)((columns * c.heads + 3) / 4), (unsigned)c.slots), 256, 0, st>>>(c, a);
-    if ((long)a.max_new * c.q_per_kv <= kCols) return hipGetLastError();
+    if ((long)a.max_new * c.q_per_kv < kTrunkTile) return hipGetLastError();
   } else if ((long)a.max_new * c.q_per_kv <= kCols) {
     few_kernel<BF16, D><<<few_workers(pairs), 256, 0, st>>>(c, a);
     return hipGetLastError();

@@ -97,6 +97,8 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 // A node is worth its shares and their joining from so many tokens on, that it saves reading (tokens that it has, times slots but one).
 constexpr int kLeastSaved = 256;
+// All of them together are worth it from so many bytes on that are not read.
+constexpr long kLeastBytes = 32L << 20;
 
 // Blocks that rows at lo .. hi see some token of, of those in [first, last).
 __device__ inline int seen_blocks(const Pages &c, int lo, int hi, int first, int last)
@@ -121,10 +123,11 @@ struct Runs {
 };
 constexpr int kRunBytes = 4 * sizeof(int) + 8 * sizeof(short);
 
-__global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *start, int rows, Plan plan, long most_columns)
+__global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *start, int rows, Plan plan, long most_columns, long least_bytes)
 {
   extern __shared__ int shared[];
   __shared__ long sums[2][kWaves];
+  __shared__ unsigned long long saved_in_all;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = c.slots, per = page_blocks(c), G = c.q_per_kv;
   Runs r;
   r.a = shared; r.hi = r.a + N; r.row = r.hi + N; r.rows = r.row + N;
@@ -152,6 +155,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     return before;
   };
 
+  if (tid == 0) saved_in_all = 0;
   int n = 0;
   for (int base = 0; base < N; base += kThreads) {
     const int s = base + tid;
@@ -161,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (s < N) {
       x = sharer_of(c, start, rows, s);
       same = plan.apart[s];
-      plan.slot[s] = -1;
+      *reinterpret_cast<int4 *>(plan.chain + 4L * (kTrunkDepth + 1) * s) = make_int4(-1, 0, 0, 0);
     }
     int all;
     const int at = n + scan((int)(x.rows.count > 0), all);
@@ -221,10 +225,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     const long saved = (long)seen_blocks(c, lo, hi, from * per, r.a[k] * per) * kBlock * (e - l - 1);
     if (lane == 0) {
       if (from > 0) r.around[k] = r.same[r.a[l] >= below ? l : e];
-      r.worth[k] = saved >= kLeastSaved;
+      r.worth[k] = saved >= (least_bytes < 0 ? kLeastSaved : 1);
+      if (r.worth[k]) atomicAdd(&saved_in_all, (unsigned long long)saved);
     }
   }
   __syncthreads();
+  const bool none = saved_in_all * (2ull * c.heads * c.head_dim) < (unsigned long long)(least_bytes < 0 ? kLeastBytes : least_bytes);
   // the outermost kTrunkDepth of the nodes around a slot are kept
   int nodes = 0;
   for (int base = 0; base < n; base += kThreads) {
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       int past = max(depth - kTrunkDepth, 0);
       for (int i = r.around[k]; i >= 0; i = r.around[i])
         if (r.worth[i] && past-- == 0) { r.near[k] = (short)i; break; }
-      keep = r.worth[k] && depth < kTrunkDepth;
+      keep = !none && r.worth[k] && depth < kTrunkDepth;
     }
     int all;
     const int at = nodes + scan((int)keep, all);
@@ -267,15 +273,18 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       i = r.same[k + 1 < n && r.a[k + 1] > r.a[k] ? k + 1 : k];
       if (i >= 0 && r.index[i] < 0) i = r.near[i];
     }
+    if (none) i = -1;
+    // one that shares nothing has a node all the same if its columns are too many for the list of few and too few for tiles of its own
+    const int columns = k < n ? r.rows[k] * G : 0;
+    const bool own = i >= 0 || (columns > kFewColumns && columns < kTrunkTile);
     int all;
-    const int at = all_nodes + scan((int)(i >= 0), all);
-    if (i >= 0) {
-      record(at, r.slot[k], r.row[k], r.rows[k], lo_of(k), r.hi[k], r.a[i] * per, kEndless, r.index[i]);
-      plan.slot[r.slot[k]] = at;
+    const int at = all_nodes + scan((int)own, all);
+    if (own) {
+      record(at, r.slot[k], r.row[k], r.rows[k], lo_of(k), r.hi[k], i >= 0 ? r.a[i] * per : 0, kEndless, i >= 0 ? r.index[i] : -1);
+      plan.chain[4L * (kTrunkDepth + 1) * r.slot[k] + 3] = at;
     }
     all_nodes += all;
-    // slots that share nothing are on the list of few columns as themselves
-    const bool direct = k < n && i < 0 && r.rows[k] * G <= kFewColumns;
+    const bool direct = k < n && !own && columns <= kFewColumns;
     const int to = few + scan((int)direct, all);
     if (direct) {
       const int steps = (seen_blocks(c, lo_of(k), r.hi[k], 0, kEndless) + kFewBlocks - 1) / kFewBlocks;
@@ -312,8 +321,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   // columns: as many times a node's as workgroups may have a piece of it
-  const bool holds = tiles * c.heads < 1L << 31;     // (a table that has more names one page over and over: counts as not shared)
-  const Trunk trunk = Trunk::of(holds ? (int)tiles : 0, c.heads);
+  const Trunk trunk = Trunk::of((int)tiles, c.heads);
   long columns = 0;
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
@@ -323,15 +331,36 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     const long at = columns + scan(i < all_nodes ? pieces * f[2] * G : 0, all);
     if (i < all_nodes) {
       f[10] = at + (long)pieces * f[2] * G <= most_columns ? (int)at : -1;
-      f[11] = pieces;
+      f[11] = f[10] >= 0 ? pieces : 0;
     }
     columns += all;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  // what a slot's rows are joined from
+  for (int k = tid; k < n; k += kThreads) {
+    int4 *chain = reinterpret_cast<int4 *>(plan.chain) + (kTrunkDepth + 1L) * r.slot[k];
+    const int columns = r.rows[k] * G;
+    int i = r.same[k + 1 < n && r.a[k + 1] > r.a[k] ? k + 1 : k];
+    if (i >= 0 && r.index[i] < 0) i = r.near[i];
+    if (none) i = -1;
+    if (i < 0 && (columns <= kFewColumns || columns >= kTrunkTile)) continue;
+    int node = chain[0].w;
+    for (int d = 0; d <= kTrunkDepth; ++d) {
+      int4 x = make_int4(0, 0, 0, 0);
+      if (node >= 0) {
+        const int *f = plan.node + (long)node * kNodeInts;
+        x = make_int4(f[10] + (r.row[k] - f[1]) * G, f[2] * G, f[11], 0);
+        node = f[7];
+      }
+      chain[d] = x;
+    }
   }
   if (tid == 0) {
     plan.head[kPlanNodes] = all_nodes;
     plan.head[kPlanTiles] = (int)tiles;
     plan.head[kPlanFew] = few;
-    plan.head[kPlanRows] = holds ? rows : -1;
+    plan.head[kPlanRows] = rows;
     plan.head[kPlanShift] = trunk.shift;
     plan.head[kPlanChunk] = trunk.chunk;
   }
@@ -339,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
 
 }  // namespace
 
-hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, long columns, hipStream_t st)
+hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const Plan &plan, long columns, long least_bytes, hipStream_t st)
 {
   agree_kernel<<<(c.slots + 3) / 4, 256, 0, st>>>(c, start, rows, plan);
   const size_t lds = (size_t)c.slots * kRunBytes;
@@ -347,7 +376,7 @@ hipError_t launch_pages_share(const Pages &c, const int *start, int rows, const 
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(plan_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  plan_kernel<<<1, kThreads, lds, st>>>(c, start, rows, plan, columns);
+  plan_kernel<<<1, kThreads, lds, st>>>(c, start, rows, plan, columns, least_bytes);
   return hipGetLastError();
 }
 

@@ -53,8 +53,8 @@ def lessdec_pages_shared_workspace_bytes(desc: PagesDesc, max_rows: int) -> int:
     return int(lib().lessdec_pages_shared_workspace_bytes(C.byref(desc), int(max_rows)))
 
 
-def lessdec_pages_share(desc: PagesDesc, start, rows: int, plan, stream=None):
-    _check(lib().lessdec_pages_share(C.byref(desc), _p(start), rows, _p(plan), _stream(stream)), "lessdec_pages_share")
+def lessdec_pages_share(desc: PagesDesc, start, rows: int, least_bytes: int, plan, stream=None):
+    _check(lib().lessdec_pages_share(C.byref(desc), _p(start), rows, least_bytes, _p(plan), _stream(stream)), "lessdec_pages_share")
 
 
 def lessdec_pages_attend_shared(desc: PagesDesc, layer: int, q, q_stride: int, out, lse, start, rows: int, max_new: int, plan, stream=None):
@@ -206,9 +206,11 @@ class PagedCache:
             raise LessdecError(f"share: {rows} rows exceed max_rows={self.max_rows} the workspace was sized for")
         return self._ints(plan, lessdec_pages_share_ints(self.desc, rows), "plan")
 
-    def share(self, start, rows, plan, stream=None):
-        """What neighbouring slots have in common, for attend_shared() calls of `rows` rows; holds until slots, lengths or start change."""
-        self._call("lessdec_pages_share", stream, self._ints(start, self.slots + 1, "start"), rows, self._plan(plan, rows))
+    def share(self, start, rows, plan, least_bytes=-1, stream=None):
+        """What neighbouring slots have in common, for attend_shared() calls of `rows` rows; holds until slots, lengths or start change.
+        Nothing is shared if that saves less than least_bytes of a layer's reading (-1: than has been measured to pay)."""
+        self._call("lessdec_pages_share", stream, self._ints(start, self.slots + 1, "start"), rows, least_bytes,
+                   self._plan(plan, rows))
 
     def attend_shared(self, layer, q, out, start, max_new, plan, lse=None, stream=None):
         """attend() that reads what slots share once for all of them; plan: of share() for these rows."""

@@ -24,14 +24,28 @@ class Shared(Pair):
         """Every slot's own part (-1: it shares nothing), and (row, rows, first block, last, node before, tiles, has few columns) of every node."""
         slots, plan = self.ref.slots, self.sharing.cpu().numpy()
         node = plan[8:8 + 36 * slots].reshape(-1, 12)[:plan[0]]
-        slot = plan[8 + 44 * slots:][:slots]
+        chain = plan[8 + 36 * slots:][:16 * slots].reshape(-1, 4, 4)
+        slot = [-1] * slots
+        for i, f in enumerate(node):
+            if f[6] == 1 << 30:
+                slot[f[0]] = i
+        for s in range(slots):                                # first columns, columns and shares of its nodes
+            at = slot[s]
+            if at < 0:
+                assert chain[s, 0, 0] == -1
+                continue
+            row = node[at][1]
+            for x in chain[s]:
+                want = (node[at][10] + (row - node[at][1]) * self.ref.group, node[at][2] * self.ref.group, node[at][11]) if at >= 0 else (0, 0, 0)
+                assert tuple(x[:3]) == want
+                at = node[at][7] if at >= 0 else -1
         return slot, [tuple(int(x) for x in (f[1], f[2], f[5], f[6], f[7], f[9], f[11])) for f in node]
 
-    def share(self, counts, behind=2):
+    def share(self, counts, behind=2, least=0):
         """The plan for these rows, looked over; the nodes of several slots."""
         r, start = self.ref, np.concatenate([[0], np.cumsum(counts)])
         self.sharing.fill_(-5)
-        self.own.share(self.ints(start), int(start[-1]) + behind, self.sharing)
+        self.own.share(self.ints(start), int(start[-1]) + behind, self.sharing, least_bytes=least)
         slot, nodes = self.nodes()
         per, several = r.page // 16, [n for n in nodes if n[3] < 1 << 30]
         assert nodes[:len(several)] == several
@@ -50,10 +64,10 @@ class Shared(Pair):
         own = set()
         for s in range(r.slots):
             if counts[s] == 0 or slot[s] < 0:
-                assert slot[s] == -1
+                assert slot[s] == -1 and not 16 < counts[s] * r.group < 128
                 continue
             row, rows, first, last, at, *_ = nodes[slot[s]]
-            assert slot[s] >= len(several) and slot[s] not in own and (row, rows, last) == (start[s], counts[s], 1 << 30) and at >= 0
+            assert slot[s] >= len(several) and slot[s] not in own and (row, rows, last) == (start[s], counts[s], 1 << 30) and (at >= 0 or first == 0)
             own.add(slot[s])
             while at >= 0:
                 assert nodes[at][3] == first
@@ -175,6 +189,21 @@ def test_sharing_that_deepens_slot_by_slot():
     p.attend_shared([1] * 8)
 
 
+def test_what_pays():
+    """Nothing is shared if that saves too little: slots of few columns are attended to as they are, others as nodes without one around them."""
+    for group in (2, 5, 40):
+        p = Shared(5, 60, 16, 20, 2, 64, "f16", q_per_kv=group)
+        prompt(p, 160, range(5))
+        p.room([1, 20, 3, 40, 5])
+        saved = 160 * 4 * 2 * 2 * 64
+        for rows in ([1] * 5, [1, 3, 0, 9, 2]):
+            for least in (-1, saved + 1):
+                assert not p.share(rows, least=least)
+                p.attend_shared(rows)
+        assert p.share([1] * 5, least=saved)
+        p.attend_shared([1] * 5)
+
+
 def test_many_slots():
     for slots, group in ((70, 1), (300, 2), (1100, 1)):
         p = Shared(slots, slots * 2 + 60, 16, 14, 1, 64, "f16", q_per_kv=group)
@@ -219,14 +248,17 @@ def test_what_a_row_does_not_see_does_not_reach_it():
 
 
 def test_plans_of_other_rows_and_other_contents():
-    """A plan for another number of rows counts as none; whatever a plan holds, nothing outside the arrays is touched and the call ends."""
+    """With a plan for another number of rows, or an empty one, nothing is written."""
     p = Shared(6, 80, 16, 20, 2, 64, "f16", q_per_kv=4)
     prompt(p, 200, range(6))
     p.room([1, 2, 3, 4, 5, 6])
     p.share([1] * 6)
-    p.attend_shared([1, 2, 3, 1, 1, 1])
+    q = p.t.zeros(11, 8, 64, dtype=p.t.float16, device="cuda")
+    out = p.t.full_like(q, 3.5)
+    p.own.attend_shared(0, q, out, p.ints([0, 1, 3, 6, 7, 8, 9]), 3, p.sharing)
     p.sharing.zero_()
-    p.attend_shared([1] * 6)
+    p.own.attend_shared(0, q, out, p.ints([0, 1, 3, 6, 7, 8, 9]), 3, p.sharing)
+    assert (out == 3.5).all()
     p.share([1] * 6)
     p.attend_shared([1] * 6)
 
@@ -247,7 +279,7 @@ def test_a_captured_step():
     def step():
         p.own.reserve(one, None, plan)
         p.own.copy(plan, slots)
-        p.own.share(start, slots, p.sharing)
+        p.own.share(start, slots, p.sharing, least_bytes=0)
         for layer in range(2):
             p.own.append(layer, k, v, start)
             p.own.attend_shared(layer, q, outs[layer], start, 1, p.sharing)
@@ -283,10 +315,10 @@ def test_rows_of_another_stream_and_wrong_tensors():
     out, out2 = torch.empty_like(q), torch.empty_like(q)
     start = p.ints(np.arange(5))
     side.wait_stream(torch.cuda.current_stream())
-    p.own.share(start, 4, p.sharing, stream=side)
+    p.own.share(start, 4, p.sharing, least_bytes=0, stream=side)
     p.own.attend_shared(0, q, out, start, 1, p.sharing, stream=side)
     side.synchronize()
-    p.own.share(start, 4, p.sharing)
+    p.own.share(start, 4, p.sharing, least_bytes=0)
     p.own.attend_shared(0, q, out2, start, 1, p.sharing)
     assert torch.equal(out, out2)
     bare = PagedCache(4, 60, 16, 16, 1, 128, "f16", q_per_kv=2, max_rows=4)

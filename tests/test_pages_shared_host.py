@@ -9,7 +9,7 @@ from tests.test_pages_host import A, B, SHAPES, desc
 
 def calls(d, layer=0, stride=0, rows=8, q=A, start=B, plan=A, out=B, most=1):
     L, p = binding.lib(), C.byref(d)
-    return (lambda: L.lessdec_pages_share(p, start, rows, plan, None),
+    return (lambda: L.lessdec_pages_share(p, start, rows, -1, plan, None),
             lambda: L.lessdec_pages_attend_shared(p, layer, q, stride, out, None, start, rows, most, plan, None))
 
 
@@ -33,6 +33,8 @@ def test_arguments_are_refused():
             assert all(call() == binding.EINVAL for call in calls(desc(**{field: value}), plan=B + 64))
     for field in ("k_codes", "v_codes", "exps"):
         assert calls(desc(**{field: None}))[1]() == binding.EINVAL
+    big = dict(slots=4096, heads=1024, pages=1 << 20, table_len=1 << 25, page_tokens=16)      # 2^31 tiles
+    assert all(call() == binding.EINVAL for call in calls(desc(**big), rows=4096, plan=B + 64))
     d = desc()
     less = binding.lib().lessdec_pages_shared_workspace_bytes(C.byref(d), 8) - 1
     for more in (dict(workspace=None), dict(workspace=A + 128), dict(workspace_bytes=less)):
@@ -41,7 +43,7 @@ def test_arguments_are_refused():
 
 def test_nothing_to_do_needs_no_pointers():
     L, p = binding.lib(), C.byref(desc(workspace=None))
-    assert L.lessdec_pages_share(p, None, 0, None, None) == binding.OK
+    assert L.lessdec_pages_share(p, None, 0, 0, None, None) == binding.OK
     assert L.lessdec_pages_attend_shared(p, 0, None, 0, None, None, None, 0, 1, None, None) == binding.OK
     assert L.lessdec_pages_attend_shared(p, 0, None, 0, None, None, None, 8, 0, None, None) == binding.OK
 
