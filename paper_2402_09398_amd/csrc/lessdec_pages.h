@@ -129,18 +129,21 @@ constexpr int kPagesWorkers = 768;                   // workgroups of the kernel
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 
 // What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
-//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, log2 of the workers, tiles of a chunk
+//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, log2 of the workers, tiles of a chunk, short entries
 //  node  [3 slots][kNodeInts]: slot whose table row is read, first row, rows, least and largest position of them, blocks [first, last), node before it
 //        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
 //        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
-//  few   [4 slots][2]: steps, slot (that shares nothing) or slots + node, of up to kFewColumns columns
+//  few   [3 slots][kNodeInts]: of nodes of up to kFewColumns columns, and of slots of so many that share nothing: steps, slot whose table row is
+//        read, first row, rows, least and largest position, blocks [first, last), first column of the plan (-1: the rows are stored), rows of several slots.
+//        From the front, in steps of kFewBlocks blocks, for a workgroup each; from the back, in steps of two, the short ones, for a wave each
 //  chain [slots][kTrunkDepth + 1][4]: of its own node and those around it, the first column of the plan that is its first row's, columns from a share to
 //        the next, shares (0: no more nodes; with -1 in the first the slot is not in any, and an entry of few or of 128 columns and more)
 //  pos   [rows]: positions of the rows
 //  apart [slots]: scratch
 // A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
-constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanShift = 4, kPlanChunk = 5, kPlanHead = 8, kNodeInts = 12, kEndless = 1 << 30;
+constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanShift = 4, kPlanChunk = 5, kPlanShort = 6, kPlanHead = 8, kNodeInts = 12, kEndless = 1 << 30;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
+constexpr int kShortBlocks = 32;                     // up to which a wave works by itself
 constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
 constexpr int kTrunkShift = 8, kTrunkLong = 4;       // 256 workers, one to a compute unit; two from so many tiles on that each of them then has
 constexpr int kTrunkWorkers = 2 << kTrunkShift, kFewWorkers = 256;     // workgroups of the launch
@@ -180,7 +183,7 @@ inline double plan_tiles(int slots, int heads, int q_per_kv, long rows, long tok
   const double n = (double)rows * q_per_kv, most = (double)slots * kTrunkTile;
   return heads * ((kTrunkDepth + 1) * (n < most ? n : most) / kTrunkTile + 2.0 * slots) * (tokens / 64 + 1);
 }
-inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (3 * kNodeInts + 4 * (kTrunkDepth + 1) + 8 + 1) + rows; }
+inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (6 * kNodeInts + 4 * (kTrunkDepth + 1) + 1) + rows; }
 inline Plan plan_at(int *p, int slots)
 {
   Plan x;
@@ -188,7 +191,7 @@ inline Plan plan_at(int *p, int slots)
   x.node = x.head + kPlanHead;                       // (16-byte aligned)
   x.chain = x.node + 3L * slots * kNodeInts;
   x.few = x.chain + 4L * (kTrunkDepth + 1) * slots;
-  x.apart = x.few + 8L * slots;
+  x.apart = x.few + 3L * slots * kNodeInts;
   x.pos = x.apart + slots;
   return x;
 }

@@ -254,10 +254,10 @@ __device__ inline int steps_of(const Pages &c, const AttendArgs &a, int s)
 // where slots share pages, entries of the plan: slots that share nothing, and nodes of few columns
 __device__ inline int steps_of(const Pages &c, const SharedArgs &a, int i)
 {
-  return min(max(a.plan.few[2L * i], 0), c.table_len * page_blocks(c) / kStepBlocks + 1);
+  return min(max(a.plan.few[(long)i * kNodeInts], 0), c.table_len * page_blocks(c) / kStepBlocks + 1);
 }
 __device__ inline int few_entries(const Pages &c, const AttendArgs &) { return c.slots; }
-__device__ inline int few_entries(const Pages &c, const SharedArgs &a) { return min(max(same(a.plan.head[kPlanFew]), 0), 4 * c.slots); }
+__device__ inline int few_entries(const Pages &c, const SharedArgs &a) { return min(max(same(a.plan.head[kPlanFew]), 0), 3 * c.slots); }
 
 // Worker w's part [begin, end) of the steps, and where it begins: slot, and step among the slot's (head by head).
 struct Part {
@@ -404,61 +404,74 @@ __device__ inline void join(int n, int cols, Share share, Done done)
 template <int D> struct FewShared {
   float sums[4][kCols][D + 4], tops[4][kCols], totals[4][kCols];
 };
-template <bool BF16, int D, typename Args>
+// kAlone: a wave has a (slot, head) of a short list by itself, in steps of 32 tokens, and no part in other waves' work.
+template <bool BF16, int D, bool kAlone = false, typename Args>
 __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int worker, int workers, FewShared<D> &shared)
 {
-  constexpr int H = D / 64, T = D / 16;
+  constexpr int H = D / 64, T = D / 16, kBlocks = kAlone ? 2 : kStepBlocks;
   auto &sums = shared.sums;
   auto &tops = shared.tops, &totals = shared.totals;
   const int wave = __builtin_amdgcn_readfirstlane(thread_of<Args>() >> 6), lane = thread_of<Args>() & 63, n = lane & 15, g = lane >> 4;
   const int G = c.q_per_kv;
-  const Part part = part_of(c, a, worker, workers);
+  Part part;
+  if constexpr (kAlone) {
+    // units to the waves of all workgroups, the workgroups first
+    part.begin = worker + wave * workers;
+    part.end = (long)min(max(same(a.plan.head[kPlanShort]), 0), 3 * c.slots) * c.heads;
+  } else {
+    part = part_of(c, a, worker, workers);
+  }
   if (part.begin >= part.end) return;
   int s = part.slot;
   long in_slot = part.in_slot;
   for (long pos = part.begin; pos < part.end;) {
-    int steps = steps_of(c, a, s);
-    if constexpr (kShares<Args>) steps = same(steps);
-    if (steps == 0) { ++s; in_slot = 0; continue; }
-    const int head = (int)((unsigned long)in_slot >> 32 ? in_slot / steps : (unsigned)in_slot / (unsigned)steps);
-    const int from = (int)(in_slot - (long)head * steps);
-    const bool skip = kShares<Args> && part.whole && from > 0;         // (another worker's)
-    const int to = kShares<Args> && part.whole ? steps : (int)min((long)steps, from + (part.end - pos));
-    if (skip) {
-      pos += to - from;
-      in_slot += to - from;
-      if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
-      continue;
+    int steps = 0, head, from, to;
+    if constexpr (kAlone) {
+      s = same((int)((unsigned)pos / (unsigned)c.heads));
+      head = same((int)pos - s * c.heads);
+      from = to = 0;
+    } else {
+      steps = steps_of(c, a, s);
+      if constexpr (kShares<Args>) steps = same(steps);
+      if (steps == 0) { ++s; in_slot = 0; continue; }
+      head = (int)((unsigned long)in_slot >> 32 ? in_slot / steps : (unsigned)in_slot / (unsigned)steps);
+      from = (int)(in_slot - (long)head * steps);
+      to = kShares<Args> && part.whole ? steps : (int)min((long)steps, from + (part.end - pos));
+      if (kShares<Args> && part.whole && from > 0) { // another worker's
+        pos += to - from;
+        in_slot += to - from;
+        if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
+        continue;
+      }
     }
 
     Rows rows;
-    int lo, hi, p, read = s;
+    int lo, hi, p, read = s, base_column = -1;
     Span span;
-    Node node;
-    bool is_node = false;
     if constexpr (kShares<Args>) {
-      const int i = same(a.plan.few[2L * s + 1]);
-      is_node = i >= c.slots;
-      if (is_node) node = node_of(c, a, min(i - c.slots, 3 * c.slots - 1));
-      else read = max(i, 0);
-    }
-    if (!is_node) {
+      const int4 *f = reinterpret_cast<const int4 *>(a.plan.few + (long)(kAlone ? 3 * c.slots - 1 - s : s) * kNodeInts);
+      const int4 x = f[0], y = f[1], z = f[2];
+      const int most = c.table_len * c.page_tokens;
+      if constexpr (kAlone) to = steps = min(max(same(x.x), 1), kShortBlocks / 2);
+      read = min(max(same(x.y), 0), c.slots - 1);
+      rows.first = min(max(same(x.z), 0), a.rows);
+      rows.count = min(max(same(x.w), 0), a.rows - rows.first);
+      lo = min(max(same(y.x), 0), most - 1);
+      hi = min(max(same(y.y), -1), most - 1);
+      span = span_of(c, lo, hi);
+      span.cut(max(same(y.z), 0), min(max(same(y.w), 0), c.table_len * page_blocks(c)));
+      base_column = same(z.x);
+      p = hi + 1 - rows.count + n / G;
+      if (same(z.y)) p = n < rows.count * G ? min(max(a.plan.pos[rows.first + n / G], -1), most - 1) : -1;
+    } else {
       rows = slot_rows(a.start, read, a.rows);
       const int len = slot_length(c, read);
       lo = len - rows.count;
       hi = len - 1;
       span = span_of(c, lo, hi);
       p = lo + n / G;
-    } else if constexpr (kShares<Args>) {
-      rows = Rows{node.row, node.rows};
-      read = node.slot;
-      lo = node.lo;
-      hi = node.hi;
-      span = span_of(c, lo, hi);
-      span.cut(node.first, node.last);
-      p = n < node.cols ? min(max(a.plan.pos[node.row + n / G], -1), c.table_len * c.page_tokens - 1) : -1;
     }
-    const int cols = min(rows.count * G, kCols);
+    const int cols = min(rows.count * G, kCols), mine = kAlone ? 0 : wave * 2;
     u4 q[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -478,7 +491,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     auto look = [&](int step) {
       base = step;
       end = min(to, base + kWave / 2);
-      const int i = (base + lane / 2) * kStepBlocks + wave * 2 + (lane & 1), block = span.block(i);
+      const int i = (base + lane / 2) * kBlocks + mine + (lane & 1), block = span.block(i);
       const bool there = base + lane / 2 < to && i < span.count;
       const int page = table[there ? entry_of(c, block) : 0];
       ats = there ? block_in(c, page, head, block) : -1;
@@ -495,7 +508,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     };
     auto tokens_of = [&](int step, int b) {          // the first token of a block, -1: not there
       const int at = __builtin_amdgcn_readlane(ats, (step - base) * 2 + b);
-      return at >= 0 ? span.block(step * kStepBlocks + wave * 2 + b) * kBlock : -1;
+      return at >= 0 ? span.block(step * kBlocks + mine + b) * kBlock : -1;
     };
 
     f4 acc[T];
@@ -614,6 +627,31 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     // the four waves' sums, relative to the largest of their scores
     total += __shfl_xor(total, 16, kWave);
     total += __shfl_xor(total, 32, kWave);
+    if constexpr (kAlone) {
+      pos += 4 * workers;
+      if (n >= cols) continue;
+      if (base_column < 0) {
+        const long to_row = (long)(rows.first + n / G) * c.heads * G + head * G + n % G;
+        const float r = 1.f / total;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          auto stored = [&](int j) { return (unsigned)Operand<BF16>::store(share_of(acc[t][j], total, r)); };
+          reinterpret_cast<uint2 *>(a.out)[to_row * (D / 4) + t * 4 + g] = make_uint2(stored(0) | stored(1) << 16, stored(2) | stored(3) << 16);
+        }
+        if (a.lse && g == 0) a.lse[to_row] = total == 0.f ? -__builtin_inff() : (top.s + (top.e + __builtin_log2f(total))) * 0.6931471805599453f;
+      } else if (base_column + n < a.columns) {
+        const long at = (long)head * a.columns + base_column + n;
+        const float unit_of_e = top.unit();
+#pragma unroll
+        for (int t = 0; t < T; ++t) *reinterpret_cast<f4 *>(a.trunk + at * D + t * 16 + g * 4) = acc[t] * unit_of_e;
+        float *tops_at = a.trunk + c.heads * a.columns * D + at;
+        if (g == 0) {
+          tops_at[0] = top.s == kLowest ? -__builtin_inff() : top.s;
+          tops_at[c.heads * a.columns] = total * unit_of_e;
+        }
+      }
+      continue;
+    } else {
     if (g == 0) { tops[wave][n] = top.s; totals[wave][n] = total * top.unit(); }
     __syncthreads();
     const float largest = fmaxf(fmaxf(tops[0][n], tops[1][n]), fmaxf(tops[2][n], tops[3][n])), f = exp2_fast(top.s - largest) * top.unit();
@@ -623,9 +661,9 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     __syncthreads();
     auto finish = [&](int col, int d, float x, float y, float m, float l) {
       if constexpr (kShares<Args>)
-        if (is_node) {
-          const long at = (long)head * a.columns + node.base + col;
-          if (node.base < 0 || (long)node.base + col >= a.columns) return;
+        if (base_column >= 0) {
+          const long at = (long)head * a.columns + base_column + col;
+          if ((long)base_column + col >= a.columns) return;
           *reinterpret_cast<float2 *>(a.trunk + at * D + d) = make_float2(x, y);
           float *tops = a.trunk + c.heads * a.columns * D;
           if (d == 0) { tops[at] = l == 0.f && m == kLowest ? -__builtin_inff() : m; tops[c.heads * a.columns + at] = l; }
@@ -689,6 +727,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
     pos += to - from;
     in_slot += to - from;
     if (in_slot == (long)steps * c.heads) { ++s; in_slot = 0; }
+    }
   }
 }
 
@@ -1290,8 +1329,14 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a, i
 {
   __shared__ WideShared<D> shared;
   if (!plan_holds(a)) return;
-  if ((int)blockIdx.x < few) few_rows<BF16, D>(c, a, blockIdx.x, few, reinterpret_cast<FewShared<D> &>(shared.tiles));
-  else trunk_pieces<BF16, D>(c, a, blockIdx.x - few, shared);
+  if (few && same(a.plan.head[kPlanTiles]) <= 0) few = gridDim.x;
+  if ((int)blockIdx.x < few) {
+    auto &parts = reinterpret_cast<FewShared<D> &>(shared.tiles);
+    few_rows<BF16, D, true>(c, a, blockIdx.x, few, parts);
+    if (same(a.plan.head[kPlanFew]) > 0) few_rows<BF16, D>(c, a, blockIdx.x, few, parts);
+  } else {
+    trunk_pieces<BF16, D>(c, a, blockIdx.x - few, shared);
+  }
 }
 
 // A wave joins a row's sums by one query head: those of its slot's own part and of the nodes around it, a lane a share.

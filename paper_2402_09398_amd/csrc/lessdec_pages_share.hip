@@ -265,7 +265,23 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (lane == 0) record(r.index[k], read, row, count, lo, hi, (up < 0 ? 0 : r.a[up]) * per, r.a[k] * per, up < 0 ? -1 : r.index[up]);
   }
   // a slot's own part, behind its innermost node, which is that of the larger of its two boundaries
-  int all_nodes = nodes, few = 0;
+  int all_nodes = nodes, few = 0, short_ones = 0;
+  // an entry of few columns for those threads that have one; all threads call it
+  auto list = [&](bool mine, int blocks, int read, int row, int count, int lo, int hi, int first, int last, int column, bool several) {
+    const bool brief = blocks <= kShortBlocks;
+    int all;
+    int at = few + scan((int)(mine && !brief), all);
+    few += all;
+    const int back = short_ones + scan((int)(mine && brief), all);
+    short_ones += all;
+    if (!mine) return;
+    if (brief) at = 3 * N - 1 - back;
+    int4 *f = reinterpret_cast<int4 *>(plan.few + (long)at * kNodeInts);
+    const int step = brief ? 2 : kFewBlocks;
+    f[0] = make_int4(max((blocks + step - 1) / step, 1), read, row, count);
+    f[1] = make_int4(lo, hi, first, last);
+    f[2] = make_int4(column, several, 0, 0);
+  };
   for (int base = 0; base < n; base += kThreads) {
     const int k = base + tid;
     int i = -1;
@@ -285,12 +301,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     }
     all_nodes += all;
     const bool direct = k < n && !own && columns <= kFewColumns;
-    const int to = few + scan((int)direct, all);
-    if (direct) {
-      const int steps = (seen_blocks(c, lo_of(k), r.hi[k], 0, kEndless) + kFewBlocks - 1) / kFewBlocks;
-      *reinterpret_cast<int2 *>(plan.few + 2L * to) = make_int2(max(steps, 1), r.slot[k]);
-    }
-    few += all;
+    const int at_k = min(k, n - 1), lo = lo_of(at_k), hi = r.hi[at_k];
+    list(direct, seen_blocks(c, lo, hi, 0, kEndless), r.slot[at_k], r.row[at_k], r.rows[at_k], lo, hi, 0, kEndless, -1, false);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -299,24 +311,20 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
     int *f = plan.node + (long)min(i, all_nodes - 1) * kNodeInts;
-    int mine = 0, wide = 0, steps = 0;
+    int mine = 0, wide = 0, narrow = 0;
     if (i < all_nodes) {
       const int columns = f[2] * G, blocks = columns > 0 ? seen_blocks(c, f[3], f[4], f[5], f[6]) : 0;
       if (columns > kFewColumns) { mine = (blocks + 3) / 4; wide = (columns + kTrunkTile - 1) / kTrunkTile; }
-      else steps = (blocks + kFewBlocks - 1) / kFewBlocks;
+      else narrow = blocks;
     }
     long sum;
-    int all;
     const long before = tiles + scan((long)mine * wide, sum);
-    const int to = few + scan((int)(steps > 0), all);
     if (i < all_nodes) {
-      f[8] = (int)min(before, (long)kEndless);
+      f[8] = (int)before;
       f[9] = mine;
-      f[11] = steps > 0;
+      f[11] = narrow;
     }
-    if (steps > 0) *reinterpret_cast<int2 *>(plan.few + 2L * to) = make_int2(steps, N + i);
     tiles += sum;
-    few += all;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -326,14 +334,16 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
     int *f = plan.node + (long)min(i, all_nodes - 1) * kNodeInts;
-    const int pieces = i >= all_nodes ? 0 : f[9] ? 2 * trunk.chunks(f[9]) : f[11];
+    const int narrow = i >= all_nodes ? 0 : f[11], pieces = i >= all_nodes ? 0 : f[9] ? 2 * trunk.chunks(f[9]) : narrow > 0;
     int all;
     const long at = columns + scan(i < all_nodes ? pieces * f[2] * G : 0, all);
+    const bool fits = at + (long)pieces * f[2] * G <= most_columns;    // (it does: plan_columns)
     if (i < all_nodes) {
-      f[10] = at + (long)pieces * f[2] * G <= most_columns ? (int)at : -1;
-      f[11] = f[10] >= 0 ? pieces : 0;
+      f[10] = fits ? (int)at : -1;
+      f[11] = fits ? pieces : 0;
     }
     columns += all;
+    list(fits && narrow > 0, narrow, f[0], f[1], f[2], f[3], f[4], f[5], f[6], (int)at, i < nodes);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -360,6 +370,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     plan.head[kPlanNodes] = all_nodes;
     plan.head[kPlanTiles] = (int)tiles;
     plan.head[kPlanFew] = few;
+    plan.head[kPlanShort] = short_ones;
     plan.head[kPlanRows] = rows;
     plan.head[kPlanShift] = trunk.shift;
     plan.head[kPlanChunk] = trunk.chunk;

@@ -21,7 +21,7 @@ class Shared(Pair):
         self.sharing = own.share_plan()
 
     def nodes(self):
-        """Every slot's own part (-1: it shares nothing), and (row, rows, first block, last, node before, tiles, has few columns) of every node."""
+        """Every slot's own part (-1: it shares nothing), and (row, rows, first block, last, node before, tiles, shares) of every node."""
         slots, plan = self.ref.slots, self.sharing.cpu().numpy()
         node = plan[8:8 + 36 * slots].reshape(-1, 12)[:plan[0]]
         chain = plan[8 + 36 * slots:][:16 * slots].reshape(-1, 4, 4)
@@ -49,9 +49,9 @@ class Shared(Pair):
         slot, nodes = self.nodes()
         per, several = r.page // 16, [n for n in nodes if n[3] < 1 << 30]
         assert nodes[:len(several)] == several
-        for row, rows, first, last, before, tiles, few in several:
+        for row, rows, first, last, before, tiles, shares in several:
             there = [s for s in range(r.slots) if counts[s] and row <= start[s] and start[s + 1] <= row + rows]
-            assert len(there) > 1 and sum(counts[s] for s in there) == rows and first % per == last % per == 0 and (tiles > 0) != few
+            assert len(there) > 1 and sum(counts[s] for s in there) == rows and first % per == last % per == 0 and shares > 0
             assert all(slot[s] >= 0 for s in there) and (before == -1 if first == 0 else several[before][3] == first)
             for j in range(first // per, last // per):
                 named = set()
@@ -224,7 +224,7 @@ def test_a_long_prefix_over_many_workgroups():
     p.room([1, 30, 7, 2, 500])
     for rows in ([1] * 5, [1, 9, 7, 2, 30]):
         nodes = p.share(rows)
-        assert nodes[0][5] > 300 or nodes[0][6]
+        assert nodes[0][5] > 300 or rows == [1] * 5
         p.attend_shared(rows)
 
 
