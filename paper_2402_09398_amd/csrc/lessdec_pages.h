@@ -129,7 +129,8 @@ constexpr int kPagesWorkers = 768;                   // workgroups of the kernel
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 
 // What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
-//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, log2 of the workers, tiles of a chunk, short entries
+//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, workers of the nodes, of the entries of few, short entries, whether workers
+//        have whole chunks
 //  node  [3 slots][kNodeInts]: slot whose table row is read, first row, rows, least and largest position of them, blocks [first, last), node before it
 //        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
 //        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
@@ -138,44 +139,40 @@ hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, h
 //        From the front, in steps of kFewBlocks blocks, for a workgroup each; from the back, in steps of two, the short ones, for a wave each
 //  chain [slots][kTrunkDepth + 1][4]: of its own node and those around it, the first column of the plan that is its first row's, columns from a share to
 //        the next, shares (0: no more nodes; with -1 in the first the slot is not in any, and an entry of few or of 128 columns and more)
+//  first [kSharedWorkers][kFirstInts]: a worker's first piece: its node as above, then head, first column, tiles [from, to), piece, whether it is a whole chunk
 //  pos   [rows]: positions of the rows
 //  apart [slots]: scratch
 // A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
-constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanShift = 4, kPlanChunk = 5, kPlanShort = 6, kPlanHead = 8, kNodeInts = 12, kEndless = 1 << 30;
+constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanFewWorkers = 5, kPlanShort = 6, kPlanWhole = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
 constexpr int kShortBlocks = 32;                     // up to which a wave works by itself
 constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
-constexpr int kTrunkShift = 8, kTrunkLong = 4;       // 256 workers, one to a compute unit; two from so many tiles on that each of them then has
-constexpr int kTrunkWorkers = 2 << kTrunkShift, kFewWorkers = 256;     // workgroups of the launch
+constexpr int kSharedWorkers = 512;                  // workgroups of the launch, two to a compute unit, multiples of 8 of them for either kind of work
 struct Plan {
-  int *head, *node, *chain, *few, *apart, *pos;
+  int *head, *node, *chain, *few, *first, *apart, *pos;
 };
-// The tiles of all heads and nodes, one behind the other, are dealt out evenly: worker w has [first(w), first(w + 1)).  Within a node and head
+// The nodes' tiles as the workers get them, in one of two ways.  Whole chunks: the tiles of a node's 128 columns by one head are cut into chunks of
+// the same length, the least with which there are no more chunks than workers, and each worker has one.  Or, where that would leave workers idle for
+// longer than a second beginning and end take: the tiles of all heads and nodes, one behind the other, are dealt out evenly, worker w has
+// [first(w), first(w + 1)).  Within a node and head
 // they are ordered by chunks of tokens, in a chunk by tiles of 128 columns, so that neighbouring workers read the same tokens at the same time.  A
 // chunk is no longer than any worker's part: what it has of 128 columns is cut into two pieces at most.
 struct Trunk {
-  int tiles, heads;                                  // of a head; all of them together are less than 2^31
-  int shift;                                         // log2 of the workers
-  int chunk;
-  __host__ __device__ inline unsigned total() const { return (unsigned)tiles * heads; }
-  __host__ __device__ inline unsigned first(unsigned w) const { return (unsigned)((unsigned long long)w * total() >> shift); }
-  __host__ __device__ inline int chunks(int n) const { return (n + chunk - 1) / chunk; }        // of n tiles of 128 columns
-  __host__ __device__ inline static Trunk of(int tiles, int heads)
+  unsigned total;                                    // less than 2^31
+  int workers, chunk;
+  __host__ __device__ inline unsigned first(unsigned w) const
   {
-    Trunk t{tiles, heads, 0, 1};
-    const unsigned n = t.total();                    // (two tiles to a worker, at least)
-    while (t.shift < kTrunkShift && n >> (t.shift + 2)) ++t.shift;
-    if (t.shift == kTrunkShift && n >> (t.shift + 1) >= kTrunkLong) ++t.shift;
-    if (n >> t.shift) t.chunk = (int)(n >> t.shift);
-    return t;
+    const unsigned each = total / workers, more = total - each * workers;
+    return w * each + (w < more ? w : more);
   }
+  __host__ __device__ inline int chunks(int n) const { return (n + chunk - 1) / chunk; }        // of n tiles of 128 columns
 };
 // Slots of up to 127 query columns share.  A row is in kTrunkDepth nodes and one of its own at most, each of which has room for two pieces, and
 // for as many more as chunks are (n tiles have n / chunk + 1 at most, and a chunk is at least half of a worker's part).
 inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
 {
   const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
-  return 2 * (kTrunkDepth + 1) * (n < most ? n : most) + 4L * kTrunkTile * (kTrunkWorkers / heads + 1);
+  return 2 * (kTrunkDepth + 1) * (n < most ? n : most) + 4L * kTrunkTile * (kSharedWorkers / heads + 1);
 }
 // tiles of all heads and nodes, at most
 inline double plan_tiles(int slots, int heads, int q_per_kv, long rows, long tokens)
@@ -183,7 +180,7 @@ inline double plan_tiles(int slots, int heads, int q_per_kv, long rows, long tok
   const double n = (double)rows * q_per_kv, most = (double)slots * kTrunkTile;
   return heads * ((kTrunkDepth + 1) * (n < most ? n : most) / kTrunkTile + 2.0 * slots) * (tokens / 64 + 1);
 }
-inline long plan_ints(int slots, long rows) { return kPlanHead + (long)slots * (6 * kNodeInts + 4 * (kTrunkDepth + 1) + 1) + rows; }
+inline long plan_ints(int slots, long rows) { return kPlanHead + kSharedWorkers * kFirstInts + (long)slots * (6 * kNodeInts + 4 * (kTrunkDepth + 1) + 1) + rows; }
 inline Plan plan_at(int *p, int slots)
 {
   Plan x;
@@ -191,7 +188,8 @@ inline Plan plan_at(int *p, int slots)
   x.node = x.head + kPlanHead;                       // (16-byte aligned)
   x.chain = x.node + 3L * slots * kNodeInts;
   x.few = x.chain + 4L * (kTrunkDepth + 1) * slots;
-  x.apart = x.few + 3L * slots * kNodeInts;
+  x.first = x.few + 3L * slots * kNodeInts;
+  x.apart = x.first + kSharedWorkers * kFirstInts;
   x.pos = x.apart + slots;
   return x;
 }

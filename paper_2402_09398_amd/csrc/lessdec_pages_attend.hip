@@ -203,10 +203,10 @@ struct Node {
   int slot, row, rows, lo, hi, first, last, before, tile, tiles, base, shares;
   int cols;
 };
-// (i: the same in all lanes)
-__device__ inline Node node_of(const Pages &c, const SharedArgs &a, int i)
+// (f: the same in all lanes)
+__device__ inline Node node_of(const Pages &c, const SharedArgs &a, const int *record)
 {
-  const int4 *f = reinterpret_cast<const int4 *>(a.plan.node + (long)i * kNodeInts);
+  const int4 *f = reinterpret_cast<const int4 *>(record);
   const int4 x = f[0], y = f[1], z = f[2];
   const int most = c.table_len * c.page_tokens;
   Node n;
@@ -825,7 +825,7 @@ template <typename Args> __device__ inline bool columns_of(const Pages &c, const
 
 template <int D> struct WideShared {
   __align__(16) u4 tiles[4][kTile * D / 8];
-  int spoiled, lo[4], hi[4];
+  int spoiled;
 };
 // A piece of the nodes' tiles: 128 columns of a node by one head, tiles [from, to), the piece-th of these columns.
 struct Piece {
@@ -867,21 +867,10 @@ __device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigne
   const bool have = t.first + wave * 32 <= last_col;
   const int row = rows.first + col / G, q_head = head * G + col % G;
   if constexpr (kTrunk) {
-    // rows of several slots: their positions as the plan has them, in any order
+    // rows of several slots, their positions in any order as the plan has them; what tiles all of them see is known from the least and the largest
     p = col <= last_col ? min(max(a.plan.pos[row], -1), c.table_len * c.page_tokens - 1) : -1;
-    wave_lo = col <= last_col ? p : 1 << 30;
-    wave_hi = p;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      wave_lo = min(wave_lo, __shfl_xor(wave_lo, d, kWave));
-      wave_hi = max(wave_hi, __shfl_xor(wave_hi, d, kWave));
-    }
-    wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
-    wave_hi = __builtin_amdgcn_readfirstlane(wave_hi);
-    if (lane == 0) { shared.lo[wave] = wave_lo; shared.hi[wave] = wave_hi; }
-    __syncthreads();
-    lo = same(min(min(shared.lo[0], shared.lo[1]), min(shared.lo[2], shared.lo[3])));
-    hi = same(max(max(shared.hi[0], shared.hi[1]), max(shared.hi[2], shared.hi[3])));
+    lo = wave_lo = trunk.node.lo;
+    hi = wave_hi = trunk.node.hi;
   } else {
     lo = before + t.first / G;
     hi = before + last_col / G;
@@ -1297,45 +1286,58 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
 template <bool BF16, int D>
 __device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, WideShared<D> &shared)
 {
-  const Trunk all{max(same(a.plan.head[kPlanTiles]), 0), c.heads, same(a.plan.head[kPlanShift]) & 15, max(same(a.plan.head[kPlanChunk]), 1)};
-  const int nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
-  if (all.tiles == 0 || nodes == 0 || w >> all.shift) return;
-  if (all.shift >= kTrunkShift) w = (w & 7) << (all.shift - 3) | w >> 3;                 // (neighbours on one die)
-  const unsigned end = all.first(w + 1);
-  for (unsigned at = all.first(w); at < end;) {
-    Piece x;
-    x.head = same((int)(at / (unsigned)all.tiles));
-    const int in_head = (int)(at - (unsigned)x.head * all.tiles);
+  // (the first piece is loaded before what says whether there is one)
+  const int *mine = a.plan.first + w * kFirstInts;
+  Piece x;
+  x.node = node_of(c, a, mine);
+  const int4 f = reinterpret_cast<const int4 *>(mine)[3], g = reinterpret_cast<const int4 *>(mine)[4];
+  const int tiles = max(same(a.plan.head[kPlanTiles]), 0), nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
+  if (tiles == 0 || nodes == 0) return;
+  Trunk all{(unsigned)tiles * c.heads, max(same(a.plan.head[kPlanWorkers]), 1), 1};
+  all.chunk = max((int)(all.total / all.workers), 1);
+  const bool whole = same(a.plan.head[kPlanWhole]) != 0;
+  const unsigned end = whole ? w + 1 : all.first(w + 1);
+  x.head = same(f.x); x.column = same(f.y); x.from = same(f.z); x.to = same(f.w); x.piece = same(g.x); x.only = same(g.y);
+  for (unsigned at = whole ? w : all.first(w); at < end;) {
+    // (no plan of this library's fails here)
+    if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.to <= x.from || x.piece < 0) return;
+    wide_item<BF16, D, true>(c, a, 0, 0, 1, x, shared);
+    at += x.to - x.from;
+    if (at >= end || whole) return;
+    __syncthreads();
+    x.head = same((int)(at / (unsigned)tiles));
+    const int in_head = (int)(at - (unsigned)x.head * tiles);
     const int i = last_at(nodes, in_head, [&](int k) { return (long)a.plan.node[(long)k * kNodeInts + 8]; });
-    x.node = node_of(c, a, same(i));
-    const int in_node = in_head - x.node.tile, tall = (x.node.cols + kWide - 1) / kWide, wide_chunk = all.chunk * tall;
-    if (x.head >= c.heads || in_node < 0 || x.node.tiles == 0 || (long)in_node >= (long)tall * x.node.tiles) return;       // (no plan is like this)
+    x.node = node_of(c, a, a.plan.node + (long)same(i) * kNodeInts);
+    const int in_node = in_head - x.node.tile, wide_chunk = all.chunk * ((x.node.cols + kWide - 1) / kWide);
+    if (in_node < 0 || wide_chunk == 0) return;
     const int k = same(in_node / wide_chunk), in_chunk = in_node - k * wide_chunk, len = min(all.chunk, x.node.tiles - k * all.chunk);
+    if (len <= 0) return;
     const int column = same(in_chunk / len), done = in_chunk - column * len;
     x.column = column * kWide;
     x.from = k * all.chunk + done;
     x.to = x.from + min(len - done, (int)(end - at));
     x.piece = 2 * k + (done > 0);
     x.only = done == 0 && x.to == x.from + len;
-    wide_item<BF16, D, true>(c, a, 0, 0, 1, x, shared);
-    __syncthreads();
-    at += x.to - x.from;
   }
 }
 
 // The plan's work: entries of few columns by the first workgroups, nodes by those behind them.
 template <bool BF16, int D>
-__global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a, int few)
+__global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a)
 {
   __shared__ WideShared<D> shared;
   if (!plan_holds(a)) return;
-  if (few && same(a.plan.head[kPlanTiles]) <= 0) few = gridDim.x;
+  const int few = same(a.plan.head[kPlanFewWorkers]) & -8, workers = same(a.plan.head[kPlanWorkers]);
   if ((int)blockIdx.x < few) {
     auto &parts = reinterpret_cast<FewShared<D> &>(shared.tiles);
     few_rows<BF16, D, true>(c, a, blockIdx.x, few, parts);
     if (same(a.plan.head[kPlanFew]) > 0) few_rows<BF16, D>(c, a, blockIdx.x, few, parts);
   } else {
-    trunk_pieces<BF16, D>(c, a, blockIdx.x - few, shared);
+    unsigned w = blockIdx.x - few;
+    if ((int)w >= workers) return;
+    if (workers % 8 == 0) w = w % 8 * (workers / 8) + w / 8;           // (neighbours on one die)
+    trunk_pieces<BF16, D>(c, a, w, shared);
   }
 }
 
@@ -1473,8 +1475,7 @@ hipError_t attend(const Pages &c, const Args &a, hipStream_t st)
 {
   const long pairs = (long)c.slots * c.heads;
   if constexpr (kShares<Args>) {
-    const int few = c.q_per_kv <= kCols ? kFewWorkers : 0;
-    shared_kernel<BF16, D><<<few + kTrunkWorkers, 256, 0, st>>>(c, a, few);
+    shared_kernel<BF16, D><<<kSharedWorkers, 256, 0, st>>>(c, a);
     const long columns = (long)a.max_new * c.q_per_kv < kTrunkTile ? (long)a.max_new * c.q_per_kv : kTrunkTile - 1;
     shared_join_kernel<BF16, D><<<dim3((unsigned)((columns * c.heads + 3) / 4), (unsigned)c.slots), 256, 0, st>>>(c, a);
     if ((long)a.max_new * c.q_per_kv < kTrunkTile) return hipGetLastError();

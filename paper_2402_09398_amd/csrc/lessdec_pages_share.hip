@@ -266,6 +266,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   }
   // a slot's own part, behind its innermost node, which is that of the larger of its two boundaries
   int all_nodes = nodes, few = 0, short_ones = 0;
+  long few_steps = 0;
   // an entry of few columns for those threads that have one; all threads call it
   auto list = [&](bool mine, int blocks, int read, int row, int count, int lo, int hi, int first, int last, int column, bool several) {
     const bool brief = blocks <= kShortBlocks;
@@ -274,6 +275,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     few += all;
     const int back = short_ones + scan((int)(mine && brief), all);
     short_ones += all;
+    long steps;
+    scan((long)(mine && !brief ? (blocks + kFewBlocks - 1) / kFewBlocks : 0), steps);
+    few_steps += steps;
     if (!mine) return;
     if (brief) at = 3 * N - 1 - back;
     int4 *f = reinterpret_cast<int4 *>(plan.few + (long)at * kNodeInts);
@@ -325,16 +329,56 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       f[11] = narrow;
     }
     tiles += sum;
+    // (columns of the plan follow)
+    list(narrow > 0, narrow, f[0], f[1], f[2], f[3], f[4], f[5], f[6], i, i < nodes);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   // columns: as many times a node's as workgroups may have a piece of it
-  const Trunk trunk = Trunk::of((int)tiles, c.heads);
+  // How many workgroups for the entries of few, which also has those of the nodes: the longer of the two kinds of work is to be short.  In units of
+  // 1/8 us, measured: a short entry by a head 15 us for each of the waves that has one, a step of a long one 0.6, a piece 11 and 2.2 a tile.
+  Trunk trunk{(unsigned)(tiles * c.heads), 8, 1};
+  int few_workers = 0;
+  if (few_steps || short_ones) {
+    unsigned best = ~0u;
+    for (int f = 32; f <= kSharedWorkers; f *= 2) {
+      if (f == kSharedWorkers && tiles) break;
+      const unsigned waves = 4 * f, a = ((unsigned)short_ones * c.heads + waves - 1) / waves * 120 + (unsigned)min(few_steps * c.heads / f, 1L << 26) * 5;
+      const unsigned b = tiles ? 88 + min(trunk.total / max(kSharedWorkers - f, 8) + 1, 1u << 26) * 18 : 0, time = max(a, b);
+      if (time < best) { best = time; few_workers = f; }
+    }
+  }
+  trunk.workers = max(min(kSharedWorkers - few_workers, (int)min(trunk.total / 2, 4096u)) & ~7, 8);
+  // Whole chunks: their length.  A piece begins and ends for the time of four tiles or five.
+  int length = max((int)((trunk.total + trunk.workers - 1) / trunk.workers), 2), chunks_of_head = 0;
+  bool whole = false;
+  for (int turn = 0; turn < 5 && tiles; ++turn) {
+    int x = 0;
+    for (int i = tid; i < all_nodes; i += kThreads) {
+      const int *f = plan.node + (long)i * kNodeInts;
+      x += min((f[2] * G + kTrunkTile - 1) / kTrunkTile * (f[9] ? (f[9] + length - 1) / length : 0), 1 << 20);
+    }
+    scan(x, chunks_of_head);
+    const long all = (long)chunks_of_head * c.heads;
+    whole = all <= trunk.workers;
+    if (whole) break;
+    length = (int)min(max((long)length + 1, length * all / trunk.workers), (long)kEndless);
+  }
+  whole = whole && (long)length * trunk.workers - trunk.total <= 4L * trunk.workers;
+  trunk.chunk = whole ? length : max((int)(trunk.total / trunk.workers), 1);
+  if (whole) trunk.workers = chunks_of_head * c.heads;
   long columns = 0;
+  int chunks = 0;
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
     int *f = plan.node + (long)min(i, all_nodes - 1) * kNodeInts;
-    const int narrow = i >= all_nodes ? 0 : f[11], pieces = i >= all_nodes ? 0 : f[9] ? 2 * trunk.chunks(f[9]) : narrow > 0;
+    const int pieces = i >= all_nodes ? 0 : f[9] ? (whole ? 1 : 2) * trunk.chunks(f[9]) : f[11] > 0;
+    if (whole) {                                     // (a node's place among the chunks of a head in place of that among its tiles)
+      int all;
+      const int at = chunks + scan(i < all_nodes && f[9] ? (f[2] * G + kTrunkTile - 1) / kTrunkTile * pieces : 0, all);
+      if (i < all_nodes) f[8] = at;
+      chunks += all;
+    }
     int all;
     const long at = columns + scan(i < all_nodes ? pieces * f[2] * G : 0, all);
     const bool fits = at + (long)pieces * f[2] * G <= most_columns;    // (it does: plan_columns)
@@ -343,10 +387,42 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       f[11] = fits ? pieces : 0;
     }
     columns += all;
-    list(fits && narrow > 0, narrow, f[0], f[1], f[2], f[3], f[4], f[5], f[6], (int)at, i < nodes);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
+  // the columns of the entries of few, which have their node's number there
+  for (int i = tid; i < few + short_ones; i += kThreads) {
+    int *f = plan.few + (long)(i < few ? i : 3 * N - 1 - (i - few)) * kNodeInts + 8;
+    if (*f >= 0) *f = plan.node[(long)*f * kNodeInts + 10];
+  }
+  // the workers' first pieces: the last node that begins no later
+  if (tiles)
+    for (int w = tid; w < trunk.workers; w += kThreads) {
+      const unsigned at = whole ? w : trunk.first(w), end = whole ? w + 1 : trunk.first(w + 1), in_all = whole ? (unsigned)chunks_of_head : (unsigned)tiles;
+      const unsigned head = at / in_all;
+      const int in_head = (int)(at - head * in_all);
+      int low = 0;
+      for (int high = all_nodes; high - low > 1;) {
+        const int mid = (low + high) / 2;
+        if (plan.node[(long)mid * kNodeInts + 8] <= in_head) low = mid;
+        else high = mid;
+      }
+      const int4 *f = reinterpret_cast<const int4 *>(plan.node + (long)low * kNodeInts);
+      int4 *to = reinterpret_cast<int4 *>(plan.first + w * kFirstInts);
+      const int4 x = f[0], y = f[1], z = f[2];
+      const int n = max(z.y, 1), tall = max((x.z * G + kTrunkTile - 1) / kTrunkTile, 1), in_node = in_head - z.x;
+      to[0] = x; to[1] = y; to[2] = z;
+      if (whole) {
+        const int each = (n + trunk.chunks(n) - 1) / trunk.chunks(n), k = in_node / tall;
+        to[3] = make_int4((int)head, (in_node - k * tall) * kTrunkTile, k * each, min(n, (k + 1) * each));
+        to[4] = make_int4(k, 0, 0, 0);
+      } else {
+        const int k = in_node / (trunk.chunk * tall), in_chunk = in_node - k * trunk.chunk * tall, len = max(min(trunk.chunk, n - k * trunk.chunk), 1);
+        const int column = in_chunk / len, done = in_chunk - column * len, now = min(len - done, (int)(end - at));
+        to[3] = make_int4((int)head, column * kTrunkTile, k * trunk.chunk + done, k * trunk.chunk + done + now);
+        to[4] = make_int4(2 * k + (done > 0), now == len, 0, 0);
+      }
+    }
   // what a slot's rows are joined from
   for (int k = tid; k < n; k += kThreads) {
     int4 *chain = reinterpret_cast<int4 *>(plan.chain) + (kTrunkDepth + 1L) * r.slot[k];
@@ -372,8 +448,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     plan.head[kPlanFew] = few;
     plan.head[kPlanShort] = short_ones;
     plan.head[kPlanRows] = rows;
-    plan.head[kPlanShift] = trunk.shift;
-    plan.head[kPlanChunk] = trunk.chunk;
+    plan.head[kPlanWorkers] = trunk.workers;
+    plan.head[kPlanFewWorkers] = few_workers;
+    plan.head[kPlanWhole] = whole;
   }
 }
 
