@@ -21,27 +21,34 @@ typedef unsigned u4a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 4 * kWave, kEach = kBeamTile / kWave;
 static_assert(kEach == 8, "eight logits a lane and tile");
-constexpr float kFar = 500.f;                        // that a logit may lie above m: e^500 times 2^28 is within fp64
-constexpr float kLeast = 700.f;                      // what lies further below m counts as e^-700
+constexpr float kFar = 500.f;                        // logits up to here are taken as they are: e^500 times 2^28 is within fp64
+constexpr float kLeast = 700.f;                      // what lies further below counts as e^-700
 
-// ---- e^t in fp64 -----------------------------------------------------------------------------------------------------------
-// 2^{y / 256} with y = 256 t / ln 2 = n + r, |r| <= 1/2 (r from the exact product): a table of 2^{i / 256}, i = n mod 256, times a polynomial of degree 3 for
-// 2^{r / 256} (its next term is 1.4e-13 at most), times 2^{n / 256} by addition to the exponent.  -700 <= t <= kFar.
+// ---- e^x to fp64 -----------------------------------------------------------------------------------------------------------
+// 2^{y / 1024} with y = 1024 x / ln 2 = n + r, |r| <= 1/2: a table of 2^{i / 1024} in fp64, i = n mod 1024, times 2^{r / 1024} = 1 + p, times
+// 2^{n / 1024 - i / 1024} by addition to the exponent.  x is an fp32, so that r, from the exact products of its fmas, and p = r (c1 + c2 r) <= 3.4e-4 may be
+// fp32, too: p is within 1e-10 of its 3.4e-4, and what the polynomial leaves out is 6.5e-12 at most.  -kLeast <= x <= kFar.
+constexpr int kTable = 1024;
 struct Exponentials {
-  double table[256];
-  __device__ inline void fill() { table[threadIdx.x] = exp2((double)threadIdx.x / 256); }
-  __device__ inline double of(double t) const
+  double table[kTable];
+  __device__ inline void fill()
   {
-    constexpr double kRound = 6755399441055744.0;    // 1.5 * 2^52: its sum with y has the nearest whole number in the low word
-    constexpr double kPer = 369.32993046757914;      // 256 / ln 2
-    constexpr double c1 = 2.7076061740622863e-03, c2 = 3.6655655969037715e-06, c3 = 3.3082995997574655e-09;    // (ln 2 / 256)^i / i!
-    const double s = fma(t, kPer, kRound);
-    const int n = (int)__double2loint(s);
-    const double r = fma(t, kPer, kRound - s), p = r * fma(r, fma(r, c3, c2), c1), power = table[n & 255];
-    const double e = fma(power, p, power);
-    return __hiloint2double(__double2hiint(e) + ((n & ~255) << 12), __double2loint(e));
+    for (int i = threadIdx.x; i < kTable; i += kThreads) table[i] = exp2((double)i / kTable);
+  }
+  __device__ inline double of(float x) const
+  {
+    constexpr float kRound = 12582912.f;             // 1.5 * 2^23: its sum with y has n in the low bits
+    constexpr double kPer = 1477.3197218702985;      // 1024 / ln 2
+    constexpr float high = (float)kPer, low = (float)(kPer - (double)high);
+    constexpr float c1 = 6.7690154351557157e-04f, c2 = 2.2909784980648572e-07f;        // (ln 2 / 1024)^i / i!
+    const float s = fmaf(x, high, kRound), n = s - kRound;
+    const float r = fmaf(x, low, fmaf(x, high, -n)), p = r * fmaf(r, c2, c1);
+    const unsigned bits = __float_as_uint(s);
+    const double power = table[bits & (kTable - 1)], e = fma(power, (double)p, power);
+    return __hiloint2double(__double2hiint(e) + (int)((bits & ~(unsigned)(kTable - 1)) << 10), __double2loint(e));
   }
 };
+
 // ---- keys ------------------------------------------------------------------------------------------------------------------
 // A logit and its token as a number that is larger for the better of two: the larger logit (-0 is 0), then the lower token.
 __device__ inline u64 key_of(float x, int token)
@@ -106,21 +113,26 @@ template <bool kTied> struct Candidates {
     const int lane = threadIdx.x & 63;
     u64 k[kRoom / kWave];
     int m[kRoom / kWave];
+    unsigned differ = 0;                             // bits of the upper words that are not the same in all
 #pragma unroll
     for (int j = 0; j < kRoom / kWave; ++j) {
       const int i = j * kWave + lane;
       k[j] = i < count ? keys[i] : 0;
       m[j] = kTied && i < count ? marks[i] : 0;
+      if (i < count) differ |= (unsigned)(k[j] >> 32) ^ (unsigned)__builtin_amdgcn_readfirstlane((int)(k[0] >> 32));
     }
+    for (int d = 1; d < kWave; d <<= 1) differ |= __shfl_xor(differ, d, kWave);
     auto reach = [&](u64 t) {
       int n = 0;
 #pragma unroll
       for (int j = 0; j < kRoom / kWave; ++j) n += __popcll(__ballot(k[j] >= t));
       return n;
     };
-    u64 t = 0;
+    // (from the first bit that differs on)
+    int bit = differ ? 63 - __clz(differ) : 31;
+    u64 t = read_lane(k[0], 0) & ~((2ull << bit) - 1);
     int n = count;
-    for (int bit = 63; bit >= 0 && n != most; --bit) {
+    for (; bit >= 0 && n != most; --bit) {
       const u64 higher = t | 1ull << bit;
       const int there = reach(higher);
       if (there >= most) { t = higher; n = there; }
@@ -154,7 +166,7 @@ template <bool kTied> struct Candidates {
     least = t;
     lds_sync();
   }
-  // after a cut: the lane's key, mark and place among at most 64
+  // the lane's key, mark and place among up to 64
   __device__ inline void rank(u64 &key, int &mark, int &place)
   {
     lds_sync();
@@ -198,7 +210,7 @@ __device__ inline bool last_to_arrive(int *counter, int n, int &arrived)
 template <bool kTied> __device__ inline void join_waves(Shared &s, Candidates<kTied> &mine)
 {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  mine.cut();                                        // at most 64 of each wave
+  if (mine.count > kWave) mine.cut();
   if (lane == 0) s.counts[wave] = mine.count;
   __syncthreads();
   if (wave == 0) {
@@ -206,7 +218,7 @@ template <bool kTied> __device__ inline void join_waves(Shared &s, Candidates<kT
       const bool there = lane < s.counts[w];
       mine.add(there, there ? s.keys[w][lane] : 0, kTied && there ? s.marks[w][lane] : 0);
     }
-    mine.cut();
+    if (mine.count > kWave) mine.cut();              // (up to 64 are ranked as they are)
   }
 }
 
@@ -275,6 +287,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
   float limit = -__builtin_inff(), m = 0;            // the K-th largest so far, or less; what exponents are relative to
   double sum = 0;
   bool bad = false;
+  // m is 0 unless a logit lies beyond kFar, or the first ones all below -kFar
   auto reference = [&](float now) {
     now = now > -3e38f && now < 3e38f ? now : 0.f;
     if (sum != 0) sum *= exp((double)m - now);
@@ -289,7 +302,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
       float top = y[0];
 #pragma unroll
       for (int i = 1; i < kEach; ++i) top = fmaxf(top, y[i]);
-      reference(lane_max(top));
+      if (__ballot(top >= -kFar) == 0) reference(lane_max(top));
       const unsigned k = (unsigned)(key_of(top, 0) >> 32);
       unsigned t = 0;
       for (int bit = 31; bit >= 0; --bit)
@@ -314,9 +327,13 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
       if (best.least > 1) limit = fmaxf(limit, logit_of(best.least));
       if (__ballot(top > m + kFar)) reference(lane_max(top));
     }
-    const float least = m - kLeast;
+    if (m == 0.f) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += s.exponentials.of((double)fmaxf(y[i], least) - m);
+      for (int i = 0; i < kEach; ++i) sum += s.exponentials.of(fmaxf(y[i], -kLeast));
+    } else {                                         // (differences need not be fp32's)
+#pragma unroll 1
+      for (int i = 0; i < kEach; ++i) sum += exp(fmax((double)y[i] - m, -(double)kLeast));
+    }
   };
   const int step = kWaves * kBeamTile;
   int v = from + wave * kBeamTile;

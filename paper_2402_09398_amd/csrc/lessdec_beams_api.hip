@@ -18,7 +18,7 @@ bool shape_ok(const lessdec_beam_desc *d)
 }
 
 // Parts of a row: as many as make kEnough workgroups of all rows, a tile for each wave at least.
-constexpr int kEnough = 2048;
+constexpr int kEnough = 1536;
 void split(const lessdec_beam_desc *d, int *parts, int *per)
 {
   const long rows = (long)d->groups * d->beams, unit = 4 * kBeamTile, units = (d->vocab + unit - 1) / unit;

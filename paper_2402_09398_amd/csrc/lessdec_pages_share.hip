@@ -188,7 +188,16 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     r.same[k] = (short)(r.a[i] == r.a[k] ? i : k);
     if (r.same[k] != k) continue;
     int j = k + 1;
-    while (j < n && r.a[j] >= r.a[k]) ++j;
+    for (bool more = true; more && j < n;) {         // eight at a time
+      int x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = r.a[min(j + q, n - 1)];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        more = more && j < n && x[q] >= r.a[k];
+        j += more;
+      }
+    }
     r.left[k] = (short)i;
     r.right[k] = (short)j;
   }
@@ -201,33 +210,29 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     }
     more = __syncthreads_or(more);
   }
-  // the slots of a run: least and largest position, and the first that has the least; a wave calls it
+  // the slots of a run: least and largest position, and the first that has the least
   auto extent = [&](int l, int e, int &lo, int &hi, int &read) {
-    lo = INT_MAX; hi = -1; read = 0;
-    for (int i = l + lane; i < e; i += kWave) {
+    lo = INT_MAX; hi = -1;
+    int at = l;
+#pragma unroll 4
+    for (int i = l; i < e; ++i) {
       const int x = lo_of(i);
-      if (x < lo) { lo = x; read = r.slot[i]; }
+      at = x < lo ? i : at;
+      lo = min(lo, x);
       hi = max(hi, r.hi[i]);
     }
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int other = __shfl_xor(lo, d, kWave), slot = __shfl_xor(read, d, kWave);
-      if (other < lo || (other == lo && slot < read)) { lo = other; read = slot; }
-      hi = max(hi, __shfl_xor(hi, d, kWave));
-    }
+    read = r.slot[at];
   };
   // which nodes are worth it, and what is around them
-  for (int k = wave; k < n; k += kWaves) {
+  for (int k = tid; k < n; k += kThreads) {
     if (r.same[k] != k) continue;
     const int l = r.left[k], e = r.right[k], below = e < n ? r.a[e] : 0, from = max(r.a[l], below);
     int lo, hi, read;
     extent(l, e, lo, hi, read);
     const long saved = (long)seen_blocks(c, lo, hi, from * per, r.a[k] * per) * kBlock * (e - l - 1);
-    if (lane == 0) {
-      if (from > 0) r.around[k] = r.same[r.a[l] >= below ? l : e];
-      r.worth[k] = saved >= (least_bytes < 0 ? kLeastSaved : 1);
-      if (r.worth[k]) atomicAdd(&saved_in_all, (unsigned long long)saved);
-    }
+    if (from > 0) r.around[k] = r.same[r.a[l] >= below ? l : e];
+    r.worth[k] = saved >= (least_bytes < 0 ? kLeastSaved : 1);
+    if (r.worth[k]) atomicAdd(&saved_in_all, (unsigned long long)saved);
   }
   __syncthreads();
   const bool none = saved_in_all * (2ull * c.heads * c.head_dim) < (unsigned long long)(least_bytes < 0 ? kLeastBytes : least_bytes);
@@ -255,14 +260,14 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     f[0] = make_int4(read, row, count, lo);
     f[1] = make_int4(hi, first, last, before);
   };
-  for (int k = wave; k < n; k += kWaves) {
+  for (int k = tid; k < n; k += kThreads) {
     if (r.same[k] != k || r.index[k] < 0) continue;
     const int l = r.left[k], e = r.right[k], up = r.near[k], row = r.row[l], end = r.row[e - 1] + r.rows[e - 1];
     int lo, hi, read;
     extent(l, e, lo, hi, read);
     // (a start that does not ascend gives a node without rows)
     const int count = end > row && (long)(end - row) * G <= (e - l) * (kTrunkTile - 1) ? end - row : 0;
-    if (lane == 0) record(r.index[k], read, row, count, lo, hi, (up < 0 ? 0 : r.a[up]) * per, r.a[k] * per, up < 0 ? -1 : r.index[up]);
+    record(r.index[k], read, row, count, lo, hi, (up < 0 ? 0 : r.a[up]) * per, r.a[k] * per, up < 0 ? -1 : r.index[up]);
   }
   // a slot's own part, behind its innermost node, which is that of the larger of its two boundaries
   int all_nodes = nodes, few = 0, short_ones = 0;
@@ -270,16 +275,14 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   // an entry of few columns for those threads that have one; all threads call it
   auto list = [&](bool mine, int blocks, int read, int row, int count, int lo, int hi, int first, int last, int column, bool several) {
     const bool brief = blocks <= kShortBlocks;
-    int all;
-    int at = few + scan((int)(mine && !brief), all);
-    few += all;
-    const int back = short_ones + scan((int)(mine && brief), all);
-    short_ones += all;
-    long steps;
-    scan((long)(mine && !brief ? (blocks + kFewBlocks - 1) / kFewBlocks : 0), steps);
-    few_steps += steps;
+    // three sums in one word: entries, short ones, steps
+    long all;
+    const long before = scan(!mine ? 0L : brief ? 1L << 14 : 1L | (long)((blocks + kFewBlocks - 1) / kFewBlocks) << 28, all);
+    const int at = brief ? 3 * N - 1 - (short_ones + (int)(before >> 14 & 16383)) : few + (int)(before & 16383);
+    few += (int)(all & 16383);
+    short_ones += (int)(all >> 14 & 16383);
+    few_steps += all >> 28;
     if (!mine) return;
-    if (brief) at = 3 * N - 1 - back;
     int4 *f = reinterpret_cast<int4 *>(plan.few + (long)at * kNodeInts);
     const int step = brief ? 2 : kFewBlocks;
     f[0] = make_int4(max((blocks + step - 1) / step, 1), read, row, count);
