@@ -49,6 +49,7 @@ class BeamSearch:
         d.workspace, d.workspace_bytes = self.workspace.data_ptr(), need
         self.desc = d
         self._bools = (torch.uint8, torch.bool)
+        self._pointer, self._lib, self._current = C.pointer(d), lib(), (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
 
     def _flat(self, t, count, types, what):
         if t.dtype not in types or t.numel() != count or not t.is_contiguous() or t.device != self.device:
@@ -68,6 +69,12 @@ class BeamSearch:
                 self._flat(parent, n, (torch.int32,), "parent"), self._flat(token, n, (torch.int32,), "token"),
                 self._flat(next_score, n, (torch.float32,), "next_score"),
                 None if next_ended is None else self._flat(next_ended, n, self._bools, "next_ended"))
-        with torch.cuda.device(self.device):
-            s = torch.cuda.current_stream() if stream is None else stream
-            _check(lib().lessdec_beam_select(C.byref(self.desc), *args, s.cuda_stream), "lessdec_beam_select")
+        raw_stream, device = self._current
+        s = raw_stream(self.device.index) if stream is None else stream.cuda_stream
+        if device() == self.device.index:
+            rc = self._lib.lessdec_beam_select(self._pointer, *args, s)
+        else:
+            with torch.cuda.device(self.device):
+                rc = self._lib.lessdec_beam_select(self._pointer, *args, s)
+        if rc:
+            _check(rc, "lessdec_beam_select")

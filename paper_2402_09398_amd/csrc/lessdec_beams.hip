@@ -4,11 +4,15 @@
 // pairs are its largest logits (ties: the lower token), found exactly and without any exponential; lse is only needed to compare beams.
 // It decides between them, so it is formed in fp64, like everything here that decides.
 //
-// One pass over the logits.  A workgroup has a part of a row, its waves take turns at tiles of 512 logits.  A wave keeps the sum of e^{x - m}
-// for an m near its first tile's largest (anything within 500 does in fp64, so m hardly ever moves) and a list of candidates in the LDS:
-// what is larger than the K-th largest so far joins it, and when it is full it is cut to the K largest.  The last workgroup of
+// One pass over the logits.  A workgroup has a part of a row, its waves take turns at tiles of 512 logits.  A wave keeps the sum of e^{x - m},
+// where m is 0 (fp64 takes e^{+-350}) unless logits lie further out, and a list of candidates in the LDS: what is larger than a lower bound of the
+// K-th largest so far joins it, and when it is full it is cut to the K largest.  The last workgroup of
 // a row joins the parts, the last of a prompt joins its rows, all in the one launch; every sum has an order of its own that depends on
 // sizes alone, and rows of the same logits have the same lse to the bit.
+//
+// Bound by the vector instructions of the exponentials, 18 a logit (65 us and 41 by a polynomial of degree 10 alone, 50 and 27 with remainders in fp32,
+// whose error of 1e-10 was not wanted); small calls by a chain of latencies.  64 prompts of 4 beams, 128256 logits in bfloat16: 45 us (1.5 TB/s); 16 of
+// 8, 50257 in fp32, 16 picks: 28; one of 4, 32000 in fp16: 14.
 #include "lessdec_beams.h"
 
 namespace lessdec {
@@ -21,14 +25,13 @@ typedef unsigned u4a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 4 * kWave, kEach = kBeamTile / kWave;
 static_assert(kEach == 8, "eight logits a lane and tile");
-constexpr float kFar = 500.f;                        // logits up to here are taken as they are: e^500 times 2^28 is within fp64
-constexpr float kLeast = 700.f;                      // what lies further below counts as e^-700
+// Logits in [-kLeast, kFar] are taken as they are, what lies further below counts as e^-kLeast: less than e^-100 of a wave's first ones, or m is not 0.
+constexpr float kFar = 250.f, kLeast = 350.f;
 
-// ---- e^x to fp64 -----------------------------------------------------------------------------------------------------------
-// 2^{y / 1024} with y = 1024 x / ln 2 = n + r, |r| <= 1/2: a table of 2^{i / 1024} in fp64, i = n mod 1024, times 2^{r / 1024} = 1 + p, times
-// 2^{n / 1024 - i / 1024} by addition to the exponent.  x is an fp32, so that r, from the exact products of its fmas, and p = r (c1 + c2 r) <= 3.4e-4 may be
-// fp32, too: p is within 1e-10 of its 3.4e-4, and what the polynomial leaves out is 6.5e-12 at most.  -kLeast <= x <= kFar.
-constexpr int kTable = 1024;
+// ---- e^x in fp64 -----------------------------------------------------------------------------------------------------------
+// 2^{y / 512} with y = 512 x / ln 2 = n + r, |r| <= 1/2: a table of 2^{i / 512}, i = n mod 512, times a polynomial of degree 3 for 2^{r / 512}
+// (its next term is 8.8e-15 at most), times 2^{n / 512 - i / 512} by addition to the exponent.  -kLeast <= x <= kFar.
+constexpr int kTable = 512;
 struct Exponentials {
   double table[kTable];
   __device__ inline void fill()
@@ -37,15 +40,14 @@ struct Exponentials {
   }
   __device__ inline double of(float x) const
   {
-    constexpr float kRound = 12582912.f;             // 1.5 * 2^23: its sum with y has n in the low bits
-    constexpr double kPer = 1477.3197218702985;      // 1024 / ln 2
-    constexpr float high = (float)kPer, low = (float)(kPer - (double)high);
-    constexpr float c1 = 6.7690154351557157e-04f, c2 = 2.2909784980648572e-07f;        // (ln 2 / 1024)^i / i!
-    const float s = fmaf(x, high, kRound), n = s - kRound;
-    const float r = fmaf(x, low, fmaf(x, high, -n)), p = r * fmaf(r, c2, c1);
-    const unsigned bits = __float_as_uint(s);
-    const double power = table[bits & (kTable - 1)], e = fma(power, (double)p, power);
-    return __hiloint2double(__double2hiint(e) + (int)((bits & ~(unsigned)(kTable - 1)) << 10), __double2loint(e));
+    constexpr double kRound = 6755399441055744.0;    // 1.5 * 2^52: its sum with y has n in the low word
+    constexpr double kPer = 738.65986093514926;      // 512 / ln 2
+    constexpr double c1 = 1.3538030870311431e-03, c2 = 9.1639139924594288e-07, c3 = 4.1353744987218336e-10;    // (ln 2 / 512)^i / i!
+    const double s = fma((double)x, kPer, kRound);
+    const int n = (int)__double2loint(s);
+    const double r = fma((double)x, kPer, kRound - s), p = r * fma(r, fma(r, c3, c2), c1);
+    const double power = table[n & (kTable - 1)], e = fma(power, p, power);
+    return __hiloint2double(__double2hiint(e) + (int)((unsigned)(n & ~(kTable - 1)) << 11), __double2loint(e));
   }
 };
 
@@ -285,63 +287,68 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
   Candidates<false> best;
   best.start(s.keys[wave], nullptr, a.picks);
   float limit = -__builtin_inff(), m = 0;            // the K-th largest so far, or less; what exponents are relative to
+  float seen = -__builtin_inff();                    // the lane's largest
+  int tile = 0, look = 0;
   double sum = 0;
-  bool bad = false;
+  bool bad = false, any = false;                     // (any: a logit above -inf)
   // m is 0 unless a logit lies beyond kFar, or the first ones all below -kFar
   auto reference = [&](float now) {
     now = now > -3e38f && now < 3e38f ? now : 0.f;
     if (sum != 0) sum *= exp((double)m - now);
     m = now;
   };
-  auto work = [&](const L &l, int v, bool first) {
+  auto work = [&](const L &l, int v) {
     float y[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) y[i] = l.get(i);
-    if (first) {
-      // every lane's largest: the K-th largest of them is reached by K logits at least
-      float top = y[0];
-#pragma unroll
-      for (int i = 1; i < kEach; ++i) top = fmaxf(top, y[i]);
-      if (__ballot(top >= -kFar) == 0) reference(lane_max(top));
-      const unsigned k = (unsigned)(key_of(top, 0) >> 32);
-      unsigned t = 0;
-      for (int bit = 31; bit >= 0; --bit)
-        if (__popcll(__ballot(k >= (t | 1u << bit))) >= a.picks) t |= 1u << bit;
-      // just below, which of 0 is not the -0 that comes before it in these numbers; -inf at least
-      limit = logit_of((u64)(t > 0x007fffffu ? t - 1 - (t == 0x80000000u) : 0x007fffffu) << 32);
-    }
     bool more = false;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) more |= !(y[i] <= limit);
     if (__ballot(more)) {
-      float top = -__builtin_inff();
+      float top = y[0];
+#pragma unroll
+      for (int i = 1; i < kEach; ++i) top = fmaxf(top, y[i]);
+      seen = fmaxf(seen, top);
+      if (!any && __ballot(top >= -kFar) == 0) reference(lane_max(top));
+      any = true;
+      if (__ballot(top > m + kFar)) reference(lane_max(top));
+      if (tile >= look) {
+        // the K-th largest of the lanes' largest is reached by K logits at least: asked for after 1, 2, 4, .. tiles
+        look = 2 * tile + 1;
+        const unsigned k = (unsigned)(key_of(seen, 0) >> 32);
+        unsigned t = 0;
+        for (int bit = 31; bit >= 0; --bit)
+          if (__popcll(__ballot(k >= (t | 1u << bit))) >= a.picks) t |= 1u << bit;
+        // just below, which of 0 is not the -0 that comes before it in these numbers; -inf at least
+        limit = fmaxf(limit, logit_of((u64)(t > 0x007fffffu ? t - 1 - (t == 0x80000000u) : 0x007fffffu) << 32));
+      }
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const bool wanted = !(y[i] <= limit);
+        if (!__ballot(wanted)) continue;
         bad |= wanted && !(y[i] < __builtin_inff());                   // NaN or infinite
-        top = fmaxf(top, y[i]);
         const u64 key = key_of(y[i], v + i);
         best.add(wanted && key >= best.least, key, 0);
       }
       // (only now, as tokens of a tile do not come in order; those of later tiles lose a tie)
       if (best.least > 1) limit = fmaxf(limit, logit_of(best.least));
-      if (__ballot(top > m + kFar)) reference(lane_max(top));
     }
     if (m == 0.f) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) sum += s.exponentials.of(fmaxf(y[i], -kLeast));
+      for (int i = 0; i < kEach; ++i) sum += s.exponentials.of(__builtin_amdgcn_fmed3f(y[i], -kLeast, kFar));
     } else {                                         // (differences need not be fp32's)
 #pragma unroll 1
-      for (int i = 0; i < kEach; ++i) sum += exp(fmax((double)y[i] - m, -(double)kLeast));
+      for (int i = 0; i < kEach; ++i) sum += exp((double)y[i] - m);
     }
   };
   const int step = kWaves * kBeamTile;
   int v = from + wave * kBeamTile;
   L now, next;
   if (v < to) load(now, v + lane * kEach);
-  for (bool first = true; v < to; v += step, first = false) {
+  for (; v < to; v += step) {
     if (v + step < to) load(next, v + step + lane * kEach);
-    work(now, v + lane * kEach, first);
+    work(now, v + lane * kEach);
+    ++tile;
     now = next;
   }
   sum = lane_sum(sum);
@@ -378,6 +385,8 @@ __device__ inline void join_parts(const BeamArgs &a, int row, bool ended, Shared
     }
     return;
   }
+  const u64 *sums = a.sums + 2 * (long)row * a.parts;
+  const u64 m_of = get(sums + 2 * min(lane, a.parts - 1)), part_of = get(sums + 2 * min(lane, a.parts - 1) + 1);
   const u64 *lists = a.lists + (long)row * a.parts * a.picks;
   const int n = a.parts * a.picks;
   Candidates<false> best;
@@ -389,9 +398,7 @@ __device__ inline void join_parts(const BeamArgs &a, int row, bool ended, Shared
   }
   join_waves(s, best);
   if (wave) return;
-  const u64 *sums = a.sums + 2 * (long)row * a.parts;
-  const double m = lane < a.parts ? __longlong_as_double(get(sums + 2 * lane)) : -__builtin_inf();
-  const double part = lane < a.parts ? __longlong_as_double(get(sums + 2 * lane + 1)) : 0;
+  const double m = lane < a.parts ? __longlong_as_double(m_of) : -__builtin_inf(), part = lane < a.parts ? __longlong_as_double(part_of) : 0;
   double top = m;
   for (int d = 1; d < kWave; d <<= 1) top = fmax(top, __shfl_xor(top, d, kWave));
   const double lse = top + log(lane_sum(lane < a.parts ? part * exp(m - top) : 0));
@@ -431,7 +438,7 @@ __device__ inline void join_rows(const BeamArgs &a, int group, Shared &s)
   if (a.next_ended) a.next_ended[to] = key && token == a.end_token;
 }
 
-template <int DTYPE> __global__ __launch_bounds__(kThreads) void beam_kernel(BeamArgs a)
+template <int DTYPE> __global__ __launch_bounds__(kThreads, 5) void beam_kernel(BeamArgs a)
 {
   __shared__ Shared s;
   const int row = blockIdx.x / (unsigned)a.parts, part = blockIdx.x % (unsigned)a.parts, group = row / a.beams;

@@ -17,8 +17,8 @@ bool shape_ok(const lessdec_beam_desc *d)
   return d->end_token >= -1 && d->end_token < d->vocab;
 }
 
-// Parts of a row: as many as make kEnough workgroups of all rows, a tile for each wave at least.
-constexpr int kEnough = 1536;
+// Parts of a row: as many as make kEnough workgroups of all rows (five to a compute unit, which the registers hold), a tile for each wave at least.
+constexpr int kEnough = 1280;
 void split(const lessdec_beam_desc *d, int *parts, int *per)
 {
   const long rows = (long)d->groups * d->beams, unit = 4 * kBeamTile, units = (d->vocab + unit - 1) / unit;

@@ -1,5 +1,5 @@
 """lessdec_beam_select on the GPU, through BeamSearch, against tests/beams_oracle.py: parents and tokens exactly, scores to half a step of
-fp32 (2^-24 of the value) and what the exponentials allow (1.4e-13, and roundings of fp64 over the sums: 1e-11 covers both)."""
+fp32 (2^-24 of the value) and what the sums allow: exponentials to 1e-14, at most 2^17 additions of 2^-53 one behind the other: 1e-11 covers both."""
 import numpy as np
 import pytest
 
