@@ -19,6 +19,8 @@
 // so the weights never leave their registers.  They are rounded to fp16 for it, the sum's are not: fp16 outputs are off by 2.6e-4 of their size in place of the
 // 2.1e-4 of fp32 weights and the output's own rounding, bfloat16 ones by 1.7e-3 either way (the cases of perf/operators.py).  A query column is a (row, query head of the group) pair: the heads of a group share the
 // cached keys and values that a tile has loaded.
+#include <type_traits>
+
 #include "lessdec_pages.h"
 
 namespace lessdec {
@@ -134,14 +136,15 @@ struct Top {
 // The blocks of 16 tokens that rows at positions lo .. hi see some token of, as a list: the first ones, then those of the window.
 struct Span {
   int sinks, window, count;                          // blocks of the first tokens; the window's first block; blocks in all
-  int skip;                                          // blocks before the list's first, where it is cut
-  __device__ inline int block(int i) const
-  {
-    i += skip;
-    return i < sinks ? i : i - sinks + window;
-  }
-  __device__ inline int place(int block) const { return min(block, sinks) + max(block - window, 0); }       // blocks of the list (uncut) before this one
-  __device__ inline void cut(int first, int last)    // to blocks first .. last - 1
+  __device__ inline int block(int i) const { return i < sinks ? i : i - sinks + window; }
+};
+// Some of such a list.
+struct Cut : Span {
+  int skip;                                          // blocks before its first
+  __device__ inline int block(int i) const { return Span::block(i + skip); }
+  __device__ inline int place(int block) const { return min(block, sinks) + max(block - window, 0); }       // blocks of the whole list before this one
+  __device__ inline Cut() {}
+  __device__ inline Cut(const Span &whole, int first, int last) : Span(whole) // those of blocks first .. last - 1
   {
     skip = min(place(first), count);
     count = max(min(place(last), count) - skip, 0);
@@ -149,7 +152,7 @@ struct Span {
 };
 __device__ inline Span span_of(const Pages &c, int lo, int hi)
 {
-  Span s = {0, 0, 0, 0};
+  Span s = {0, 0, 0};
   if (hi < 0) return s;
   const int last = hi / kBlock;
   if (c.window > 0 && lo >= c.window) {
@@ -175,9 +178,17 @@ __device__ inline int inner_first(const Pages &c, const Span &s, int hi)
 {
   if (c.window == 0 || hi < c.window) return 0;
   const int block = (hi - c.window + kBlock) / kBlock;                 // the first whose tokens are all > hi - window
+  return (max(block - s.window, 0) + s.sinks + 3) / 4;
+}
+__device__ inline int inner_last(const Span &s, int lo) { return max((lo + 1) / kBlock - s.window + s.sinks, 0) / 4; }
+// (of some of a list, which may end before the rows do)
+__device__ inline int inner_first(const Pages &c, const Cut &s, int hi)
+{
+  if (c.window == 0 || hi < c.window) return 0;
+  const int block = (hi - c.window + kBlock) / kBlock;
   return (max(max(block - s.window, 0) + s.sinks - s.skip, 0) + 3) / 4;
 }
-__device__ inline int inner_last(const Span &s, int lo) { return max((lo + 1) / kBlock - s.window + s.sinks - s.skip, 0) / 4; }
+__device__ inline int inner_last(const Cut &s, int lo) { return min(max((lo + 1) / kBlock - s.window + s.sinks - s.skip, 0), s.count) / 4; }
 __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 
 // ---- slots that share pages --------------------------------------------------------------------------------------------
@@ -447,7 +458,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
 
     Rows rows;
     int lo, hi, p, read = s, base_column = -1;
-    Span span;
+    std::conditional_t<kShares<Args>, Cut, Span> span;
     if constexpr (kShares<Args>) {
       const int4 *f = reinterpret_cast<const int4 *>(a.plan.few + (long)(kAlone ? 3 * c.slots - 1 - s : s) * kNodeInts);
       const int4 x = f[0], y = f[1], z = f[2];
@@ -458,8 +469,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
       rows.count = min(max(same(x.w), 0), a.rows - rows.first);
       lo = min(max(same(y.x), 0), most - 1);
       hi = min(max(same(y.y), -1), most - 1);
-      span = span_of(c, lo, hi);
-      span.cut(max(same(y.z), 0), min(max(same(y.w), 0), c.table_len * page_blocks(c)));
+      span = Cut(span_of(c, lo, hi), max(same(y.z), 0), min(max(same(y.w), 0), c.table_len * page_blocks(c)));
       base_column = same(z.x);
       p = hi + 1 - rows.count + n / G;
       if (same(z.y)) p = n < rows.count * G ? min(max(a.plan.pos[rows.first + n / G], -1), most - 1) : -1;
@@ -471,7 +481,7 @@ __device__ __forceinline__ void few_rows(const Pages &c, const Args &a, int work
       span = span_of(c, lo, hi);
       p = lo + n / G;
     }
-    const int cols = min(rows.count * G, kCols), mine = kAlone ? 0 : wave * 2;
+    const int cols = kShares<Args> ? min(rows.count * G, kCols) : rows.count * G, mine = kAlone ? 0 : wave * 2;
     u4 q[H][2];
 #pragma unroll
     for (int h = 0; h < H; ++h)
@@ -823,10 +833,7 @@ template <typename Args> __device__ inline bool columns_of(const Pages &c, const
   return true;
 }
 
-template <int D> struct WideShared {
-  __align__(16) u4 tiles[4][kTile * D / 8];
-  int spoiled;
-};
+template <int D> using Tiles = u4[4][kTile * D / 8];  // of keys, two, and of values
 // A piece of the nodes' tiles: 128 columns of a node by one head, tiles [from, to), the piece-th of these columns.
 struct Piece {
   Node node;
@@ -834,444 +841,17 @@ struct Piece {
   bool only;                                         // the chunk has no second piece
 };
 
-// Item `id` of a launch, or with kTrunk a piece of the plan's.
-template <bool BF16, int D, bool kTrunk, typename Args>
-__device__ __forceinline__ void wide_item(const Pages &c, const Args &a, unsigned id, unsigned items, int splits, const Piece &trunk, WideShared<D> &shared)
-{
-  constexpr int H = D / 64, KK = D / 16, OB = D / 32;
-  auto &spoiled = shared.spoiled;
-  auto keys = shared.tiles, values = shared.tiles + 2;
-  const int wave = __builtin_amdgcn_readfirstlane(thread_of<Args>() >> 6), lane = thread_of<Args>() & 63, n = lane & 31, h = lane >> 5;
-  const int G = c.q_per_kv;
-  const int split = kTrunk ? 0 : id % (unsigned)splits;
-  const unsigned item = kTrunk ? 0 : id / (unsigned)splits;
-  const int head = kTrunk ? trunk.head : item / items;
-  Columns t;
-  Rows rows;
-  Span span;
-  int from, to, lo, hi, wave_lo, wave_hi, p;
-  if constexpr (kTrunk) {
-    t = Columns{trunk.node.slot, trunk.column, trunk.node.cols, 0};
-    rows = Rows{trunk.node.row, trunk.node.rows};
-    span = span_of(c, trunk.node.lo, trunk.node.hi);
-    span.cut(trunk.node.first, trunk.node.last);
-    from = trunk.from;
-    to = min((span.count + 3) / 4, trunk.to);
-  } else {
-    if (!columns_of(c, a, item % items, splits == 1 && c.slots <= kWave, t, rows)) return;
-  }
-  const int before = t.len - rows.count;
-  const int last_col = min(t.first + kWide, t.count) - 1;
-  // this wave's columns
-  const int col = t.first + wave * 32 + n;
-  const bool have = t.first + wave * 32 <= last_col;
-  const int row = rows.first + col / G, q_head = head * G + col % G;
-  if constexpr (kTrunk) {
-    // rows of several slots, their positions in any order as the plan has them; what tiles all of them see is known from the least and the largest
-    p = col <= last_col ? min(max(a.plan.pos[row], -1), c.table_len * c.page_tokens - 1) : -1;
-    lo = wave_lo = trunk.node.lo;
-    hi = wave_hi = trunk.node.hi;
-  } else {
-    lo = before + t.first / G;
-    hi = before + last_col / G;
-    span = span_of(c, lo, hi);
-    const int tiles = (span.count + 3) / 4, each = max(2, (tiles + splits - 1) / splits);
-    from = split * each;
-    to = min(tiles, from + each);
-    wave_lo = before + (t.first + wave * 32) / G;
-    wave_hi = before + min(t.first + wave * 32 + 31, last_col) / G;
-    // the row, at p, sees the tokens from_token .. p and those before first_tokens
-    p = col <= last_col ? before + col / G : -1;
-  }
-  const int from_token = c.window > 0 ? max(max(p, 0) - c.window + 1, 0) : 0, first_tokens = c.window > 0 ? min(c.sinks, p + 1) : 0;
-  u4 q[KK];
-#pragma unroll
-  for (int k = 0; k < KK; ++k) {
-    q[k] = u4{0, 0, 0, 0};
-    if (col <= last_col) q[k] = reinterpret_cast<const u4 *>(a.q)[row * (a.stride / 8) + q_head * (D / 8) + k * 2 + h];
-  }
-
-  // Tiles that all rows of the workgroup, of this wave, see in full: a range [first, last) of the list, none where a page of the
-  // slot is missing (which the look-ups below find before such a tile is reached).
-  const int all_first = inner_first(c, span, hi), mine_first = inner_first(c, span, wave_hi);
-  int all_last = inner_last(span, lo), mine_last = inner_last(span, wave_lo);
-  if constexpr (kTrunk) {                            // (a list that ends before the rows do)
-    all_last = min(all_last, span.count / 4);
-    mine_last = min(mine_last, span.count / 4);
-  }
-
-  // Blocks are looked up for sixteen tiles at a time, a lane each: the table a chunk ahead, the exponents half a chunk ahead.
-  constexpr int kChunk = kWave / 4;
-  const int *table = c.table + (size_t)t.slot * c.table_len;
-  int chunk = from, page, at, at_next, exps_next;    // at: the lane's block in the pool, -1: not there
-  float factor, shift, unit;                         // of the lane's block: t = factor x + shift; its weights add to the sum times unit
-  auto look = [&](int tile) {                        // of the chunk that begins with this tile
-    const int i = tile * 4 + lane;
-    page = table[i < to * 4 && i < span.count ? entry_of(c, span.block(i)) : 0];      // (not looked at here: it is on its way)
-  };
-  auto place = [&](int tile) {
-    const int i = tile * 4 + lane;
-    at_next = i < to * 4 && i < span.count ? block_in(c, page, head, span.block(i)) : -1;
-    exps_next = reinterpret_cast<const unsigned short *>(c.exps)[max(at_next, 0)];
-    if (__ballot(at_next < 0 && i < to * 4 && i < span.count)) all_last = mine_last = 0;
-  };
-  auto turn = [&] {
-    at = at_next;
-    const int ex = at < 0 ? 0 : exps_next;           // (of what is not there the load gave any block's: powers of two that are no numbers, perhaps)
-    factor = pow2((signed char)ex) * c.scale_log2;
-    const int e = (signed char)(ex >> 8);
-    shift = (float)e;
-    unit = pow2(-e);
-  };
-  auto at_of = [&](int tile, int b) {
-    const int i = tile - chunk;
-    return __builtin_amdgcn_readlane(i < kChunk ? at : at_next, i % kChunk * 4 + b);
-  };
-
-  // Staging.  A wave brings halves of 64 channels of a block: D = 128 two of them (blocks wave / 2 and wave / 2 + 2), D = 64 one.  Every load
-  // is made (of the pool's first block where there is none to read).
-  u4 kc[H], vc[H];
-  auto piece_block = [&](int j) { return H == 2 ? wave / 2 + 2 * j : wave; };
-  const int half = H == 2 ? wave % 2 : 0;
-  auto request = [&](int tile) {
-    if (tile >= to) return;
-#pragma unroll
-    for (int j = 0; j < H; ++j) {
-      const int block = max(at_of(tile, piece_block(j)), 0);
-      const Bytes k = scalar_bytes(c.k, block * ((long)kBlock * D)), v = scalar_bytes(c.v, block * ((long)kBlock * D));
-      kc[j] = *(Pieces)(k + (unsigned)(half * kWave + lane) * 16);
-      vc[j] = *(Pieces)(v + (unsigned)(half * kWave + lane) * 16);
-    }
-  };
-  // A node's tokens are in no L2 yet: a word of every line of the tile that comes kAhead later is read, so that they are when it is requested (a
-  // wave has a block: sixteen lines of 16 D / 128 keys each, and as many of values).
-  constexpr int kAhead = 5;
-  unsigned touched = 0, touching = 0;
-  auto touch = [&](int tile) {
-    const int block = max(at_of(min(tile, to - 1), wave), 0);
-    constexpr int kLines = kBlock * D / 128;
-    const unsigned char *line = ((lane & kLines) ? c.v : c.k) + block * ((long)kBlock * D) + (unsigned)(lane % kLines) * 128;
-    touched |= touching;                             // (the one before is waited for here, a tile later)
-    touching = *reinterpret_cast<const unsigned *>(line);
-  };
-  // where a word of four tokens' codes of channel 64 half + 16 i + (lane & 15) goes: [block][32 channels][which eight of the 16
-  // tokens][channel], tokens 0-3 and 8-11, or 4-7 and 12-15
-  auto value_at = [&](int j, int i) {
-    const int d = half * 64 + i * 16 + (lane & 15), g = lane >> 4;
-    return (((piece_block(j) * OB + d / 32) * 2 + (g & 1)) * 32 + d % 32) * 2 + (g >> 1);
-  };
-  bool mine_spoiled = false;
-  auto stage = [&](int tile, int buf) {
-    const int tok = lane & 15, g = lane >> 4;
-    // what no row sees is left out, and a NaN among values that only some rows see is taken out (0 * NaN is NaN) and given to those
-    // that see it in the end
-    if (tile < all_first || tile >= all_last) {
-#pragma unroll
-      for (int j = 0; j < H; ++j) {
-        const bool there = at_of(tile, piece_block(j)) >= 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned bad = code_nans(vc[j][i]);
-          mine_spoiled |= there && bad != 0;
-          vc[j][i] = there ? vc[j][i] & ~bad : 0;
-        }
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < H; ++j) {
-      const int b = piece_block(j);
-      // key operands: [32 tokens][16 channels][half of 8 channels][token]
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        keys[buf][(((b >> 1) * KK + half * 4 + g) * 2 + e) * 32 + (b & 1) * 16 + tok] = widen<BF16>(kc[j][2 * e], kc[j][2 * e + 1]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        reinterpret_cast<uint2 *>(values[buf])[value_at(j, i)] = make_uint2(Operand<false>::pair(vc[j][i], false), Operand<false>::pair(vc[j][i], true));
-    }
-  };
-
-  f16v acc[OB];
-#pragma unroll
-  for (int o = 0; o < OB; ++o) acc[o] = f16v{0};
-  Top top = {kLowest, kFirstE};
-  float level = kLowest;                             // M less kBase, in one
-  unsigned long long far = 0;                        // lanes whose M is beyond kNear (as a bool 587 us at 8192 tokens, 32 heads, so 571)
-  float sum = 0;
-  if (threadIdx.x == 0) spoiled = 0;
-  if (from < to) {
-    look(from);
-    place(from);
-    turn();
-    look(from + kChunk);
-    request(from);
-    stage(from, from & 1);
-    request(from + 1);
-  }
-
-  // A tile's 64 tokens are worked on as two halves: the scores of the second are multiplied while the weights of the first are
-  // computed, and its weights while the first half's go into the values.
-  bool whole, active;
-  float f[4], add[4], units[4];
-  f16v x[2];
-  auto enter = [&](int tile) {
-    const int i = (tile - chunk) * 4;
-    whole = tile >= mine_first && tile < mine_last;
-    active = have;
-    if (!whole) {
-      bool some = false;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int t0 = span.block(tile * 4 + b) * kBlock;
-        some |= at_of(tile, b) >= 0 && t0 <= wave_hi && (c.window == 0 || t0 + kBlock + c.window > wave_lo || t0 < c.sinks);
-      }
-      active &= some;
-    }
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      f[b] = read_lane(factor, i + b);
-      add[b] = read_lane(shift, i + b);
-      units[b] = read_lane(unit, i + b);
-    }
-  };
-  // The operands of a product are read from the LDS ahead of what comes before it, so that it does not wait (8192 tokens, 32 heads, a call
-  // at a time: 624 us; with the first half of them ahead 631.  Each read as soon as the product before has used its registers: 628, and 657
-  // with the barrier before a tile's last product, which then meets no wait for the LDS at all).
-  static_assert(KK == 2 * OB, "as many operands of keys as of values");
-  u4 ahead[KK];
-  auto keys_ahead = [&](int buf, int m) {
-#pragma unroll
-    for (int k = 0; k < KK; ++k) ahead[k] = keys[buf][(m * KK + k) * 64 + lane];
-  };
-  auto values_ahead = [&](int buf, int m) {
-#pragma unroll
-    for (int o = 0; o < KK; ++o) ahead[o] = values[buf][(m * KK + o) * 64 + lane];
-  };
-  auto scores = [&](int m) {
-    x[m] = f16v{0};
-#pragma unroll
-    for (int k = 0; k < KK; ++k) x[m] = Operand<BF16>::mma32(ahead[k], q[k], x[m]);
-  };
-  // Which of the lane's eight tokens of a block the row sees is a word of bits (four compares a score took 470
-  // us at 40 heads, 4 x 4096 tokens, a window of 820, two 440, this 415).
-  auto mask = [&](int tile, int m) {
-    auto below = [](int n) { return (1u << min(max(n, 0), 12)) - 1; };
-#pragma unroll
-    for (int b = 2 * m; b < 2 * m + 2; ++b) {
-      const int t0 = span.block(tile * 4 + b) * kBlock + 4 * h;        // the lane has t0 .. t0 + 3 and t0 + 8 .. t0 + 11
-      unsigned seen = (below(p + 1 - t0) & ~below(from_token - t0)) | below(first_tokens - t0);
-      if (at_of(tile, b) < 0) seen = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const unsigned all = (unsigned)((int)(seen << (31 - (i & 3) - 8 * (i >> 2))) >> 31);
-        x[m][b % 2 * 8 + i] = __uint_as_float((__float_as_uint(x[m][b % 2 * 8 + i]) & all) | (0xff800000u & ~all));
-      }
-    }
-  };
-  // Weights of half m, and what they add to the sum (before 2^-e).  Whether one is too large for fp16 shows in these, so the maximum is
-  // only looked for where one is, or where scores are far from 0: then M is moved and the weights are computed again, each step rounded by itself.
-  u4 weights[2];
-  float part[2];
-  auto weigh = [&](int m) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const float zero = add[2 * m + b] - level;
-      part[b] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float y = exp2_fast(fmaf(x[m][b * 8 + i], f[2 * m + b], zero)), z = exp2_fast(fmaf(x[m][b * 8 + i + 1], f[2 * m + b], zero));
-        part[b] += y + z;
-        weights[b][i / 2] = half_pair(y, z);
-      }
-    }
-  };
-  auto weigh_exactly = [&](int m) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const float factor = f[2 * m + b], e = add[2 * m + b] - top.e;
-      part[b] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float y = exp2_fast((product(x[m][b * 8 + i], factor) - top.s) + e), z = exp2_fast((product(x[m][b * 8 + i + 1], factor) - top.s) + e);
-        part[b] += y + z;
-        weights[b][i / 2] = half_pair(y, z);
-      }
-    }
-  };
-  auto settle = [&](int m) {
-    if (far | __ballot(fmaxf(part[0], part[1]) > kMost)) {
-      Top most;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float y = x[m][b * 8];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) y = fmaxf(y, x[m][b * 8 + i]);      // (the factor is positive)
-        const float score = product(y, f[2 * m + b]), e = add[2 * m + b] - kBase;
-        if (b == 0) most = Top{score, e};
-        else most.raise(score, e);
-      }
-      most.raise_over<32>();
-      const Top was = top;
-      top.raise(most.s, most.e);
-      const float less = exp2_fast(top.above(was.s, was.e));
-      level = top.s + top.e;
-      far = __ballot(fabsf(top.s) > kNear && top.s > kLowest);
-      sum *= less;
-#pragma unroll
-      for (int o = 0; o < OB; ++o) acc[o] *= less;
-      weigh_exactly(m);
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b) sum = fmaf(part[b], units[2 * m + b], sum);
-  };
-  auto gather = [&](const u4 (&w)[2]) {
-#pragma unroll
-    for (int o = 0; o < KK; ++o) acc[o % OB] = Operand<false>::mma32(ahead[o], w[o / OB], acc[o % OB]);
-  };
-#pragma unroll
-  for (int k = 0; k < KK; ++k) asm volatile("" : "+v"(q[k]));          // the queries are waited for here, not (with all codes requested since) in the loop
-  __syncthreads();
-  if (from < to) {
-    enter(from);
-    if (active) {
-      keys_ahead(from & 1, 0);
-      scores(0);
-      if (!whole) mask(from, 0);
-    }
-  }
-  for (int tile = from; tile < to; ++tile) {
-    const int buf = tile & 1;
-    __builtin_amdgcn_s_setprio(0);
-    keys_ahead(buf, 1);
-    if (tile - chunk == kChunk / 2) place(chunk + kChunk);
-    if (tile + 1 < to) {                             // (requested a round ago)
-      stage(tile + 1, buf ^ 1);
-      request(tile + 2);
-    }
-    if constexpr (kTrunk) touch(tile + kAhead);
-    if (active) {
-      // products before the other workgroup's staging: 661 -> 621 us at 32 heads x 8192 tokens, clocks settled
-      __builtin_amdgcn_s_setprio(1);
-      scores(1);
-      weigh(0);
-      values_ahead(buf, 0);
-      settle(0);
-      if (!whole) mask(tile, 1);
-      const u4 first[2] = {weights[0], weights[1]};
-      gather(first);
-      weigh(1);
-      values_ahead(buf, 1);
-      settle(1);
-      gather(weights);
-    }
-    if (tile + 1 == to) break;
-    if (tile + 1 - chunk == kChunk) {
-      turn();
-      chunk += kChunk;
-      look(chunk + kChunk);
-    }
-    enter(tile + 1);
-    __syncthreads();
-    if (active) {
-      keys_ahead(buf ^ 1, 0);
-      scores(0);
-      if (!whole) mask(tile + 1, 0);
-    }
-  }
-
-  if constexpr (kTrunk) asm volatile("" :: "v"(touched));
-  if (mine_spoiled) spoiled = 1;
-  __syncthreads();
-  if (spoiled)                                       // the NaN that were taken out, counted for the rows that see them
-    for (int tile = from; tile < to; ++tile) {
-      chunk = tile;
-      look(tile);
-      place(tile);
-      at = at_next;
-      if (tile >= all_first && tile < all_last) continue;
-      request(tile);
-#pragma unroll
-      for (int j = 0; j < H; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned one = code_nans(vc[j][i]) & 0x38383838u;      // the code of 1
-          reinterpret_cast<uint2 *>(values[0])[value_at(j, i)] = make_uint2(Operand<false>::pair(one, false), Operand<false>::pair(one, true));
-        }
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int t0 = span.block(tile * 4 + b) * kBlock;
-        half8 seen;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) seen[i] = at_of(tile, b) >= 0 && sees(c, p, t0 + (i & 3) + 4 * h + 8 * (i >> 2)) ? 1 : 0;
-#pragma unroll
-        for (int o = 0; o < OB; ++o) {
-          const f16v count = Operand<false>::mma32(values[0][(b * OB + o) * 64 + lane], __builtin_bit_cast(u4, seen), f16v{0});
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[o][i] = count[i] > 0 ? __builtin_nanf("") : acc[o][i];
-        }
-      }
-      __syncthreads();
-    }
-
-  sum += __shfl_xor(sum, 32, kWave);
-  if constexpr (kTrunk) {
-    if (col > last_col) return;
-    const long in_head = trunk.node.base + (long)trunk.piece * trunk.node.cols + col, at = head * a.columns + in_head;
-    if (trunk.node.base < 0 || in_head >= a.columns) return;
-    const float unit_of_e = top.unit();
-    if (from < to)
-#pragma unroll
-      for (int o = 0; o < OB; ++o)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f4 *>(a.trunk + at * D + o * 32 + i * 8 + h * 4) =
-              f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]} * unit_of_e;
-    if (h == 0) {
-      float *tops = a.trunk + c.heads * a.columns * D;
-      tops[at] = from < to ? top.s : -__builtin_inff();
-      if (trunk.only && in_head + trunk.node.cols < a.columns) tops[at + trunk.node.cols] = -__builtin_inff();
-      tops[c.heads * a.columns + at] = sum * unit_of_e;
-    }
-    return;
-  }
-  if (splits > 1) {
-    float *share = a.parts + few_floats(G, D) + (long)id * wide_floats(D);
-    const int mine = wave * 32 + n;
-    const float unit_of_e = top.unit();
-    if (from < to)
-#pragma unroll
-      for (int o = 0; o < OB; ++o)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f4 *>(share + mine * D + o * 32 + i * 8 + h * 4) =
-              f4{acc[o][4 * i], acc[o][4 * i + 1], acc[o][4 * i + 2], acc[o][4 * i + 3]} * unit_of_e;
-    if (h == 0) { share[kWide * D + mine] = from < to ? top.s : -__builtin_inff(); share[kWide * (D + 1) + mine] = sum * unit_of_e; }
-    return;
-  }
-  if (col > last_col) return;
-  const float r = 1.f / sum;
-  const long to_row = (long)row * c.heads * G + q_head;
-#pragma unroll
-  for (int o = 0; o < OB; ++o)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      auto stored = [&](int j) { return (unsigned)Operand<BF16>::store(share_of(acc[o][4 * i + j], sum, r)); };
-      const uint2 y = make_uint2(stored(0) | stored(1) << 16, stored(2) | stored(3) << 16);
-      reinterpret_cast<uint2 *>(a.out)[to_row * (D / 4) + o * 8 + i * 2 + h] = y;
-    }
-  if (a.lse && h == 0) a.lse[to_row] = sum == 0.f ? -__builtin_inff() : (top.s + (top.e + __builtin_log2f(sum))) * 0.6931471805599453f;
-}
-
 template <bool BF16, int D, typename Args>
 __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned items, int splits)
 {
-  __shared__ WideShared<D> shared;
+  __shared__ __align__(16) Tiles<D> tiles_of;
+  __shared__ int spoiled;
   if constexpr (kShares<Args>)
     if (!plan_holds(a)) return;
   const unsigned total = items * c.heads * splits;
   if (blockIdx.x >= total) {
-    static_assert(sizeof(FewShared<D>) <= sizeof shared.tiles, "the slots of few rows work in the same LDS");
-    if constexpr (!kShares<Args>) few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(shared.tiles));
+    static_assert(sizeof(FewShared<D>) <= sizeof tiles_of, "the slots of few rows work in the same LDS");
+    if constexpr (!kShares<Args>) few_rows<BF16, D>(c, a, blockIdx.x - total, gridDim.x - total, reinterpret_cast<FewShared<D> &>(tiles_of));
     return;
   }
   // Where the workgroups divide by the dies, each die works through neighbouring items, head by head, and what a (slot, head) has cached stays in
@@ -1279,12 +859,25 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
   // and short ones on another, no slower: 8191 rows, 4 heads of 8 557 and 557, 4095 rows, 2 heads of 16 150 and 150.
   unsigned id = blockIdx.x;
   if (total % 8 == 0) id = id % 8 * (total / 8) + id / 8;
-  wide_item<BF16, D, false>(c, a, id, items, splits, Piece(), shared);
+  constexpr bool kTrunk = false;
+  constexpr Piece trunk = {};
+#include "lessdec_pages_wide.h"
+}
+
+// A piece of the nodes' tiles.
+template <bool BF16, int D>
+__device__ __forceinline__ void wide_piece(const Pages &c, const SharedArgs &a, const Piece &trunk, Tiles<D> &tiles_of, int &spoiled)
+{
+  using Args = SharedArgs;
+  constexpr bool kTrunk = true;
+  constexpr unsigned id = 0, items = 1;
+  constexpr int splits = 1;
+#include "lessdec_pages_wide.h"
 }
 
 // Worker w's pieces of the nodes' tiles.
 template <bool BF16, int D>
-__device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, WideShared<D> &shared)
+__device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, Tiles<D> &tiles_of, int &spoiled)
 {
   // (the first piece is loaded before what says whether there is one)
   const int *mine = a.plan.first + w * kFirstInts;
@@ -1301,7 +894,7 @@ __device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a
   for (unsigned at = whole ? w : all.first(w); at < end;) {
     // (no plan of this library's fails here)
     if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.to <= x.from || x.piece < 0) return;
-    wide_item<BF16, D, true>(c, a, 0, 0, 1, x, shared);
+    wide_piece<BF16, D>(c, a, x, tiles_of, spoiled);
     at += x.to - x.from;
     if (at >= end || whole) return;
     __syncthreads();
@@ -1326,18 +919,19 @@ __device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a
 template <bool BF16, int D>
 __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a)
 {
-  __shared__ WideShared<D> shared;
+  __shared__ __align__(16) Tiles<D> tiles_of;
+  __shared__ int spoiled;
   if (!plan_holds(a)) return;
   const int few = same(a.plan.head[kPlanFewWorkers]) & -8, workers = same(a.plan.head[kPlanWorkers]);
   if ((int)blockIdx.x < few) {
-    auto &parts = reinterpret_cast<FewShared<D> &>(shared.tiles);
+    auto &parts = reinterpret_cast<FewShared<D> &>(tiles_of);
     few_rows<BF16, D, true>(c, a, blockIdx.x, few, parts);
     if (same(a.plan.head[kPlanFew]) > 0) few_rows<BF16, D>(c, a, blockIdx.x, few, parts);
   } else {
     unsigned w = blockIdx.x - few;
     if ((int)w >= workers) return;
     if (workers % 8 == 0) w = w % 8 * (workers / 8) + w / 8;           // (neighbours on one die)
-    trunk_pieces<BF16, D>(c, a, w, shared);
+    trunk_pieces<BF16, D>(c, a, w, tiles_of, spoiled);
   }
 }
 
