@@ -327,3 +327,70 @@ def test_rows_of_another_stream_and_wrong_tensors():
                  lambda: p.own.share(start, 4, p.sharing[1:])):
         with pytest.raises(LessdecError):
             call()
+
+
+@pytest.mark.parametrize("slots", [1900, 4096])
+def test_as_many_slots_as_there_can_be(slots):
+    p = Shared(slots, slots * 2 + 8, 16, 6, 1, 64, "bf16")
+    prompt(p, 60, range(slots))
+    p.room([1 + s % 3 for s in range(slots)])
+    rows = [0, 0] + [1] * (slots - 2)
+    assert len(p.share(rows)) == 1
+    p.attend_shared(rows)
+    rows = [s % 5 != 3 for s in range(slots)]
+    p.select([s - s % 2 for s in range(slots)])
+    p.share(rows)
+    p.attend_shared(rows)
+
+
+def test_many_columns_beside_few():
+    """Slots of more columns than a tile has, that share nothing, before, between and behind those that do; head sizes and types."""
+    for dim, dtype, group, window in ((64, "bf16", 2, 0), (128, "bf16", 5, 0), (64, "f16", 40, 100), (128, "f16", 1, 90)):
+        p = Shared(7, 220, 16, 40, 2, dim, dtype, q_per_kv=group, window=window, sinks=3 if window else 0)
+        prompt(p, 170, range(7))
+        p.room([300, 1, 9, 300, 2, 30, 290])
+        for rows in ([200, 1, 2, 130, 1, 3, 257], [0, 1, 9, 300, 2, 30, 0], [300, 1, 1, 0, 1, 1, 290]):
+            p.share(rows)
+            p.attend_shared(rows)
+
+
+def test_offsets_past_31_bits():
+    """A pool of 2.5 GiB a tensor: what is shared and what is not at its end, in the last layer."""
+    import torch
+    from paper_2402_09398_amd import PagedCache
+    pages, heads, dim = 40960, 8, 128
+    own = PagedCache(3, pages, 16, 16, heads, dim, "f16", layers=4, max_rows=64, shared=True)
+    ref = po.Cache(3, 32, 16, 16, heads, dim)
+    g = torch.Generator().manual_seed(5)
+    far = [pages - 1, pages - 7, 33000, 5, pages - 2, pages - 100, 39999, pages - 50]
+    at = iter(list(range(pages - 300, pages - 285)))
+    tail = {s: [next(at) for _ in range(2)] for s in range(3)}
+    names = {x: i for i, x in enumerate(far + sum(tail.values(), []))}
+    ref.table[:] = -1
+    for s in range(3):
+        row = far + tail[s]
+        own.table[s, :10] = torch.tensor(row, dtype=torch.int32)
+        ref.table[s, :10] = [names[x] for x in row]
+        ref.length[s] = 128 + 13 + s
+    k, v, q = (torch.randn(192, heads, dim, generator=g).half() for _ in range(3))
+    for counts, base in (([128, 0, 0], 0), ([13, 14, 15], 128)):
+        lengths = [128, 128, 128] if base == 0 else [141, 142, 143]
+        own.length[:] = torch.tensor(lengths, dtype=torch.int32)
+        ref.length[:] = lengths
+        start = np.concatenate([[0], np.cumsum(counts)])
+        dev = torch.tensor(start, dtype=torch.int32).cuda()
+        rows = slice(base, base + int(start[-1]))
+        for layer in (0, 3):
+            own.append(layer, k[rows].cuda(), v[rows].cuda(), dev)
+        ref.append(0, k[rows].double().numpy(), v[rows].double().numpy(), start)
+    plan = own.share_plan()
+    for counts in ([1, 1, 1], [13, 14, 15]):
+        start = np.concatenate([[0], np.cumsum(counts)])
+        n, dev = int(start[-1]), torch.tensor(start, dtype=torch.int32).cuda()
+        want, _, tol, _ = ref.attend(0, q[:n].double().numpy(), start, 2.0 ** -11)
+        own.share(dev, n, plan, least_bytes=0)
+        assert int(plan[0]) > 3 or counts == [1, 1, 1]
+        for layer in (0, 3):
+            out = torch.empty_like(q[:n]).cuda()
+            own.attend_shared(layer, q[:n].cuda(), out, dev, max(counts), plan)
+            assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
