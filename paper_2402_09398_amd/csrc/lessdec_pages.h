@@ -129,8 +129,8 @@ constexpr int kPagesWorkers = 768;                   // workgroups of the kernel
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 
 // What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
-//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, workers of the nodes, of the entries of few, short entries, whether workers
-//        have whole chunks
+//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, workers of the nodes, of the entries of few, short entries, slots and (the
+//        last bit) whether workers have whole chunks
 //  node  [3 slots][kNodeInts]: slot whose table row is read, first row, rows, least and largest position of them, blocks [first, last), node before it
 //        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
 //        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
@@ -143,7 +143,7 @@ hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, h
 //  pos   [rows]: positions of the rows
 //  apart [slots]: scratch
 // A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
-constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanFewWorkers = 5, kPlanShort = 6, kPlanWhole = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
+constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanFewWorkers = 5, kPlanShort = 6, kPlanShape = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
 constexpr int kShortBlocks = 32;                     // up to which a wave works by itself
 constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile

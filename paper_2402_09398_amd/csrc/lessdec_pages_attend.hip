@@ -233,7 +233,11 @@ __device__ inline Node node_of(const Pages &c, const SharedArgs &a, const int *r
   n.cols = n.rows * c.q_per_kv;
   return n;
 }
-__device__ inline bool plan_holds(const SharedArgs &a) { return same(a.plan.head[kPlanRows]) == a.rows; }
+// whether it was made for so many rows and slots
+__device__ inline bool plan_holds(const Pages &c, const SharedArgs &a)
+{
+  return same(a.plan.head[kPlanRows]) == a.rows && same(a.plan.head[kPlanShape]) >> 1 == c.slots;
+}
 
 // ---- few rows a slot: up to 16 query columns -----------------------------------------------------------------------------
 //
@@ -847,7 +851,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(Pages c, Args a, unsigned 
   __shared__ __align__(16) Tiles<D> tiles_of;
   __shared__ int spoiled;
   if constexpr (kShares<Args>)
-    if (!plan_holds(a)) return;
+    if (!plan_holds(c, a)) return;
   const unsigned total = items * c.heads * splits;
   if (blockIdx.x >= total) {
     static_assert(sizeof(FewShared<D>) <= sizeof tiles_of, "the slots of few rows work in the same LDS");
@@ -888,12 +892,13 @@ __device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a
   if (tiles == 0 || nodes == 0) return;
   Trunk all{(unsigned)tiles * c.heads, max(same(a.plan.head[kPlanWorkers]), 1), 1};
   all.chunk = max((int)(all.total / all.workers), 1);
-  const bool whole = same(a.plan.head[kPlanWhole]) != 0;
+  const bool whole = same(a.plan.head[kPlanShape]) & 1;
   const unsigned end = whole ? w + 1 : all.first(w + 1);
   x.head = same(f.x); x.column = same(f.y); x.from = same(f.z); x.to = same(f.w); x.piece = same(g.x); x.only = same(g.y);
   for (unsigned at = whole ? w : all.first(w); at < end;) {
     // (no plan of this library's fails here)
-    if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.to <= x.from || x.piece < 0) return;
+    if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.to <= x.from || x.piece < 0 ||
+        x.to > c.table_len * page_blocks(c) / 4 + 1) return;
     wide_piece<BF16, D>(c, a, x, tiles_of, spoiled);
     at += x.to - x.from;
     if (at >= end || whole) return;
@@ -921,7 +926,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a)
 {
   __shared__ __align__(16) Tiles<D> tiles_of;
   __shared__ int spoiled;
-  if (!plan_holds(a)) return;
+  if (!plan_holds(c, a)) return;
   const int few = same(a.plan.head[kPlanFewWorkers]) & -8, workers = same(a.plan.head[kPlanWorkers]);
   if ((int)blockIdx.x < few) {
     auto &parts = reinterpret_cast<FewShared<D> &>(tiles_of);
@@ -945,13 +950,16 @@ __global__ __launch_bounds__(256) void shared_join_kernel(Pages c, SharedArgs a)
   const Rows rows = slot_rows(a.start, slot, a.rows);
   int4 chain[kNodes];
 #pragma unroll
-  for (int d = 0; d < kNodes; ++d) chain[d] = reinterpret_cast<const int4 *>(a.plan.chain)[(long)kNodes * slot + d];
+  for (int d = 0; d < kNodes; ++d) {
+    chain[d] = reinterpret_cast<const int4 *>(a.plan.chain)[(long)kNodes * slot + d];
+    chain[d].y = max(chain[d].y, 0);
+  }
   const int in_slot = id / heads, q_head = id - in_slot * heads, head = q_head / G, g = q_head - head * G;
-  if (in_slot >= rows.count || !plan_holds(a) || chain[0].x < 0) return;
+  if (in_slot >= rows.count || !plan_holds(c, a) || chain[0].x < 0) return;
   int upto[kNodes];                                  // shares of the nodes so far
 #pragma unroll
   for (int d = 0; d < kNodes; ++d) {
-    const long last = (long)max(chain[d].x, 0) + (long)max(chain[d].y, 0) * max(chain[d].z - 1, 0) + in_slot * G + g;
+    const long last = (long)max(chain[d].x, 0) + (long)chain[d].y * max(chain[d].z - 1, 0) + in_slot * G + g;
     upto[d] = (d ? upto[d - 1] : 0) + (last < a.columns ? max(chain[d].z, 0) : 0);
   }
   const float *tops = a.trunk + c.heads * a.columns * D + (long)head * a.columns, *totals = tops + c.heads * a.columns;
@@ -1024,7 +1032,7 @@ __global__ __launch_bounds__(256) void wide_join_kernel(Pages c, Args a, unsigne
   Columns t;
   Rows rows;
   if constexpr (kShares<Args>)
-    if (!plan_holds(a)) return;
+    if (!plan_holds(c, a)) return;
   if (!columns_of(c, a, item % items, false, t, rows)) return;
   const float *base = a.parts + few_floats(G, D) + (long)item * splits * wide_floats(D);
   for (int i = threadIdx.x; i < kJoinColumns * (D / 2); i += 256) {

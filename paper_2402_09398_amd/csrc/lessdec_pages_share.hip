@@ -9,8 +9,8 @@
 // has let go what it no longer sees itself, so that one slot may name a page and the next one none; the slot whose rows lie furthest back sees all that
 // any of them sees, and its row is the one that is read for the node.
 //
-// Made once a step for all layers, from a few bytes a page and slot: bound by the latency of its dependent steps.  No atomics; the
-// same tables give the same plan.
+// Made once a step for all layers, from a few bytes a page and slot: bound by the latency of its dependent steps.  The same tables give
+// the same plan.
 #include "lessdec_pages.h"
 
 namespace lessdec {
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     plan.head[kPlanRows] = rows;
     plan.head[kPlanWorkers] = trunk.workers;
     plan.head[kPlanFewWorkers] = few_workers;
-    plan.head[kPlanWhole] = whole;
+    plan.head[kPlanShape] = 2 * N | whole;
   }
 }
 

@@ -394,3 +394,33 @@ def test_offsets_past_31_bits():
             out = torch.empty_like(q[:n]).cuda()
             own.attend_shared(layer, q[:n].cuda(), out, dev, max(counts), plan)
             assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+
+
+def test_rows_before_a_slots_first_token():
+    """More rows than a slot has tokens, and slots that have none: what sees nothing is written as attend() writes it."""
+    for group, rows in ((1, [3, 1, 9, 2, 4, 1]), (4, [6, 1, 30, 3, 9, 4]), (9, [2, 1, 14, 4, 2, 3]), (40, [5, 4, 1, 2, 2, 3])):
+        p = Shared(6, 60, 16, 8, 2, 64, "f16", q_per_kv=group)
+        p.room([2, 0, 2, 40, 40, 0])
+        p.select([0, -1, 0, 3, 3, -1])
+        p.room([0, 0, 1, 0, 1, 0])
+        p.share(rows)
+        out = p.attend_shared(rows)
+        start = np.concatenate([[0], np.cumsum(rows)])
+        for s in range(6):
+            unseen = max(rows[s] - int(p.ref.length[s]), 0)
+            assert (out[start[s]:start[s] + unseen] == 0).all() and (unseen > 0) == (s < 3 and rows[s] > p.ref.length[s] or s in (1, 5))
+
+
+def test_plans_of_other_caches():
+    """A plan that was made for as many rows of a cache with other slots writes nothing."""
+    p, other = (Shared(n, 80, 16, 20, 2, 64, "f16", q_per_kv=4) for n in (6, 3))
+    for x, rows in ((p, [1] * 6), (other, [2] * 3)):
+        prompt(x, 200, range(len(rows)))
+        x.room(rows)
+        x.share(rows, behind=0)
+    q = p.t.zeros(6, 8, 64, dtype=p.t.float16, device="cuda")
+    out = p.t.full_like(q, 3.5)
+    plan = p.own.share_plan()
+    plan[:other.sharing.numel()] = other.sharing[:plan.numel()]
+    p.own.attend_shared(0, q, out, p.ints(np.arange(7)), 1, plan)
+    assert (out == 3.5).all()
