@@ -129,21 +129,22 @@ constexpr int kPagesWorkers = 768;                   // workgroups of the kernel
 hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, hipStream_t st);
 
 // What neighbouring slots have in common, for a call's rows (lessdec_pages_share.hip), in the caller's memory.
-//  head  [8]: nodes, tiles of a head, entries of few, rows that it was made for, workers of the nodes, of the entries of few, short entries, slots and (the
-//        last bit) whether workers have whole chunks
+//  head  [8]: nodes, units of a head, entries of few, rows that it was made for, workers of the nodes and (kPlanFewShift) of the entries of few, tiles of a
+//        chunk, short entries, slots and (the last bit) whether workers have whole chunks
 //  node  [3 slots][kNodeInts]: slot whose table row is read, first row, rows, least and largest position of them, blocks [first, last), node before it
-//        (-1: none), its first tile among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
+//        (-1: none), its first unit (or chunk, where workers have whole ones) among a head's, tiles (of 64 tokens; 0: few columns, or nothing of its own), first column (-1: none), shares of a column.
 //        First the nodes of several slots, then a slot's own part, which reaches to kEndless.
 //  few   [3 slots][kNodeInts]: of nodes of up to kFewColumns columns, and of slots of so many that share nothing: steps, slot whose table row is
 //        read, first row, rows, least and largest position, blocks [first, last), first column of the plan (-1: the rows are stored), rows of several slots.
 //        From the front, in steps of kFewBlocks blocks, for a workgroup each; from the back, in steps of two, the short ones, for a wave each
 //  chain [slots][kTrunkDepth + 1][4]: of its own node and those around it, the first column of the plan that is its first row's, columns from a share to
 //        the next, shares (0: no more nodes; with -1 in the first the slot is not in any, and an entry of few or of 128 columns and more)
-//  first [kSharedWorkers][kFirstInts]: a worker's first piece: its node as above, then head, first column, tiles [from, to), piece, whether it is a whole chunk
+//  first [kSharedWorkers][kFirstInts]: a worker's first piece: its node as above, then head, first column, tiles [from, to), piece, whether it is a whole chunk, units
 //  pos   [rows]: positions of the rows
 //  apart [slots]: scratch
 // A (head, column of the plan) has a sum of D floats, a maximum and a total in the workspace.
-constexpr int kPlanNodes = 0, kPlanTiles = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanFewWorkers = 5, kPlanShort = 6, kPlanShape = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
+constexpr int kPlanNodes = 0, kPlanUnits = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanChunk = 5, kPlanShort = 6, kPlanShape = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
+constexpr int kPlanFewShift = 16;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
 constexpr int kShortBlocks = 32;                     // up to which a wave works by itself
 constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
@@ -153,32 +154,55 @@ struct Plan {
 };
 // The nodes' tiles as the workers get them, in one of two ways.  Whole chunks: the tiles of a node's 128 columns by one head are cut into chunks of
 // the same length, the least with which there are no more chunks than workers, and each worker has one.  Or, where that would leave workers idle for
-// longer than a second beginning and end take: the tiles of all heads and nodes, one behind the other, are dealt out evenly, worker w has
-// [first(w), first(w + 1)).  Within a node and head
-// they are ordered by chunks of tokens, in a chunk by tiles of 128 columns, so that neighbouring workers read the same tokens at the same time.  A
-// chunk is no longer than any worker's part: what it has of 128 columns is cut into two pieces at most.
+// longer than a second beginning and end take: the chunks of all heads and nodes, one behind the other, are dealt out evenly, in units of a tile's
+// time.  A chunk begins with kBegin units that stand for what a piece costs beside its tiles, so that a worker of many short parts has no more to do
+// than one of a long one; worker w has [first(w), first(w + 1)).  32 questions of 24 tokens behind 16384, 32 heads: 393 us dealt
+// by tiles alone, 277 so, 285 and 290 with 5 and 8 units; behind 8192: 277, 160, 167 and 177.
+// Within a node and head the order is by chunks of tokens, in a chunk by tiles of 128 columns, so that neighbouring workers read the same tokens at the
+// same time.  A chunk has no more tiles than any worker has units: what it has of 128 columns is cut into two pieces at most.
+constexpr int kBegin = 3;
 struct Trunk {
-  unsigned total;                                    // less than 2^31
-  int workers, chunk;
+  unsigned total;                                    // units of all heads, less than 2^31
+  int workers, chunk;                                // tiles of a chunk
   __host__ __device__ inline unsigned first(unsigned w) const
   {
     const unsigned each = total / workers, more = total - each * workers;
     return w * each + (w < more ? w : more);
   }
   __host__ __device__ inline int chunks(int n) const { return (n + chunk - 1) / chunk; }        // of n tiles of 128 columns
+  __host__ __device__ inline int units(int n, int columns) const // of a node by a head
+  {
+    return n ? (columns + kTrunkTile - 1) / kTrunkTile * (n + kBegin * chunks(n)) : 0;
+  }
+  // The piece of a node of n tiles at unit `at` of the node's, up to `left` units of it: 128 columns from `column` on, tiles [from, to), which may be none.
+  struct Dealt { int column, from, to, piece, only, units; };
+  __device__ inline Dealt dealt(int n, int columns, int at, int left) const
+  {
+    const int tall = (columns + kTrunkTile - 1) / kTrunkTile, k = at / max((chunk + kBegin) * tall, 1), in_chunk = at - k * (chunk + kBegin) * tall;
+    const int len = max(min(chunk, n - k * chunk), 0), column = in_chunk / (len + kBegin), done = in_chunk - column * (len + kBegin);
+    Dealt x;
+    x.units = min(len + kBegin - done, left);
+    x.column = column * kTrunkTile;
+    const int from = max(done - kBegin, 0), to = max(done + x.units - kBegin, 0);
+    x.from = k * chunk + from;
+    x.to = k * chunk + to;
+    x.piece = 2 * k + (from > 0);
+    x.only = from == 0 && to == len;
+    return x;
+  }
 };
 // Slots of up to 127 query columns share.  A row is in kTrunkDepth nodes and one of its own at most, each of which has room for two pieces, and
-// for as many more as chunks are (n tiles have n / chunk + 1 at most, and a chunk is at least half of a worker's part).
+// for as many more as chunks are (n tiles have n / chunk + 1 at most, and a chunk has at least half as many as a worker has units).
 inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
 {
   const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;
   return 2 * (kTrunkDepth + 1) * (n < most ? n : most) + 4L * kTrunkTile * (kSharedWorkers / heads + 1);
 }
-// tiles of all heads and nodes, at most
-inline double plan_tiles(int slots, int heads, int q_per_kv, long rows, long tokens)
+// units of all heads and nodes, at most
+inline double plan_units(int slots, int heads, int q_per_kv, long rows, long tokens)
 {
   const double n = (double)rows * q_per_kv, most = (double)slots * kTrunkTile;
-  return heads * ((kTrunkDepth + 1) * (n < most ? n : most) / kTrunkTile + 2.0 * slots) * (tokens / 64 + 1);
+  return heads * ((kTrunkDepth + 1) * (n < most ? n : most) / kTrunkTile + 2.0 * slots) * (tokens / 64 + 1 + kBegin) + 2.0 * kBegin * kSharedWorkers;
 }
 inline long plan_ints(int slots, long rows) { return kPlanHead + kSharedWorkers * kFirstInts + (long)slots * (6 * kNodeInts + 4 * (kTrunkDepth + 1) + 1) + rows; }
 inline Plan plan_at(int *p, int slots)

@@ -94,9 +94,9 @@ bool rows_ok(const Pages &c, int rows)
   return rows >= 0 && (long)rows * c.q_per_kv < 1L << 31 && ((long)rows * c.q_per_kv / 128 + c.slots) * c.heads <= 1L << 30;
 }
 
-bool tiles_ok(const Pages &c, int rows)
+bool units_ok(const Pages &c, int rows)
 {
-  return plan_tiles(c.slots, c.heads, c.q_per_kv, rows, (long)c.table_len * c.page_tokens) < 0x1p31;
+  return plan_units(c.slots, c.heads, c.q_per_kv, rows, (long)c.table_len * c.page_tokens) < 0x1p31;
 }
 
 }  // namespace
@@ -181,7 +181,7 @@ int lessdec_pages_share(const lessdec_pages_desc *desc, const int32_t *start, in
   Pages c;
   const int rc = check(desc, 0, 0, 0, &c);
   if (rc) return rc;
-  if (!rows_ok(c, rows) || !tiles_ok(c, rows)) return LESSDEC_EINVAL;
+  if (!rows_ok(c, rows) || !units_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0) return LESSDEC_OK;
   if (!start || !plan || !aligned(start, 4) || !aligned(plan, 16) || plan == start || plan == desc->table || plan == desc->length) return LESSDEC_EINVAL;
   return result(launch_pages_share(c, start, rows, plan_at(plan, c.slots), plan_columns(c.slots, c.heads, c.q_per_kv, rows), least_bytes,
@@ -195,7 +195,7 @@ int lessdec_pages_attend_shared(const lessdec_pages_desc *desc, int32_t layer, c
   const int rc = check(desc, kPool, 0, layer, &c);
   if (rc) return rc;
   const long step = row_stride(stride, (long)desc->heads * c.q_per_kv * desc->head_dim);
-  if (step < 0 || max_new < 0 || !rows_ok(c, rows) || !tiles_ok(c, rows)) return LESSDEC_EINVAL;
+  if (step < 0 || max_new < 0 || !rows_ok(c, rows) || !units_ok(c, rows)) return LESSDEC_EINVAL;
   if (rows == 0 || max_new == 0) return LESSDEC_OK;
   if (!desc->workspace || !aligned(desc->workspace, 256) || desc->workspace_bytes < shared_workspace_for(desc, rows)) return LESSDEC_EWORKSPACE;
   if (!q || !out || !start || !plan || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(start, 4) || !aligned(plan, 16)) return LESSDEC_EINVAL;

@@ -211,7 +211,7 @@ template <typename Args> __device__ inline int thread_of()
 }
 
 struct Node {
-  int slot, row, rows, lo, hi, first, last, before, tile, tiles, base, shares;
+  int slot, row, rows, lo, hi, first, last, before, unit, tiles, base, shares;
   int cols;
 };
 // (f: the same in all lanes)
@@ -229,7 +229,7 @@ __device__ inline Node node_of(const Pages &c, const SharedArgs &a, const int *r
   n.first = max(same(y.y), 0);
   n.last = min(max(same(y.z), 0), c.table_len * page_blocks(c));
   n.before = same(y.w);
-  n.tile = same(z.x); n.tiles = max(same(z.y), 0); n.base = same(z.z); n.shares = max(same(z.w), 0);
+  n.unit = same(z.x); n.tiles = max(same(z.y), 0); n.base = same(z.z); n.shares = max(same(z.w), 0);
   n.cols = n.rows * c.q_per_kv;
   return n;
 }
@@ -881,42 +881,36 @@ __device__ __forceinline__ void wide_piece(const Pages &c, const SharedArgs &a, 
 
 // Worker w's pieces of the nodes' tiles.
 template <bool BF16, int D>
-__device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, Tiles<D> &tiles_of, int &spoiled)
+__device__ __forceinline__ void trunk_pieces(const Pages &c, const SharedArgs &a, unsigned w, int workers, Tiles<D> &tiles_of, int &spoiled)
 {
   // (the first piece is loaded before what says whether there is one)
   const int *mine = a.plan.first + w * kFirstInts;
   Piece x;
   x.node = node_of(c, a, mine);
   const int4 f = reinterpret_cast<const int4 *>(mine)[3], g = reinterpret_cast<const int4 *>(mine)[4];
-  const int tiles = max(same(a.plan.head[kPlanTiles]), 0), nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
-  if (tiles == 0 || nodes == 0) return;
-  Trunk all{(unsigned)tiles * c.heads, max(same(a.plan.head[kPlanWorkers]), 1), 1};
-  all.chunk = max((int)(all.total / all.workers), 1);
+  const int units = max(same(a.plan.head[kPlanUnits]), 0), nodes = min(max(same(a.plan.head[kPlanNodes]), 0), 3 * c.slots);
+  if (units == 0 || nodes == 0) return;
+  const Trunk all{(unsigned)units * c.heads, max(workers, 1), max(same(a.plan.head[kPlanChunk]), 1)};
   const bool whole = same(a.plan.head[kPlanShape]) & 1;
   const unsigned end = whole ? w + 1 : all.first(w + 1);
   x.head = same(f.x); x.column = same(f.y); x.from = same(f.z); x.to = same(f.w); x.piece = same(g.x); x.only = same(g.y);
+  int now = same(g.z);
   for (unsigned at = whole ? w : all.first(w); at < end;) {
     // (no plan of this library's fails here)
-    if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.to <= x.from || x.piece < 0 ||
+    if ((unsigned)x.head >= (unsigned)c.heads || (unsigned)x.column >= (unsigned)x.node.cols || x.from < 0 || x.piece < 0 || now <= 0 ||
         x.to > c.table_len * page_blocks(c) / 4 + 1) return;
-    wide_piece<BF16, D>(c, a, x, tiles_of, spoiled);
-    at += x.to - x.from;
+    if (x.from < x.to) wide_piece<BF16, D>(c, a, x, tiles_of, spoiled);
+    at += now;
     if (at >= end || whole) return;
     __syncthreads();
-    x.head = same((int)(at / (unsigned)tiles));
-    const int in_head = (int)(at - (unsigned)x.head * tiles);
+    x.head = same((int)(at / (unsigned)units));
+    const int in_head = (int)(at - (unsigned)x.head * units);
     const int i = last_at(nodes, in_head, [&](int k) { return (long)a.plan.node[(long)k * kNodeInts + 8]; });
     x.node = node_of(c, a, a.plan.node + (long)same(i) * kNodeInts);
-    const int in_node = in_head - x.node.tile, wide_chunk = all.chunk * ((x.node.cols + kWide - 1) / kWide);
-    if (in_node < 0 || wide_chunk == 0) return;
-    const int k = same(in_node / wide_chunk), in_chunk = in_node - k * wide_chunk, len = min(all.chunk, x.node.tiles - k * all.chunk);
-    if (len <= 0) return;
-    const int column = same(in_chunk / len), done = in_chunk - column * len;
-    x.column = column * kWide;
-    x.from = k * all.chunk + done;
-    x.to = x.from + min(len - done, (int)(end - at));
-    x.piece = 2 * k + (done > 0);
-    x.only = done == 0 && x.to == x.from + len;
+    if (in_head < x.node.unit) return;
+    const Trunk::Dealt y = all.dealt(x.node.tiles, x.node.cols, in_head - x.node.unit, (int)(end - at));
+    x.column = same(y.column); x.from = same(y.from); x.to = same(y.to); x.piece = same(y.piece); x.only = same(y.only);
+    now = same(y.units);
   }
 }
 
@@ -927,7 +921,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a)
   __shared__ __align__(16) Tiles<D> tiles_of;
   __shared__ int spoiled;
   if (!plan_holds(c, a)) return;
-  const int few = same(a.plan.head[kPlanFewWorkers]) & -8, workers = same(a.plan.head[kPlanWorkers]);
+  const int both = same(a.plan.head[kPlanWorkers]), few = both >> kPlanFewShift, workers = both & ((1 << kPlanFewShift) - 1);
   if ((int)blockIdx.x < few) {
     auto &parts = reinterpret_cast<FewShared<D> &>(tiles_of);
     few_rows<BF16, D, true>(c, a, blockIdx.x, few, parts);
@@ -936,7 +930,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(Pages c, SharedArgs a)
     unsigned w = blockIdx.x - few;
     if ((int)w >= workers) return;
     if (workers % 8 == 0) w = w % 8 * (workers / 8) + w / 8;           // (neighbours on one die)
-    trunk_pieces<BF16, D>(c, a, w, tiles_of, spoiled);
+    trunk_pieces<BF16, D>(c, a, w, workers, tiles_of, spoiled);
   }
 }
 

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   // tiles of the nodes of more than kFewColumns columns, steps of the others
-  long tiles = 0;
+  long tiles = 0, columns_of_tiles = 0;              // of a head: tiles, and columns of 128 that have some
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
     int *f = plan.node + (long)min(i, all_nodes - 1) * kNodeInts;
@@ -325,13 +325,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       else narrow = blocks;
     }
     long sum;
-    const long before = tiles + scan((long)mine * wide, sum);
+    scan((long)mine * wide << 20 | (mine ? wide : 0), sum);
     if (i < all_nodes) {
-      f[8] = (int)before;
       f[9] = mine;
       f[11] = narrow;
     }
-    tiles += sum;
+    tiles += sum >> 20;
+    columns_of_tiles += sum & 1048575;
     // (columns of the plan follow)
     list(narrow > 0, narrow, f[0], f[1], f[2], f[3], f[4], f[5], f[6], i, i < nodes);
   }
@@ -340,20 +340,21 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   // columns: as many times a node's as workgroups may have a piece of it
   // How many workgroups for the entries of few, which also has those of the nodes: the longer of the two kinds of work is to be short.  In units of
   // 1/8 us, measured: a short entry by a head 15 us for each of the waves that has one, a step of a long one 0.6, a piece 11 and 2.2 a tile.
-  Trunk trunk{(unsigned)(tiles * c.heads), 8, 1};
+  const unsigned all_tiles = (unsigned)(tiles * c.heads), begun = (unsigned)(tiles + columns_of_tiles * kBegin) * c.heads;     // (begun: in units, a chunk a column)
+  Trunk trunk{0, 8, 1};
   int few_workers = 0;
   if (few_steps || short_ones) {
     unsigned best = ~0u;
     for (int f = 32; f <= kSharedWorkers; f *= 2) {
       if (f == kSharedWorkers && tiles) break;
       const unsigned waves = 4 * f, a = ((unsigned)short_ones * c.heads + waves - 1) / waves * 120 + (unsigned)min(few_steps * c.heads / f, 1L << 26) * 5;
-      const unsigned b = tiles ? 88 + min(trunk.total / max(kSharedWorkers - f, 8) + 1, 1u << 26) * 18 : 0, time = max(a, b);
+      const unsigned b = tiles ? 88 + min(begun / max(kSharedWorkers - f, 8) + 1, 1u << 26) * 18 : 0, time = max(a, b);
       if (time < best) { best = time; few_workers = f; }
     }
   }
-  trunk.workers = max(min(kSharedWorkers - few_workers, (int)min(trunk.total / 2, 4096u)) & ~7, 8);
-  // Whole chunks: their length.  A piece begins and ends for the time of four tiles or five.
-  int length = max((int)((trunk.total + trunk.workers - 1) / trunk.workers), 2), chunks_of_head = 0;
+  trunk.workers = max(min(kSharedWorkers - few_workers, (int)min(all_tiles / 2, 4096u)) & ~7, 8);
+  // Whole chunks: their length.
+  int length = max((int)((all_tiles + trunk.workers - 1) / trunk.workers), 2), chunks_of_head = 0;
   bool whole = false;
   for (int turn = 0; turn < 5 && tiles; ++turn) {
     int x = 0;
@@ -367,25 +368,26 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (whole) break;
     length = (int)min(max((long)length + 1, length * all / trunk.workers), (long)kEndless);
   }
-  whole = whole && (long)length * trunk.workers - trunk.total <= 4L * trunk.workers;
-  trunk.chunk = whole ? length : max((int)(trunk.total / trunk.workers), 1);
+  // (else a worker's units, less what a piece costs, but no less than half of them, as there is room for so many chunks)
+  const int part = (int)(begun / trunk.workers);
+  whole = whole && length < part + kBegin;
+  trunk.chunk = whole ? length : max(max(part - kBegin, (part + 1) / 2), 1);
   if (whole) trunk.workers = chunks_of_head * c.heads;
   long columns = 0;
-  int chunks = 0;
+  int units = 0;                                     // or chunks, where workers have whole ones
   for (int base = 0; base < all_nodes; base += kThreads) {
     const int i = base + tid;
     int *f = plan.node + (long)min(i, all_nodes - 1) * kNodeInts;
     const int pieces = i >= all_nodes ? 0 : f[9] ? (whole ? 1 : 2) * trunk.chunks(f[9]) : f[11] > 0;
-    if (whole) {                                     // (a node's place among the chunks of a head in place of that among its tiles)
-      int all;
-      const int at = chunks + scan(i < all_nodes && f[9] ? (f[2] * G + kTrunkTile - 1) / kTrunkTile * pieces : 0, all);
-      if (i < all_nodes) f[8] = at;
-      chunks += all;
-    }
+    const int mine = i >= all_nodes ? 0 : whole ? (f[9] ? (f[2] * G + kTrunkTile - 1) / kTrunkTile * pieces : 0) : trunk.units(f[9], f[2] * G);
+    int upto;
+    const int unit = units + scan(mine, upto);
+    units += upto;
     int all;
     const long at = columns + scan(i < all_nodes ? pieces * f[2] * G : 0, all);
     const bool fits = at + (long)pieces * f[2] * G <= most_columns;    // (it does: plan_columns)
     if (i < all_nodes) {
+      f[8] = unit;
       f[10] = fits ? (int)at : -1;
       f[11] = fits ? pieces : 0;
     }
@@ -399,11 +401,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (*f >= 0) *f = plan.node[(long)*f * kNodeInts + 10];
   }
   // the workers' first pieces: the last node that begins no later
+  trunk.total = (unsigned)units * c.heads;
   if (tiles)
     for (int w = tid; w < trunk.workers; w += kThreads) {
-      const unsigned at = whole ? w : trunk.first(w), end = whole ? w + 1 : trunk.first(w + 1), in_all = whole ? (unsigned)chunks_of_head : (unsigned)tiles;
-      const unsigned head = at / in_all;
-      const int in_head = (int)(at - head * in_all);
+      const unsigned at = whole ? w : trunk.first(w), end = whole ? w + 1 : trunk.first(w + 1);
+      const unsigned head = at / (unsigned)units;
+      const int in_head = (int)(at - head * units);
       int low = 0;
       for (int high = all_nodes; high - low > 1;) {
         const int mid = (low + high) / 2;
@@ -413,17 +416,16 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       const int4 *f = reinterpret_cast<const int4 *>(plan.node + (long)low * kNodeInts);
       int4 *to = reinterpret_cast<int4 *>(plan.first + w * kFirstInts);
       const int4 x = f[0], y = f[1], z = f[2];
-      const int n = max(z.y, 1), tall = max((x.z * G + kTrunkTile - 1) / kTrunkTile, 1), in_node = in_head - z.x;
+      const int in_node = in_head - z.x;
       to[0] = x; to[1] = y; to[2] = z;
       if (whole) {
-        const int each = (n + trunk.chunks(n) - 1) / trunk.chunks(n), k = in_node / tall;
+        const int n = max(z.y, 1), tall = max((x.z * G + kTrunkTile - 1) / kTrunkTile, 1), each = (n + trunk.chunks(n) - 1) / trunk.chunks(n), k = in_node / tall;
         to[3] = make_int4((int)head, (in_node - k * tall) * kTrunkTile, k * each, min(n, (k + 1) * each));
-        to[4] = make_int4(k, 0, 0, 0);
+        to[4] = make_int4(k, 0, 1, 0);
       } else {
-        const int k = in_node / (trunk.chunk * tall), in_chunk = in_node - k * trunk.chunk * tall, len = max(min(trunk.chunk, n - k * trunk.chunk), 1);
-        const int column = in_chunk / len, done = in_chunk - column * len, now = min(len - done, (int)(end - at));
-        to[3] = make_int4((int)head, column * kTrunkTile, k * trunk.chunk + done, k * trunk.chunk + done + now);
-        to[4] = make_int4(2 * k + (done > 0), now == len, 0, 0);
+        const Trunk::Dealt p = trunk.dealt(z.y, x.z * G, in_node, (int)(end - at));
+        to[3] = make_int4((int)head, p.column, p.from, p.to);
+        to[4] = make_int4(p.piece, p.only, p.units, 0);
       }
     }
   // what a slot's rows are joined from
@@ -447,12 +449,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   }
   if (tid == 0) {
     plan.head[kPlanNodes] = all_nodes;
-    plan.head[kPlanTiles] = (int)tiles;
+    plan.head[kPlanUnits] = units;
     plan.head[kPlanFew] = few;
     plan.head[kPlanShort] = short_ones;
     plan.head[kPlanRows] = rows;
-    plan.head[kPlanWorkers] = trunk.workers;
-    plan.head[kPlanFewWorkers] = few_workers;
+    plan.head[kPlanWorkers] = trunk.workers | few_workers << kPlanFewShift;
+    plan.head[kPlanChunk] = trunk.chunk;
     plan.head[kPlanShape] = 2 * N | whole;
   }
 }
