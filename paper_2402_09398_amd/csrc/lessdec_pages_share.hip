@@ -35,6 +35,7 @@ __device__ inline bool sees_entry(const Pages &c, int lo, int j)
 
 // A wave for every slot: positions of its rows, and how many leading entries it shares with the slot that has rows before it.  Sixteen
 // entries a lane on their way, up to the first that differs.
+constexpr int kEach = 16;
 __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, int rows, Plan plan)
 {
   const int s = __builtin_amdgcn_readfirstlane((blockIdx.x * 256 + threadIdx.x) / kWave), lane = threadIdx.x & 63;
@@ -58,19 +59,22 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
     const int *mine = c.table + (size_t)s * c.table_len, *theirs = c.table + (size_t)max(first, 0) * c.table_len;
     auto page_of = [&](int x) { return (unsigned)x < (unsigned)c.pages ? x : -1; };
     same = most;
-    for (int base = 0; base < most; base += 16 * kWave) {
-      int x[16], y[16];
+    for (int base = 0; base < most; base += kEach * kWave) {
+      int x[kEach], y[kEach];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < kEach; ++i) {
         const int j = min(base + i * kWave + lane, most - 1);
         x[i] = mine[j];
         y[i] = theirs[j];
       }
-      int differs = most;
+      unsigned apart = 0;
 #pragma unroll
-      for (int i = 15; i >= 0; --i) {
+      for (int i = 0; i < kEach; ++i) apart |= (unsigned)(page_of(x[i]) != page_of(y[i])) << i;
+      if (!__ballot(apart)) continue;
+      int differs = most;
+      for (int i = 0; i < kEach && differs == most; ++i) {
         const int j = base + i * kWave + lane;
-        bool differ = j < most && page_of(x[i]) != page_of(y[i]) && sees_entry(c, me.lo, j);
+        bool differ = (apart >> i & 1) && j < most && sees_entry(c, me.lo, j);
         // where the slot before does not see the page, the last one that does is asked (rare: slots whose windows begin apart)
         bool asking = differ && !sees_entry(c, other.lo, j);
         for (int f = first; __ballot(asking);) {
@@ -81,7 +85,8 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
             break;
           }
           if (asking && sees_entry(c, z.lo, j)) {
-            differ = j >= z.entries || page_of(x[i]) != page_of(c.table[(size_t)f * c.table_len + min(j, c.table_len - 1)]);
+            const int theirs = c.table[(size_t)f * c.table_len + min(j, c.table_len - 1)];
+            differ = j >= z.entries || page_of(mine[min(j, most - 1)]) != page_of(theirs);
             asking = false;
           }
         }
@@ -131,8 +136,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = c.slots, per = page_blocks(c), G = c.q_per_kv;
   Runs r;
   r.a = shared; r.hi = r.a + N; r.row = r.hi + N; r.rows = r.row + N;
-  r.slot = reinterpret_cast<short *>(r.rows + N);
-  r.left = r.slot + N; r.right = r.left + N; r.same = r.right + N; r.around = r.same + N; r.worth = r.around + N; r.near = r.worth + N; r.index = r.near + N;
+  r.left = reinterpret_cast<short *>(r.rows + N);
+  r.right = r.left + N; r.around = r.right + N; r.worth = r.around + N; r.slot = r.worth + N; r.same = r.slot + N; r.near = r.same + N; r.index = r.near + N;
+  int *unit = r.rows + N;                            // of the plan's nodes, two a slot at most, once the four above are done with
   auto lo_of = [&](int k) { return max(r.hi[k] + 1 - r.rows[k], 0); };
   // sum over the threads before this one, and over all; sums are held twice, so that one barrier a call is enough
   int which = 0;
@@ -183,9 +189,21 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   for (int k = tid; k < n; k += kThreads) {
     r.same[k] = r.left[k] = r.right[k] = r.around[k] = r.worth[k] = r.near[k] = r.index[k] = -1;
     if (r.a[k] == 0) continue;
-    int i = k - 1;
-    while (r.a[i] > r.a[k]) --i;                     // (a[0] is 0)
-    r.same[k] = (short)(r.a[i] == r.a[k] ? i : k);
+    // eight at a time, to the first that is smaller; among the nearest 64, the furthest that is as large
+    int i = k - 1, same = k;
+    for (bool more = true; more;) {
+      int x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = r.a[max(i - q, 0)];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {                  // (a[0] is 0)
+        more = more && x[q] >= r.a[k];
+        same = more && x[q] == r.a[k] ? i : same;
+        i -= more;
+      }
+      more = more && (same == k || k - i < kWave);
+    }
+    r.same[k] = (short)same;
     if (r.same[k] != k) continue;
     int j = k + 1;
     for (bool more = true; more && j < n;) {         // eight at a time
@@ -214,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   auto extent = [&](int l, int e, int &lo, int &hi, int &read) {
     lo = INT_MAX; hi = -1;
     int at = l;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = l; i < e; ++i) {
       const int x = lo_of(i);
       at = x < lo ? i : at;
@@ -356,11 +374,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   // Whole chunks: their length.
   int length = max((int)((all_tiles + trunk.workers - 1) / trunk.workers), 2), chunks_of_head = 0;
   bool whole = false;
+  // a thread's first node stays in registers
+  const int columns0 = tid < all_nodes ? plan.node[(long)tid * kNodeInts + 2] * G : 0, tiles0 = tid < all_nodes ? plan.node[(long)tid * kNodeInts + 9] : 0;
   for (int turn = 0; turn < 5 && tiles; ++turn) {
     int x = 0;
     for (int i = tid; i < all_nodes; i += kThreads) {
-      const int *f = plan.node + (long)i * kNodeInts;
-      x += min((f[2] * G + kTrunkTile - 1) / kTrunkTile * (f[9] ? (f[9] + length - 1) / length : 0), 1 << 20);
+      const int *f = plan.node + (long)i * kNodeInts, columns = i == tid ? columns0 : f[2] * G, n = i == tid ? tiles0 : f[9];
+      x += min((columns + kTrunkTile - 1) / kTrunkTile * ((n + length - 1) / length), 1 << 20);
     }
     scan(x, chunks_of_head);
     const long all = (long)chunks_of_head * c.heads;
@@ -381,13 +401,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     const int pieces = i >= all_nodes ? 0 : f[9] ? (whole ? 1 : 2) * trunk.chunks(f[9]) : f[11] > 0;
     const int mine = i >= all_nodes ? 0 : whole ? (f[9] ? (f[2] * G + kTrunkTile - 1) / kTrunkTile * pieces : 0) : trunk.units(f[9], f[2] * G);
     int upto;
-    const int unit = units + scan(mine, upto);
+    const int at_unit = units + scan(mine, upto);
     units += upto;
     int all;
     const long at = columns + scan(i < all_nodes ? pieces * f[2] * G : 0, all);
     const bool fits = at + (long)pieces * f[2] * G <= most_columns;    // (it does: plan_columns)
     if (i < all_nodes) {
-      f[8] = unit;
+      f[8] = unit[i] = at_unit;
       f[10] = fits ? (int)at : -1;
       f[11] = fits ? pieces : 0;
     }
@@ -410,7 +430,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
       int low = 0;
       for (int high = all_nodes; high - low > 1;) {
         const int mid = (low + high) / 2;
-        if (plan.node[(long)mid * kNodeInts + 8] <= in_head) low = mid;
+        if (unit[mid] <= in_head) low = mid;
         else high = mid;
       }
       const int4 *f = reinterpret_cast<const int4 *>(plan.node + (long)low * kNodeInts);
