@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
   if (lane == 0) plan.apart[s] = same;
 }
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 512, kWaves = kThreads / kWave;
 // A node is worth its shares and their joining from so many tokens on, that it saves reading (tokens that it has, times slots but one).
 constexpr int kLeastSaved = 256;
 // All of them together are worth it from so many bytes on that are not read.
@@ -186,38 +186,56 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   }
   __syncthreads();
   // intervals: from the boundary to the left that is smaller (one as large: the same node as that) to the one on the right
-  for (int k = tid; k < n; k += kThreads) {
+  for (int base = wave * kWave; base < n; base += kThreads) {
+    const int k = base + lane, mine = k < n ? r.a[k] : 0;
+    // among the wave's 64, from which of them are smaller or as large, a bit each
+    unsigned smaller[2], like[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      smaller[half] = like[half] = 0;
+      for (int eight = 0; eight < 32 && half * 32 + eight < n - base; eight += 8)
+#pragma unroll
+        for (int q = eight; q < eight + 8; ++q) {
+          const int x = __builtin_amdgcn_readlane(mine, half * 32 + q);
+          smaller[half] |= (unsigned)(x < mine) << q;
+          like[half] |= (unsigned)(x == mine) << q;
+        }
+    }
+    if (k >= n) continue;
     r.same[k] = r.left[k] = r.right[k] = r.around[k] = r.worth[k] = r.near[k] = r.index[k] = -1;
-    if (r.a[k] == 0) continue;
-    // eight at a time, to the first that is smaller; among the nearest 64, the furthest that is as large
-    int i = k - 1, same = k;
-    for (bool more = true; more;) {
+    if (mine == 0) continue;
+    const unsigned long long less = (unsigned long long)smaller[1] << 32 | smaller[0], before = less & ((1ull << lane) - 1), after = less & ~((2ull << lane) - 1);
+    const int below = 63 - __clzll(before);          // (-1: none)
+    const unsigned long long equal = ((unsigned long long)like[1] << 32 | like[0]) & ((1ull << lane) - 1) & ~((1ull << (below + 1)) - 1);
+    int i = base + below, same = equal ? base + __ffsll(equal) - 1 : k;
+    // and on through those before and behind, eight at a time
+    for (bool more = same == k && !before; more;) {
       int x[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[q] = r.a[max(i - q, 0)];
 #pragma unroll
       for (int q = 0; q < 8; ++q) {                  // (a[0] is 0)
-        more = more && x[q] >= r.a[k];
-        same = more && x[q] == r.a[k] ? i : same;
+        more = more && x[q] >= mine;
+        same = more && x[q] == mine ? i : same;
         i -= more;
       }
-      more = more && (same == k || k - i < kWave);
+      more = more && same == k;
     }
     r.same[k] = (short)same;
-    if (r.same[k] != k) continue;
-    int j = k + 1;
-    for (bool more = true; more && j < n;) {         // eight at a time
+    if (same != k) continue;
+    int j = after ? base + __ffsll(after) - 1 : base + kWave;
+    for (bool more = !after; more && j < n;) {
       int x[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[q] = r.a[min(j + q, n - 1)];
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        more = more && j < n && x[q] >= r.a[k];
+        more = more && j < n && x[q] >= mine;
         j += more;
       }
     }
     r.left[k] = (short)i;
-    r.right[k] = (short)j;
+    r.right[k] = (short)min(j, n);
   }
   __syncthreads();
   for (bool more = true; more;) {                    // the chains of `same`, shortened until they have one link
@@ -241,12 +259,14 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     }
     read = r.slot[at];
   };
-  // which nodes are worth it, and what is around them
+  // which nodes are worth it, and what is around them; a thread's first node keeps its extent in registers
+  int lo0 = 0, hi0 = 0, read0 = 0;
   for (int k = tid; k < n; k += kThreads) {
     if (r.same[k] != k) continue;
     const int l = r.left[k], e = r.right[k], below = e < n ? r.a[e] : 0, from = max(r.a[l], below);
     int lo, hi, read;
     extent(l, e, lo, hi, read);
+    if (k == tid) { lo0 = lo; hi0 = hi; read0 = read; }
     const long saved = (long)seen_blocks(c, lo, hi, from * per, r.a[k] * per) * kBlock * (e - l - 1);
     if (from > 0) r.around[k] = r.same[r.a[l] >= below ? l : e];
     r.worth[k] = saved >= (least_bytes < 0 ? kLeastSaved : 1);
@@ -281,8 +301,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   for (int k = tid; k < n; k += kThreads) {
     if (r.same[k] != k || r.index[k] < 0) continue;
     const int l = r.left[k], e = r.right[k], up = r.near[k], row = r.row[l], end = r.row[e - 1] + r.rows[e - 1];
-    int lo, hi, read;
-    extent(l, e, lo, hi, read);
+    int lo = lo0, hi = hi0, read = read0;
+    if (k != tid) extent(l, e, lo, hi, read);
     // (a start that does not ascend gives a node without rows)
     const int count = end > row && (long)(end - row) * G <= (e - l) * (kTrunkTile - 1) ? end - row : 0;
     record(r.index[k], read, row, count, lo, hi, (up < 0 ? 0 : r.a[up]) * per, r.a[k] * per, up < 0 ? -1 : r.index[up]);
@@ -363,9 +383,11 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   int few_workers = 0;
   if (few_steps || short_ones) {
     unsigned best = ~0u;
-    for (int f = 32; f <= kSharedWorkers; f *= 2) {
+#pragma unroll 1
+    for (int s = 5; 1 << s <= kSharedWorkers; ++s) {
+      const int f = 1 << s;
       if (f == kSharedWorkers && tiles) break;
-      const unsigned waves = 4 * f, a = ((unsigned)short_ones * c.heads + waves - 1) / waves * 120 + (unsigned)min(few_steps * c.heads / f, 1L << 26) * 5;
+      const unsigned waves = 4 * f, a = (((unsigned)short_ones * c.heads + waves - 1) >> (s + 2)) * 120 + (unsigned)min(few_steps * c.heads >> s, 1L << 26) * 5;
       const unsigned b = tiles ? 88 + min(begun / max(kSharedWorkers - f, 8) + 1, 1u << 26) * 18 : 0, time = max(a, b);
       if (time < best) { best = time; few_workers = f; }
     }
@@ -376,6 +398,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
   bool whole = false;
   // a thread's first node stays in registers
   const int columns0 = tid < all_nodes ? plan.node[(long)tid * kNodeInts + 2] * G : 0, tiles0 = tid < all_nodes ? plan.node[(long)tid * kNodeInts + 9] : 0;
+#pragma unroll 1
   for (int turn = 0; turn < 5 && tiles; ++turn) {
     int x = 0;
     for (int i = tid; i < all_nodes; i += kThreads) {
@@ -386,7 +409,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     const long all = (long)chunks_of_head * c.heads;
     whole = all <= trunk.workers;
     if (whole) break;
-    length = (int)min(max((long)length + 1, length * all / trunk.workers), (long)kEndless);
+    length = max(length + 1, (int)min((float)length * (float)all / (float)trunk.workers, (float)kEndless));
   }
   // (else a worker's units, less what a piece costs, but no less than half of them, as there is room for so many chunks)
   const int part = (int)(begun / trunk.workers);
