@@ -401,12 +401,12 @@ int lessdec_pages_attend(const lessdec_pages_desc *desc, int32_t layer, const vo
  * lessdec_pages_attend_shared gets them, and less than 128 query columns (rows * q_per_kv) each.  With `window` pages count as far as a slot sees them.
  * least_bytes: what it has to save of a layer's reading, or nothing is shared (0: whatever there is; -1: what has been measured to pay).
  * plan: at least lessdec_pages_share_ints(desc, max_rows >= rows) ints, 16-byte aligned; what is in it is the library's own.  It
- * holds until table or length change or rows of other sizes are given (with a plan made for another number of rows nothing is
+ * holds until table or length change or rows of other sizes are given (with a plan made for another number of rows or slots nothing is
  * written).  Slots that share want neighbouring indices: what lies apart is read apart.
  *
  * lessdec_pages_attend_shared gives what lessdec_pages_attend gives, within the same bounds on its roundings (its sums are joined in another order).
  * The workspace: lessdec_pages_shared_workspace_bytes(desc, max_rows) bytes.  Where nothing is shared it costs a launch more than lessdec_pages_attend.
- * heads * (rows * q_per_kv / 32 + 2 slots) * (table_len * page_tokens / 64 + 1) < 2^31.
+ * heads * (rows * q_per_kv / 32 + 2 slots) * (table_len * page_tokens / 64 + 4) < 2^31 - 4096.
  */
 size_t lessdec_pages_share_ints(const lessdec_pages_desc *desc, int32_t max_rows);
 size_t lessdec_pages_shared_workspace_bytes(const lessdec_pages_desc *desc, int32_t max_rows);

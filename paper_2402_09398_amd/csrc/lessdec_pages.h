@@ -146,8 +146,13 @@ hipError_t launch_pages_attend(const Pages &c, int dtype, const AttendArgs &a, h
 constexpr int kPlanNodes = 0, kPlanUnits = 1, kPlanFew = 2, kPlanRows = 3, kPlanWorkers = 4, kPlanChunk = 5, kPlanShort = 6, kPlanShape = 7, kPlanHead = 8, kNodeInts = 12, kFirstInts = 20, kEndless = 1 << 30;
 constexpr int kPlanFewShift = 16;
 constexpr int kFewColumns = 16, kFewBlocks = 8;      // columns of the kernel of few rows, and its blocks a step
-constexpr int kShortBlocks = 32;                     // up to which a wave works by itself
-constexpr int kTrunkDepth = 3, kTrunkTile = 128;     // nodes around a slot; columns of a tile
+// Up to how many blocks an entry of few is a wave's by itself.  64 beams with up to 300 tokens of their own, 8 heads: 34 us a layer, 60 with 8 blocks (a
+// workgroup has an entry's beginning and end to itself), 33 with 128; but 8 slots with 100, 32 heads: 26, 26 and 50, few waves with long lists.
+constexpr int kShortBlocks = 32;
+// Nodes around a slot (instructions, a prompt, its samples' fork).  Samples of 16 prompts behind the same instructions: 39 us a layer with 3 and with 2,
+// 89 with 1.
+constexpr int kTrunkDepth = 3;
+constexpr int kTrunkTile = 128;                      // columns of a tile
 constexpr int kSharedWorkers = 512;                  // workgroups of the launch, two to a compute unit, multiples of 8 of them for either kind of work
 struct Plan {
   int *head, *node, *chain, *few, *first, *apart, *pos;

@@ -71,8 +71,8 @@ class PagedCache:
     """Owns the device buffers of a paged cache (or takes a program's own, `buffers`) and its descriptor.
 
     Plumbing only: allocation with torch, checks of tensors, pointer marshalling, no arithmetic.  dtype: "f16" or "bf16", of the
-    rows that go in and come out.  max_rows: the most rows that an attend() gets in one call.  shared: whether there is scratch for attend_shared(), too.  Calls run on the cache's device,
-    on its current stream if none is given.
+    rows that go in and come out.  max_rows: the most rows that an attend() gets in one call.  shared: whether there is scratch for
+    attend_shared(), too.  Calls run on the cache's device, on its current stream if none is given.
     """
 
     # every buffer that makes up the cache (a checkpoint copies these)
