@@ -77,19 +77,23 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
         bool differ = (apart >> i & 1) && j < most && sees_entry(c, me.lo, j);
         // where the slot before does not see the page, the last one that does is asked (rare: slots whose windows begin apart)
         bool asking = differ && !sees_entry(c, other.lo, j);
-        for (int f = first; __ballot(asking);) {
-          f = before(f);
-          const Sharer z = sharer_of(c, start, rows, max(f, 0));
-          if (f < 0 || z.entries == 0) {
-            if (asking) differ = f >= 0;             // (no one sees it; or no run reaches past that slot)
-            break;
-          }
-          if (asking && sees_entry(c, z.lo, j)) {
-            const int theirs = c.table[(size_t)f * c.table_len + min(j, c.table_len - 1)];
-            differ = j >= z.entries || page_of(mine[min(j, most - 1)]) != page_of(theirs);
-            asking = false;
+        int asked = -1;                              // it
+        for (int end = first; __ballot(asking); end -= kWave) {        // 64 slots at a time, from registers
+          const Sharer z = sharer_of(c, start, rows, max(end - 1 - lane, 0));
+          for (int l = 0; l < kWave && __ballot(asking); ++l) {
+            const int entries = __builtin_amdgcn_readlane(z.entries, l), lo = __builtin_amdgcn_readlane(z.lo, l);
+            if (end - 1 - l >= 0 && __builtin_amdgcn_readlane(z.rows.count, l) == 0) continue;
+            if (end - 1 - l < 0 || entries == 0) {
+              if (asking) differ = end - 1 - l >= 0; // (no one sees it; or no run reaches past that slot)
+              asking = false;
+            } else if (asking && sees_entry(c, lo, j)) {
+              differ = j >= entries;
+              asked = differ ? -1 : end - 1 - l;
+              asking = false;
+            }
           }
         }
+        if (asked >= 0) differ = page_of(mine[min(j, most - 1)]) != page_of(c.table[(size_t)asked * c.table_len + j]);
         const unsigned long long who = __ballot(differ);
         if (who) differs = base + i * kWave + __ffsll(who) - 1;
       }
