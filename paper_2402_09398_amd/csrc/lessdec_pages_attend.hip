@@ -199,7 +199,7 @@ __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__
 // Nodes of more than 16 columns are tiles of 128 columns by 64 tokens, as below: bound by the instruction streams where they are long, else by what a
 // piece costs beside its tiles (11 us: the plan's record, the table, keys, values, then 64 KB of sums) and by the second launch, which reads
 // the sums again.  Both kinds of work are in one launch as neither fills the chip: 64 beams of 8192 tokens, 8 heads, 4 query heads each: 27 + 7 us a layer
-// (132 apart); one document of 131072, 24 slots, 5 query heads: 101 + 9 (930 apart), 640 TFLOP/s; 32 questions of 24 tokens behind 16384, 32 heads: 285 + 23
+// (132 apart); one document of 131072, 24 slots, 5 query heads: 101 + 9 (930 apart), 640 TFLOP/s; 32 questions of 24 tokens behind 16384, 32 heads: 280 + 22
 // (785), 735 TFLOP/s; 64 samples of 16 prompts behind 1000 tokens: 34 + 6 (73).
 template <typename Args> constexpr bool kShares = false;
 template <> constexpr bool kShares<SharedArgs> = true;

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     r.right[k] = (short)min(j, n);
   }
   __syncthreads();
-  for (bool more = true; more;) {                    // the chains of `same`, shortened until they have one link
+  for (bool more = n > kWave; more;) {               // the chains of `same` across waves, shortened until they have one link
     more = false;
     for (int k = tid; k < n; k += kThreads) {
       const int x = r.same[k], y = x >= 0 ? r.same[x] : -1;            // (whichever thread goes first, y is on k's chain)
