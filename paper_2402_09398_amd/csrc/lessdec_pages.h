@@ -174,6 +174,13 @@ struct Trunk {
     const unsigned each = total / workers, more = total - each * workers;
     return w * each + (w < more ? w : more);
   }
+  // where workers have `part` units at least: those less what a piece costs, but so many that all tiles make no more than two chunks a worker, which there
+  // is room for
+  __host__ __device__ static inline int chunk_of(unsigned tiles, int part, int workers)
+  {
+    const int least = (int)((tiles + 2u * workers - 1) / (2u * workers)), most = part - kBegin;
+    return most > least ? most : least > 1 ? least : 1;
+  }
   __host__ __device__ inline int chunks(int n) const { return (n + chunk - 1) / chunk; }        // of n tiles of 128 columns
   __host__ __device__ inline int units(int n, int columns) const // of a node by a head
   {
@@ -197,7 +204,7 @@ struct Trunk {
   }
 };
 // Slots of up to 127 query columns share.  A row is in kTrunkDepth nodes and one of its own at most, each of which has room for two pieces, and
-// for as many more as chunks are (n tiles have n / chunk + 1 at most, and a chunk has at least half as many as a worker has units).
+// for as many more as chunks are (n tiles have n / chunk + 1 at most, and all tiles make two chunks a worker at most).
 inline long plan_columns(int slots, int heads, int q_per_kv, long rows)
 {
   const long n = rows * q_per_kv, most = (long)slots * kTrunkTile;

@@ -419,10 +419,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (whole) break;
     length = max(length + 1, (int)min((float)length * (float)all / (float)trunk.workers, (float)kEndless));
   }
-  // (else a worker's units, less what a piece costs, but no less than half of them, as there is room for so many chunks)
   const int part = (int)(begun / trunk.workers);
   whole = whole && length < part + kBegin;
-  trunk.chunk = whole ? length : max(max(part - kBegin, (part + 1) / 2), 1);
+  trunk.chunk = whole ? length : Trunk::chunk_of(all_tiles, part, trunk.workers);
   if (whole) trunk.workers = chunks_of_head * c.heads;
   long columns = 0;
   int units = 0;                                     // or chunks, where workers have whole ones
