@@ -25,7 +25,8 @@ typedef unsigned u4a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kRoom = 4 * kWave, kEach = kBeamTile / kWave;
 static_assert(kEach == 8, "eight logits a lane and tile");
-// Logits in [-kLeast, kFar] are taken as they are, what lies further below counts as e^-kLeast: less than e^-100 of a wave's first ones, or m is not 0.
+// Where m is 0, logits in [-kLeast, kFar] are taken as they are and what lies further below counts as e^-kLeast: less than e^-100 of one that the wave has
+// seen, as m is 0 only once there is one in [-kFar, kFar].  What comes before a wave's first logit above -inf is not in its sum at all.
 constexpr float kFar = 250.f, kLeast = 350.f;
 
 // ---- e^x in fp64 -----------------------------------------------------------------------------------------------------------
@@ -290,7 +291,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
   float seen = -__builtin_inff();                    // the lane's largest
   int tile = 0, look = 0;
   double sum = 0;
-  bool bad = false, any = false;                     // (any: a logit above -inf)
+  bool bad = false, any = false;                     // (any: a logit above -inf; until then m means nothing and the sum is 0)
   // m is 0 unless a logit lies beyond kFar, or the first ones all below -kFar
   auto reference = [&](float now) {
     now = now > -3e38f && now < 3e38f ? now : 0.f;
@@ -333,6 +334,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
       // (only now, as tokens of a tile do not come in order; those of later tiles lose a tie)
       if (best.least > 1) limit = fmaxf(limit, logit_of(best.least));
     }
+    if (!any) return;
     if (m == 0.f) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) sum += s.exponentials.of(__builtin_amdgcn_fmed3f(y[i], -kLeast, kFar));
@@ -353,7 +355,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
   }
   sum = lane_sum(sum);
   if (__ballot(bad)) sum = __builtin_nan("");
-  if (lane == 0) { s.sums[wave] = sum; s.tops[wave] = from + wave * kBeamTile < to ? m : -__builtin_inf(); }
+  if (lane == 0) { s.sums[wave] = sum; s.tops[wave] = any ? m : -__builtin_inf(); }
   join_waves(s, best);
   if (wave) return;
   u64 key;
