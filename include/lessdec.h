@@ -461,7 +461,8 @@ size_t lessdec_beam_workspace_bytes(const lessdec_beam_desc *desc);
  * Pairs of one row come in the order of their logits, then of their tokens (the lower first), those of different rows in that of c, then of their
  * beams.  What has no c above -inf is none: tokens with a logit of -inf, rows with a score of -inf, rows with a NaN among score and logits or with a
  * logit of +inf.  Where a prompt has fewer than `picks`, the rest get parent -1, token -1, -inf and 0.
- * c is formed in fp64 (its exponentials to 1e-14) and decides; next_score is c rounded once.
+ * c is formed in fp64 (its exponentials to 1e-14) and decides; next_score is c rounded once.  Logits may lie anywhere, and be masked by -inf or by any
+ * finite value, which counts as it is.
  */
 int lessdec_beam_select(const lessdec_beam_desc *desc, const void *logits, int64_t row_stride, const float *score, const uint8_t *ended,
                         int32_t *parent, int32_t *token, float *next_score, uint8_t *next_ended, void *hip_stream);

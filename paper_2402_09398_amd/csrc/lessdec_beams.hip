@@ -294,7 +294,7 @@ template <int DTYPE> __device__ inline void scan_part(const BeamArgs &a, int row
   bool bad = false, any = false;                     // (any: a logit above -inf; until then m means nothing and the sum is 0)
   // m is 0 unless a logit lies beyond kFar, or the first ones all below -kFar
   auto reference = [&](float now) {
-    now = now > -3e38f && now < 3e38f ? now : 0.f;
+    now = fabsf(now) < __builtin_inff() ? now : 0.f;                   // (else the row has no sum: `bad`)
     if (sum != 0) sum *= exp((double)m - now);
     m = now;
   };
@@ -403,12 +403,13 @@ __device__ inline void join_parts(const BeamArgs &a, int row, bool ended, Shared
   const double m = lane < a.parts ? __longlong_as_double(m_of) : -__builtin_inf(), part = lane < a.parts ? __longlong_as_double(part_of) : 0;
   double top = m;
   for (int d = 1; d < kWave; d <<= 1) top = fmax(top, __shfl_xor(top, d, kWave));
-  const double lse = top + log(lane_sum(lane < a.parts ? part * exp(m - top) : 0));
+  const double log_sum = log(lane_sum(lane < a.parts ? part * exp(m - top) : 0)), lse = top + log_sum;
+  const bool far = fabs(top) > 65536;                // where lse would lose log_sum (fp16 does not come so far)
   u64 key;
   int mark, place;
   best.rank(key, mark, place);
   if (place < a.picks) {
-    put(scores + place, key ? key_of(score + ((double)logit_of(key) - lse)) : 0);
+    put(scores + place, key ? key_of(score + (far ? (logit_of(key) - top) - log_sum : logit_of(key) - lse)) : 0);
     __hip_atomic_store(tokens + place, token_of(key), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }

@@ -1,4 +1,4 @@
-"""lessdec_beam_select on logits that lie far from 0 beside masked ones, whole tiles of them.  Adding a number to all
+"""lessdec_beam_select on logits that lie far from 0 beside masked ones, whole tiles of them: -inf, the type's lowest value, -1e4.  Adding a number to all
 logits of a row changes nothing, so the oracle of tests/beams_oracle.py gets every row less its largest logit (exact in fp64 for what decides), and the
 scores are held to half a step of fp32 (2^-24 of the value) and to 1e-11 for the sums, as in tests/test_gpu_beams.py."""
 import numpy as np
@@ -61,6 +61,38 @@ def rows_of(rows, vocab, dtype, seed, mask, value):
 def test_masked_with_infinity(dtype, rows, beams, vocab, mask):
     x, score = rows_of(rows, vocab, dtype, len(mask), MASKS[mask], -np.inf)
     check(x, score, rows // beams, beams, 2 * beams, dtype)
+
+
+@pytest.mark.parametrize("mask", ["first 512", "first 2048", "every other tile", "all but the last three", "all but the first three"])
+@pytest.mark.parametrize("rows,beams,vocab", SIZES[1:])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_masked_with_finite_values(dtype, rows, beams, vocab, mask):
+    """The type's lowest value, and one that is below most rows and above others (whose unmasked logits then weigh nothing)."""
+    import torch
+    for value in (torch.finfo(types()[dtype]).min, -5e3):
+        x, score = rows_of(rows, vocab, dtype, len(mask), MASKS[mask], value)
+        check(x, score, rows // beams, beams, 2 * beams, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_rows_of_extremes(dtype):
+    """Rows of nothing but the type's lowest or largest value (every token has the same share, the lowest tokens come first), rows that step down from
+    it, and rows of one value in one tile; masked and not."""
+    import torch
+    t, vocab = types()[dtype], 6001
+    low, high = torch.finfo(t).min, torch.finfo(t).max
+    x = torch.full((8, vocab), low, dtype=t)
+    x[1] = high
+    x[2, 4000:] = high
+    x[3, :700] = -np.inf
+    x[4, ::2] = -np.inf
+    x[5, 5999] = low / 2
+    x[6] = -np.inf
+    x[6, 1030:1050] = low
+    x[7, 3000] = 0
+    for picks in (1, 8, 64):
+        check(x.cuda(), np.linspace(-3, 0, 8), 1, 8, picks, dtype)
+        check(x.cuda(), np.linspace(0, -3, 8), 8, 1, picks, dtype)
 
 
 def test_logits_that_change_scale_within_a_row():
