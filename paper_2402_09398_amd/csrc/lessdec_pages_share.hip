@@ -5,9 +5,10 @@
 // intervals of a (from one entry that is smaller than all within to the next), nested like the forks were: a node for each.  A node covers
 // the entries from where the node around it ends up to the least a within it; what is behind a slot's innermost node is a node of its own.
 //
-// Entries count as shared where the slots that see any of the page's tokens name the same page.  Of a window's pages every slot
-// has let go what it no longer sees itself, so that one slot may name a page and the next one none; the slot whose rows lie furthest back sees all that
-// any of them sees, and its row is the one that is read for the node.
+// Entries count as shared where the slots that see any of the page's tokens name the same page.  What a slot names that it does not see says
+// nothing: it may have let go of it or not.  So neighbours are compared where both see the page, and what a slot sees and the one before it does not
+// is compared with the last slot before that which does: where these differ, they have no node with the entry, and one of the boundaries between them is
+// cut.  The slot whose rows lie furthest back sees all that any of them sees, and its row is the one that is read for the node.
 //
 // Made once a step for all layers, from a few bytes a page and slot: bound by the latency of its dependent steps.  The same tables give
 // the same plan.
@@ -28,20 +29,26 @@ __device__ inline Sharer sharer_of(const Pages &c, const int *start, int rows, i
   x.entries = x.rows.count * c.q_per_kv >= kTrunkTile ? 0 : (x.len + c.page_tokens - 1) / c.page_tokens;
   return x;
 }
-__device__ inline bool sees_entry(const Pages &c, int lo, int j)
+// the first entry behind those of the first tokens that rows from position lo on see
+__device__ inline int first_seen(const Pages &c, int lo)
 {
-  return c.window == 0 || lo < c.window || j >= (lo - c.window + 1) / c.page_tokens || (long)j * c.page_tokens < c.sinks;
+  if (c.window == 0 || lo < c.window) return 0;
+  return max((lo - c.window + 1) / c.page_tokens, (int)min(((long)c.sinks + c.page_tokens - 1) / c.page_tokens, (long)c.table_len));
 }
+__device__ inline bool sees_entry(const Pages &c, int lo, int j) { return j >= first_seen(c, lo) || (long)j * c.page_tokens < c.sinks; }
 
-// A wave for every slot: positions of its rows, and how many leading entries it shares with the slot that has rows before it.  Sixteen
-// entries a lane on their way, up to the first that differs.
+// A wave for every slot: positions of its rows, and how many leading entries it shares with the slot that has rows before it, up to the first that both
+// see and name differently, sixteen entries a lane on their way; with a window also the first that it sees and the slot before it does not, and that the last one
+// before which does names differently, and that one (of several the nearest), or -1.
 constexpr int kEach = 16;
+__device__ inline int2 *cuts_of(const Plan &plan) { return reinterpret_cast<int2 *>(plan.few); }       // (not made yet)
 __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, int rows, Plan plan)
 {
   const int s = __builtin_amdgcn_readfirstlane((blockIdx.x * 256 + threadIdx.x) / kWave), lane = threadIdx.x & 63;
   if (s >= c.slots) return;
   const Sharer me = sharer_of(c, start, rows, s);
   int same = 0;
+  int2 cut = make_int2(-1, -1);
   if (me.rows.count > 0 && me.entries > 0) {
     for (int i = lane; i < me.rows.count; i += kWave) plan.pos[me.rows.first + i] = me.len - me.rows.count + i;
     // the slot with rows before x, -1: none
@@ -74,33 +81,43 @@ __global__ __launch_bounds__(256) void agree_kernel(Pages c, const int *start, i
       int differs = most;
       for (int i = 0; i < kEach && differs == most; ++i) {
         const int j = base + i * kWave + lane;
-        bool differ = (apart >> i & 1) && j < most && sees_entry(c, me.lo, j);
-        // where the slot before does not see the page, the last one that does is asked (rare: slots whose windows begin apart)
-        bool asking = differ && !sees_entry(c, other.lo, j);
-        int asked = -1;                              // it
-        for (int end = first; __ballot(asking); end -= kWave) {        // 64 slots at a time, from registers
-          const Sharer z = sharer_of(c, start, rows, max(end - 1 - lane, 0));
-          for (int l = 0; l < kWave && __ballot(asking); ++l) {
-            const int entries = __builtin_amdgcn_readlane(z.entries, l), lo = __builtin_amdgcn_readlane(z.lo, l);
-            if (end - 1 - l >= 0 && __builtin_amdgcn_readlane(z.rows.count, l) == 0) continue;
-            if (end - 1 - l < 0 || entries == 0) {
-              if (asking) differ = end - 1 - l >= 0; // (no one sees it; or no run reaches past that slot)
-              asking = false;
-            } else if (asking && sees_entry(c, lo, j)) {
-              differ = j >= entries;
-              asked = differ ? -1 : end - 1 - l;
-              asking = false;
-            }
-          }
-        }
-        if (asked >= 0) differ = page_of(mine[min(j, most - 1)]) != page_of(c.table[(size_t)asked * c.table_len + j]);
+        const bool differ = (apart >> i & 1) && j < most && sees_entry(c, me.lo, j) && sees_entry(c, other.lo, j);
         const unsigned long long who = __ballot(differ);
         if (who) differs = base + i * kWave + __ffsll(who) - 1;
       }
       if (differs < most) { same = differs; break; }
     }
+    const int to = first < 0 ? 0 : min(first_seen(c, other.lo), same);
+    for (int base = first_seen(c, me.lo); base < to; base += kWave) {
+      const int j = base + lane;
+      bool asking = j < to;
+      int asked = -1;                                // the last slot that sees the entry, if a node could have both
+      for (int end = first; __ballot(asking); end -= kWave) {          // 64 slots at a time, from registers
+        const Sharer z = sharer_of(c, start, rows, max(end - 1 - lane, 0));
+        const int seen = first_seen(c, z.lo);
+        for (int l = 0; l < kWave && __ballot(asking); ++l) {
+          const int at = end - 1 - l, entries = __builtin_amdgcn_readlane(z.entries, l), from = __builtin_amdgcn_readlane(seen, l);
+          if (at >= 0 && __builtin_amdgcn_readlane(z.rows.count, l) == 0) continue;
+          if (at < 0 || entries == 0) {              // (no one sees it; or no run reaches past that slot)
+            asking = false;
+          } else if (asking && from <= j) {
+            if (j < entries) asked = at;
+            asking = false;
+          }
+        }
+      }
+      if (asked >= 0 && page_of(mine[j]) == page_of(c.table[(size_t)asked * c.table_len + j])) asked = -1;
+      const unsigned long long who = __ballot(asked >= 0);
+      if (!who) continue;
+      if (cut.x < 0) cut.x = base + __ffsll(who) - 1;
+      for (int d = 1; d < kWave; d <<= 1) asked = max(asked, __shfl_xor(asked, d, kWave));
+      cut.y = max(cut.y, asked);
+    }
   }
-  if (lane == 0) plan.apart[s] = same;
+  if (lane == 0) {
+    plan.apart[s] = same;
+    if (c.window > 0) cuts_of(plan)[s] = cut;
+  }
 }
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
@@ -171,6 +188,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
 
   if (tid == 0) saved_in_all = 0;
   int n = 0;
+  bool cut = false;
   for (int base = 0; base < N; base += kThreads) {
     const int s = base + tid;
     Sharer x;
@@ -179,6 +197,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     if (s < N) {
       x = sharer_of(c, start, rows, s);
       same = plan.apart[s];
+      if (c.window > 0) cut |= cuts_of(plan)[s].x >= 0;
       *reinterpret_cast<int4 *>(plan.chain + 4L * (kTrunkDepth + 1) * s) = make_int4(-1, 0, 0, 0);
     }
     int all;
@@ -192,7 +211,23 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(Pages c, const int *star
     }
     n += all;
   }
-  __syncthreads();
+  if (__syncthreads_or(cut)) {
+    // Of the boundaries between a slot and the one that it was compared with the one with the least in common is cut, unless that is no more than the entry
+    // already (of equal ones the last): most likely that between two prompts.
+    int *least = unit;                               // (what follows there is not in use yet)
+    for (int k = tid; k < n; k += kThreads) least[k] = r.a[k];
+    __syncthreads();
+    for (int k = tid; k < n; k += kThreads) {
+      const int2 x = cuts_of(plan)[r.slot[k]];
+      if (x.x < 0) continue;
+      int at = k;
+      for (int i = k - 1; i > 0 && r.slot[i] > x.y; --i) at = r.a[i] < r.a[at] ? i : at;
+      if (r.a[at] > x.x) atomicMin(least + at, x.x);
+    }
+    __syncthreads();
+    for (int k = tid; k < n; k += kThreads) r.a[k] = least[k];
+    __syncthreads();
+  }
   // intervals: from the boundary to the left that is smaller (one as large: the same node as that) to the one on the right
   for (int base = wave * kWave; base < n; base += kThreads) {
     const int k = base + lane, mine = k < n ? r.a[k] : 0;
