@@ -2,17 +2,18 @@
 //
 // With x the logits of a beam's row, c = score + (x_v - lse), lse = ln sum_v e^{x_v}.  Within a row c rises with x, so a row's best
 // pairs are its largest logits (ties: the lower token), found exactly and without any exponential; lse is only needed to compare beams.
-// It decides between them, so it is formed in fp64, like everything here that decides.
+// It decides between them, so it is formed in fp64, like everything here that decides, and so that a number added to all of a row's logits changes nothing.
 //
 // One pass over the logits.  A workgroup has a part of a row, its waves take turns at tiles of 512 logits.  A wave keeps the sum of e^{x - m},
-// where m is 0 (fp64 takes e^{+-350}) unless logits lie further out, and a list of candidates in the LDS: what is larger than a lower bound of the
+// where m is 0 (fp64 takes e^{+-350}) unless logits lie further out, from the first logit above -inf on, and a list of candidates in the LDS: what is larger than a lower bound of the
 // K-th largest so far joins it, and when it is full it is cut to the K largest.  The last workgroup of
 // a row joins the parts, the last of a prompt joins its rows, all in the one launch; every sum has an order of its own that depends on
 // sizes alone, and rows of the same logits have the same lse to the bit.
 //
 // Bound by the vector instructions of the exponentials, 18 a logit (65 us and 41 by a polynomial of degree 10 alone, 50 and 27 with remainders in fp32,
 // whose error of 1e-10 was not wanted); small calls by a chain of latencies.  64 prompts of 4 beams, 128256 logits in bfloat16: 45 us (1.5 TB/s); 16 of
-// 8, 50257 in fp32, 16 picks: 28; one of 4, 32000 in fp16: 14.
+// 8, 50257 in fp32, 16 picks: 28; one of 4, 32000 in fp16: 14.  The largest with half of the logits masked by -inf: 36, by the type's lowest value 55; with all
+// of them below -250: 73.
 #include "lessdec_beams.h"
 
 namespace lessdec {

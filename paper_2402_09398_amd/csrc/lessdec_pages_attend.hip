@@ -17,7 +17,8 @@
 // Both kernels form the scores transposed, S^T = K Q^T, with tokens along the rows of a matrix tile: a lane's accumulator
 // registers are then tokens of one query column, and just those tokens are what the lane has to bring to the second product, O^T = V^T P^T,
 // so the weights never leave their registers.  They are rounded to fp16 for it, the sum's are not: fp16 outputs are off by 2.6e-4 of their size in place of the
-// 2.1e-4 of fp32 weights and the output's own rounding, bfloat16 ones by 1.7e-3 either way (the cases of perf/operators.py).  A query column is a (row, query head of the group) pair: the heads of a group share the
+// 2.1e-4 of fp32 weights and the output's own rounding, bfloat16 ones by 1.7e-3 either way (the cases of perf/operators.py; those of perf/more_operators.py,
+// where slots share pages: 2.3e-4 to 2.9e-4, 1.7e-3).  A query column is a (row, query head of the group) pair: the heads of a group share the
 // cached keys and values that a tile has loaded.
 #include <type_traits>
 
@@ -199,8 +200,8 @@ __device__ inline float read_lane(float x, int lane) { return __uint_as_float(__
 // Nodes of more than 16 columns are tiles of 128 columns by 64 tokens, as below: bound by the instruction streams where they are long, else by what a
 // piece costs beside its tiles (11 us: the plan's record, the table, keys, values, then 64 KB of sums) and by the second launch, which reads
 // the sums again.  Both kinds of work are in one launch as neither fills the chip: 64 beams of 8192 tokens, 8 heads, 4 query heads each: 27 + 7 us a layer
-// (132 apart); one document of 131072, 24 slots, 5 query heads: 101 + 9 (930 apart), 640 TFLOP/s; 32 questions of 24 tokens behind 16384, 32 heads: 280 + 22
-// (785), 735 TFLOP/s; 64 samples of 16 prompts behind 1000 tokens: 34 + 6 (73).
+// (132 apart); one document of 131072, 24 slots, 5 query heads: 103 + 9 (930 apart), 625 TFLOP/s; 32 questions of 24 tokens behind 16384, 32 heads: 306 + 22
+// (785), 685 TFLOP/s, call by call (at clocks that have settled the pass takes 292 with its plan); 64 samples of 16 prompts behind 1000 tokens: 34 + 6 (73).
 template <typename Args> constexpr bool kShares = false;
 template <> constexpr bool kShares<SharedArgs> = true;
 

@@ -213,7 +213,8 @@ class PagedCache:
                    self._plan(plan, rows))
 
     def attend_shared(self, layer, q, out, start, max_new, plan, lse=None, stream=None):
-        """attend() that reads what slots share once for all of them; plan: of share() for these rows."""
+        """attend() that reads what slots share once for all of them; plan: of share() for these rows (with one for another number of rows, or slots, out is
+        left as it is)."""
         if not self.shared:
             raise LessdecError("attend_shared: the cache was made without shared=True")
         n, args = self._attention(layer, q, out, start, max_new, lse)
